@@ -28,7 +28,7 @@
 #include <new>
 #include <vector>
 
-#include "merak_stage.h"
+#include "abi.h"
 #include "kernels.h"
 
 using namespace merak;
@@ -205,8 +205,6 @@ WsLayout ws_layout(const Dims& D) {
   return W;
 }
 
-bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
-
 }  // namespace
 
 // ---------------------------------------------------------------------------
@@ -381,12 +379,6 @@ char* block_acts(merak_stage* S, int l, int phase) {
   if (phase == 0) return S->ws + S->W.fwd_tmp;
   return S->rc + (size_t)S->W.rc_slot[l] * S->W.act.size;
 }
-
-#define HIP_TRY(expr)                          \
-  do {                                         \
-    hipError_t e_ = (expr);                    \
-    if (e_ != hipSuccess) return MERAK_ERR_HIP; \
-  } while (0)
 
 // Run `launch` (returns hipError_t); if its kernel class is being timed, record
 // a start/stop event pair around it on `st`.
@@ -665,18 +657,6 @@ int join(merak_stage* S, hipStream_t s0, hipStream_t s1) {
   HIP_TRY(hipStreamWaitEvent(s0, S->ev_s1, 0));
   return MERAK_OK;
 }
-
-int check_ptr(const void* p) {
-  if (!p) return MERAK_ERR_INVALID_ARG;
-  if (!aligned(p, 16)) return MERAK_ERR_ALIGN;
-  return MERAK_OK;
-}
-
-#define TRY(expr)               \
-  do {                          \
-    int r_ = (expr);            \
-    if (r_ != MERAK_OK) return r_; \
-  } while (0)
 
 }  // namespace
 
