@@ -465,6 +465,110 @@ int merak_attention_bwd(int dtype, int batch, int seq, int heads, int head_dim,
                         const void* qkv, const void* o, const float* lse, const void* dout,
                         void* dqkv, float* delta, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Operators around the blocks.  Conventions as for the per-kernel entry points:
+ * caller-owned memory, 16-byte alignment, positive sizes, nothing enqueued on an
+ * argument error, no allocation.  A call reads and writes only its arguments, so
+ * calls on different streams need different outputs and scratch, and nothing
+ * else.  Deterministic (no floating-point atomics).
+ * ---------------------------------------------------------------------- */
+
+/* Element type of token ids. */
+typedef enum { MERAK_I32 = 0, MERAK_I64 = 1 } merak_id_type;
+
+/* Embedding lookup with scaling, on one tensor-parallel rank's share of the
+ * vocabulary: y[t, :] = scale * table[ids[t] - first_id, :], computed in fp32 and
+ * rounded once.  ids [tokens] of id_type; table [table_rows, hidden] and y
+ * [tokens, hidden] of dtype.  An id outside first_id .. first_id + table_rows - 1
+ * (another rank's, or padding such as -1) gives a row of zeros, so the ranks' y
+ * add up to the whole lookup.  hidden % 8 == 0 and at most 2^20; tokens and
+ * table_rows at most 2^30; first_id >= 0; scale finite. */
+int merak_embedding_fwd(int dtype, int id_type, int tokens, int hidden, int table_rows, int64_t first_id,
+                        float scale, const void* ids, const void* table, void* y, void* stream);
+
+/* Its gradient: dtable[v, :] (= or +=) scale * sum over the tokens t with ids[t] -
+ * first_id = v of dy[t, :], fp32, in one fixed order (tokens sorted by row).
+ * accumulate = 0 writes every row, zeros where no token names it; accumulate = 1
+ * leaves those rows untouched.  Ids outside the table add nothing.  scratch:
+ * merak_embedding_scratch_bytes(tokens, hidden) bytes (may be NULL when that is
+ * 0). */
+size_t merak_embedding_scratch_bytes(int tokens, int hidden);
+int merak_embedding_bwd(int dtype, int id_type, int tokens, int hidden, int table_rows, int64_t first_id,
+                        float scale, const void* ids, const void* dy, float* dtable, int accumulate,
+                        void* scratch, void* stream);
+
+/* Rotation table: table[p][i] = (cos a, sin a), a = p * theta^(-2 i / rope_dim),
+ * for p < positions and i < rope_dim / 2, evaluated in fp64 and rounded to fp32.
+ * rope_dim a multiple of 16, at most 256.  A caller with other angles (stretched
+ * positions, other frequencies) may fill a table itself. */
+int merak_rope_table(int positions, int rope_dim, double theta, float* table, void* stream);
+
+/* RMS norm of every query and key head, then rotation by the token's position, in
+ * one pass over qkv [tokens, q_heads + 2 * kv_heads, head_dim] (queries, keys,
+ * values; with q_heads = kv_heads the packed layout that the QKV GEMM writes and
+ * attention reads).  For each query and key head x:
+ *   z = gamma * x / sqrt(mean(x^2) + eps)   (q_gamma or k_gamma, [head_dim])
+ *   (a, b) -> (a cos - b sin, b cos + a sin) for the rotated pairs of z:
+ *   (z[i], z[i + rope_dim/2]), or (z[2i], z[2i+1]) when interleaved = 1,
+ *   i < rope_dim / 2; features from rope_dim on are not rotated.
+ * Values are copied.  out may be qkv itself (values are then left alone; the
+ * gradient needs the raw rows, so training keeps them) and must not overlap it
+ * otherwise.
+ *   table      [table_rows, rope_dim / 2, 2] as above; ignored if rope_dim = 0
+ *   positions  [tokens], or NULL: token t is at t % seq_len (seq_len at most
+ *              table_rows; ignored otherwise).  A position outside the table
+ *              makes the token's rotated features NaN.
+ * head_dim a multiple of 8, at most 256 (else MERAK_ERR_UNSUPPORTED); rope_dim a
+ * multiple of 16, at most head_dim; at most 4096 heads of a kind; eps > 0. */
+int merak_qk_norm_rope_fwd(int dtype, int tokens, int q_heads, int kv_heads, int head_dim, int rope_dim,
+                           int interleaved, float eps, const void* qkv, const void* q_gamma,
+                           const void* k_gamma, const float* table, int table_rows,
+                           const int32_t* positions, int seq_len, void* out, void* stream);
+
+/* Its gradient, from the gradient dout of `out` (all heads; attention's dqkv) and
+ * the raw qkv: dqkv [tokens, q_heads + 2 * kv_heads, head_dim] and the gains'
+ * gradients dq_gamma, dk_gamma fp32 [head_dim], summed over tokens and heads and
+ * written (accumulate = 0) or added (accumulate = 1).  dqkv may be dout itself (the
+ * values' gradient is then left alone) and must not overlap dout or qkv otherwise.
+ * scratch: fp32, merak_qk_norm_rope_scratch_elems(...) elements. */
+size_t merak_qk_norm_rope_scratch_elems(int tokens, int q_heads, int kv_heads, int head_dim);
+int merak_qk_norm_rope_bwd(int dtype, int tokens, int q_heads, int kv_heads, int head_dim, int rope_dim,
+                           int interleaved, float eps, const void* dout, const void* qkv,
+                           const void* q_gamma, const void* k_gamma, const float* table, int table_rows,
+                           const int32_t* positions, int seq_len, void* dqkv, float* dq_gamma,
+                           float* dk_gamma, int accumulate, float* scratch, void* stream);
+
+/* Activation checkpoints in 8 bits: x [rows, cols] (dtype) is kept as q [rows, cols],
+ * e4m3 codes (1 sign, 4 exponent, 3 fraction bits; largest value 448), and scales
+ * [rows, cols / 32], one byte b for 32 consecutive features of a row, standing for
+ * 2^(b - 127): 33 bytes for 32 values.  The scale is the smallest power of two, at
+ * least 2^-117, that brings the block's largest finite magnitude to 448 or less;
+ * values are rounded to nearest, ties to even.  A restored value is off by at most
+ * 2^-4 of itself, or by 2^-10 of the scale below 2^-6 of it.  Magnitudes
+ * above 240 * 2^120 (3.19e38) come back as that; NaN and infinities come back as NaN
+ * and do not touch their neighbours.  cols % 32 == 0. */
+int merak_act8_save(int dtype, int rows, int cols, const void* x, uint8_t* q, uint8_t* scales, void* stream);
+
+/* x from its checkpoint (exact in either dtype: 4 significant bits). */
+int merak_act8_restore(int dtype, int rows, int cols, const uint8_t* q, const uint8_t* scales, void* x,
+                       void* stream);
+
+/* GeLU (tanh form) backward from a checkpoint of its input u: du = dg * GeLU'(u)
+ * and, unless g is NULL, g = GeLU(u) again (the next layer's weight gradient needs
+ * it).  dg, du and g are [rows, cols] of dtype; du may be dg itself. */
+int merak_act8_gelu_bwd(int dtype, int rows, int cols, const void* dg, const uint8_t* q, const uint8_t* scales,
+                        void* du, void* g, void* stream);
+
+/* Weight gradient of a linear layer from a checkpoint of its input X [tokens, n_in]:
+ * dw [n_out, n_in] fp32 (= or +=) sum over tokens t of dy[t, n] X[t, m], dy [tokens,
+ * n_out] of dtype, fp32 accumulation (bf16 MFMA in MERAK_BF16 mode, to which X's
+ * restored values go unrounded).  Any number of tokens; n_out % 8 == 0, n_in % 32
+ * == 0, both at most 2^20.  scratch: merak_act8_gemm_dw_scratch_bytes(...) bytes (may be NULL
+ * when that is 0). */
+size_t merak_act8_gemm_dw_scratch_bytes(int dtype, int tokens, int n_out, int n_in);
+int merak_act8_gemm_dw(int dtype, int tokens, int n_out, int n_in, const void* dy, const uint8_t* q,
+                       const uint8_t* scales, float* dw, int accumulate, void* scratch, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

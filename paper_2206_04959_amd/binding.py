@@ -42,6 +42,7 @@ class StageConfig(ctypes.Structure):
 
 _lib = None
 _P, _I, _SZ, _F = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_float
+_L = ctypes.c_int64
 _SIGS = {
     "merak_status_str": ([_I], ctypes.c_char_p),
     "merak_stage_validate": ([ctypes.POINTER(StageConfig)], _I),
@@ -75,6 +76,19 @@ _SIGS = {
     "merak_count_nonfinite": ([_I, _P, ctypes.c_int64, _P, _P], _I),
     "merak_attention_fwd": ([_I, _I, _I, _I, _I, _P, _P, _P, _P], _I),
     "merak_attention_bwd": ([_I, _I, _I, _I, _I, _P, _P, _P, _P, _P, _P, _P], _I),
+    "merak_embedding_fwd": ([_I, _I, _I, _I, _I, _L, _F, _P, _P, _P, _P], _I),
+    "merak_embedding_scratch_bytes": ([_I, _I], _SZ),
+    "merak_embedding_bwd": ([_I, _I, _I, _I, _I, _L, _F, _P, _P, _P, _I, _P, _P], _I),
+    "merak_rope_table": ([_I, _I, ctypes.c_double, _P, _P], _I),
+    "merak_qk_norm_rope_fwd": ([_I, _I, _I, _I, _I, _I, _I, _F, _P, _P, _P, _P, _I, _P, _I, _P, _P], _I),
+    "merak_qk_norm_rope_scratch_elems": ([_I, _I, _I, _I], _SZ),
+    "merak_qk_norm_rope_bwd": ([_I, _I, _I, _I, _I, _I, _I, _F, _P, _P, _P, _P, _P, _I, _P, _I, _P, _P, _P, _I, _P,
+                                _P], _I),
+    "merak_act8_save": ([_I, _I, _I, _P, _P, _P, _P], _I),
+    "merak_act8_restore": ([_I, _I, _I, _P, _P, _P, _P], _I),
+    "merak_act8_gelu_bwd": ([_I, _I, _I, _P, _P, _P, _P, _P, _P], _I),
+    "merak_act8_gemm_dw_scratch_bytes": ([_I, _I, _I, _I], _SZ),
+    "merak_act8_gemm_dw": ([_I, _I, _I, _I, _P, _P, _P, _P, _I, _P, _P], _I),
 }
 
 
@@ -373,3 +387,234 @@ def attention_fwd(qkv, o, lse, batch, seq, heads, head_dim, stream=None) -> None
 def attention_bwd(qkv, o, lse, dout, dqkv, delta, batch, seq, heads, head_dim, stream=None) -> None:
     _check(lib().merak_attention_bwd(_dt(qkv), batch, seq, heads, head_dim, _ptr(qkv), _ptr(o), _ptr(lse),
                                      _ptr(dout), _ptr(dqkv), _ptr(delta), _stream(stream)), "merak_attention_bwd")
+
+
+# ---------------------------------------------------------------------------
+# Operators around the blocks
+# ---------------------------------------------------------------------------
+
+I32, I64 = 0, 1
+
+
+def _require(ok: bool, what: str, why: str) -> None:
+    if not ok:
+        raise ValueError(f"{what}: {why}")
+
+
+def _call(what: str, name: str, make_args, stream, **tensors) -> None:
+    """Call the entry point `name` with make_args() and the stream, after checking that the
+    tensors are dense and on one GPU.  The call goes to that GPU: its current stream
+    unless `stream` names another one of its streams."""
+    import torch
+    given = {k: t for k, t in tensors.items() if t is not None}
+    for k, t in given.items():
+        _require(t.is_contiguous(), what, f"{k} is not contiguous")
+    devices = {t.device for t in given.values()}
+    _require(len(devices) == 1 and next(iter(devices)).type == "cuda", what,
+             f"tensors are not on one GPU ({', '.join(f'{k}: {t.device}' for k, t in given.items())})")
+    device = devices.pop()
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    _require(stream.device == device, what, f"the stream is on {stream.device}, the tensors on {device}")
+    if torch.cuda.current_device() == device.index:
+        _check(getattr(lib(), name)(*make_args(), stream.cuda_stream), name)
+    else:
+        with torch.cuda.device(device):
+            _check(getattr(lib(), name)(*make_args(), stream.cuda_stream), name)
+
+
+def _element(what: str, *tensors) -> int:
+    """BF16 or FP32 of tensors that share that type."""
+    import torch
+    dt = tensors[0].dtype
+    _require(dt in (torch.bfloat16, torch.float32), what, f"element type {dt}: bf16 or fp32")
+    _require(all(t.dtype == dt for t in tensors), what, "element types differ")
+    return BF16 if dt == torch.bfloat16 else FP32
+
+
+def _scratch(what: str, scratch, nbytes: int):
+    """Pointer of a scratch tensor of at least nbytes (None if it needs none)."""
+    if nbytes == 0:
+        return None
+    _require(scratch is not None and scratch.numel() * scratch.element_size() >= nbytes, what,
+             f"scratch of {nbytes} bytes needed")
+    return scratch.data_ptr()
+
+
+def _id_type(what: str, ids) -> int:
+    import torch
+    _require(ids.dtype in (torch.int32, torch.int64), what, f"ids of type {ids.dtype}: int32 or int64")
+    return I32 if ids.dtype == torch.int32 else I64
+
+
+def embedding_fwd(ids, table, y, scale=1.0, first_id=0, stream=None) -> None:
+    """y[t] = scale * table[ids[t] - first_id]; zeros for ids outside the table's rows.
+    ids int32 or int64 of any shape, table [rows, hidden], y ids.shape + [hidden]."""
+    what = "embedding_fwd"
+    dt, it = _element(what, table, y), _id_type(what, ids)
+    _require(table.dim() == 2, what, "table is [rows, hidden]")
+    rows, hidden = table.shape
+    _require(y.numel() == ids.numel() * hidden and y.shape[-1] == hidden, what, "y is one row for each id")
+    _call(what, "merak_embedding_fwd",
+          lambda: (dt, it, ids.numel(), hidden, rows, first_id, scale, _ptr(ids), _ptr(table), _ptr(y)), stream,
+          ids=ids, table=table, y=y)
+
+
+def embedding_scratch_bytes(tokens: int, hidden: int) -> int:
+    return int(lib().merak_embedding_scratch_bytes(tokens, hidden))
+
+
+def embedding_bwd(ids, dy, dtable, scratch=None, scale=1.0, first_id=0, accumulate=False, stream=None) -> None:
+    """dtable[v] (= or +=) scale * sum of dy[t] over the tokens t with ids[t] - first_id = v;
+    dtable fp32 [rows, hidden], scratch of embedding_scratch_bytes(tokens, hidden) bytes."""
+    import torch
+    what = "embedding_bwd"
+    dt, it = _element(what, dy), _id_type(what, ids)
+    _require(dtable.dim() == 2 and dtable.dtype == torch.float32, what, "dtable is fp32 [rows, hidden]")
+    rows, hidden = dtable.shape
+    _require(dy.numel() == ids.numel() * hidden and dy.shape[-1] == hidden, what, "dy is one row for each id")
+    sp = _scratch(what, scratch, embedding_scratch_bytes(ids.numel(), hidden))
+    _call(what, "merak_embedding_bwd",
+          lambda: (dt, it, ids.numel(), hidden, rows, first_id, scale, _ptr(ids), _ptr(dy), _ptr(dtable),
+                   int(accumulate), sp), stream, ids=ids, dy=dy, dtable=dtable, scratch=scratch)
+
+
+def rope_table(table, theta=10000.0, stream=None) -> None:
+    """Fill table fp32 [positions, rope_dim / 2, 2] with the cosines and sines of
+    position * theta^(-2 i / rope_dim)."""
+    import torch
+    what = "rope_table"
+    _require(table.dim() == 3 and table.shape[2] == 2 and table.dtype == torch.float32, what,
+             "table is fp32 [positions, rope_dim / 2, 2]")
+    _call(what, "merak_rope_table", lambda: (table.shape[0], 2 * table.shape[1], theta, _ptr(table)), stream,
+          table=table)
+
+
+def _qk_args(what, qkv, q_gamma, k_gamma, table, positions, q_heads, kv_heads, seq_len, interleaved, eps):
+    """(leading arguments, table and position arguments) of the query/key norm calls."""
+    import torch
+    dt = _element(what, qkv, q_gamma, k_gamma)
+    d = q_gamma.numel()
+    _require(k_gamma.numel() == d, what, "q_gamma and k_gamma hold one head's features")
+    row = (q_heads + 2 * kv_heads) * d
+    _require(q_heads > 0 and kv_heads > 0 and row > 0 and qkv.numel() % row == 0, what,
+             "qkv is [tokens, q_heads + 2 * kv_heads, head_dim]")
+    tokens, rope, rows = qkv.numel() // row, 0, 0
+    if table is not None:
+        _require(table.dim() == 3 and table.shape[2] == 2 and table.dtype == torch.float32, what,
+                 "table is fp32 [positions, rope_dim / 2, 2]")
+        rope, rows = 2 * table.shape[1], table.shape[0]
+        if positions is not None:
+            _require(positions.dtype == torch.int32 and positions.numel() == tokens, what,
+                     "positions is int32, one for each token")
+        else:
+            _require(seq_len is not None, what, "positions or seq_len needed")
+    return ((dt, tokens, q_heads, kv_heads, d, rope, int(interleaved), eps),
+            (_ptr(table), rows, _ptr(positions), int(seq_len or 0)))
+
+
+def qk_norm_rope_fwd(qkv, q_gamma, k_gamma, table, out, q_heads, kv_heads, positions=None, seq_len=None,
+                     interleaved=False, eps=1e-6, stream=None) -> None:
+    """RMS norm of each query and key head of qkv [.., q_heads + 2 * kv_heads, head_dim] and
+    rotation by the token's position, into out (qkv itself or another tensor).  Without a
+    table the heads are only normalised; without positions token t is at t % seq_len."""
+    what = "qk_norm_rope_fwd"
+    head, tail = _qk_args(what, qkv, q_gamma, k_gamma, table, positions, q_heads, kv_heads, seq_len, interleaved, eps)
+    _element(what, qkv, out)
+    _require(out.numel() == qkv.numel(), what, "out has qkv's size")
+    _call(what, "merak_qk_norm_rope_fwd",
+          lambda: (*head, _ptr(qkv), _ptr(q_gamma), _ptr(k_gamma), *tail, _ptr(out)), stream,
+          qkv=qkv, q_gamma=q_gamma, k_gamma=k_gamma, table=table, positions=positions, out=out)
+
+
+def qk_norm_rope_scratch_elems(tokens: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
+    return int(lib().merak_qk_norm_rope_scratch_elems(tokens, q_heads, kv_heads, head_dim))
+
+
+def qk_norm_rope_bwd(dout, qkv, q_gamma, k_gamma, table, dqkv, dq_gamma, dk_gamma, scratch, q_heads, kv_heads,
+                     positions=None, seq_len=None, interleaved=False, eps=1e-6, accumulate=False,
+                     stream=None) -> None:
+    """Gradient of qk_norm_rope_fwd from the raw qkv: dqkv (dout itself or another tensor) and
+    the gains' fp32 gradients, written or added."""
+    import torch
+    what = "qk_norm_rope_bwd"
+    head, tail = _qk_args(what, qkv, q_gamma, k_gamma, table, positions, q_heads, kv_heads, seq_len, interleaved, eps)
+    _element(what, qkv, dout, dqkv)
+    _require(dout.numel() == qkv.numel() and dqkv.numel() == qkv.numel(), what, "dout and dqkv have qkv's size")
+    d = q_gamma.numel()
+    _require(all(g.dtype == torch.float32 and g.numel() == d for g in (dq_gamma, dk_gamma)), what,
+             "dq_gamma and dk_gamma are fp32 [head_dim]")
+    sp = _scratch(what, scratch, 4 * qk_norm_rope_scratch_elems(head[1], q_heads, kv_heads, d))
+    _call(what, "merak_qk_norm_rope_bwd",
+          lambda: (*head, _ptr(dout), _ptr(qkv), _ptr(q_gamma), _ptr(k_gamma), *tail, _ptr(dqkv), _ptr(dq_gamma),
+                   _ptr(dk_gamma), int(accumulate), sp), stream,
+          dout=dout, qkv=qkv, q_gamma=q_gamma, k_gamma=k_gamma, table=table, positions=positions, dqkv=dqkv,
+          dq_gamma=dq_gamma, dk_gamma=dk_gamma, scratch=scratch)
+
+
+def _act8(what, q, scales):
+    """(rows, cols) of a checkpoint."""
+    import torch
+    _require(q.dtype == torch.uint8 and scales.dtype == torch.uint8, what, "q and scales are uint8")
+    _require(q.dim() >= 1 and q.shape[-1] > 0, what, "q is [rows, cols]")
+    cols = q.shape[-1]
+    _require(cols % 32 == 0, what, f"cols {cols} is no multiple of 32")
+    _require(scales.numel() * 32 == q.numel() and scales.shape[-1] * 32 == cols, what,
+             "scales is [rows, cols / 32]")
+    return q.numel() // cols, cols
+
+
+def act8_save(x, q, scales, stream=None) -> None:
+    """Keep x [.., cols] as e4m3 codes q uint8 [.., cols] and scales uint8 [.., cols / 32]."""
+    what = "act8_save"
+    dt = _element(what, x)
+    rows, cols = _act8(what, q, scales)
+    _require(x.numel() == q.numel() and x.shape[-1] == cols, what, "x has q's shape")
+    _call(what, "merak_act8_save", lambda: (dt, rows, cols, _ptr(x), _ptr(q), _ptr(scales)), stream,
+          x=x, q=q, scales=scales)
+
+
+def act8_restore(q, scales, x, stream=None) -> None:
+    """x from its checkpoint."""
+    what = "act8_restore"
+    dt = _element(what, x)
+    rows, cols = _act8(what, q, scales)
+    _require(x.numel() == q.numel() and x.shape[-1] == cols, what, "x has q's shape")
+    _call(what, "merak_act8_restore", lambda: (dt, rows, cols, _ptr(q), _ptr(scales), _ptr(x)), stream,
+          q=q, scales=scales, x=x)
+
+
+def act8_gelu_bwd(dg, q, scales, du, g=None, stream=None) -> None:
+    """du = dg * GeLU'(u) and, if given, g = GeLU(u), with u from its checkpoint; du may be dg."""
+    what = "act8_gelu_bwd"
+    rest = (du,) if g is None else (du, g)
+    dt = _element(what, dg, *rest)
+    rows, cols = _act8(what, q, scales)
+    _require(all(t.numel() == q.numel() and t.shape[-1] == cols for t in (dg, *rest)), what,
+             "dg, du and g have q's shape")
+    _call(what, "merak_act8_gelu_bwd",
+          lambda: (dt, rows, cols, _ptr(dg), _ptr(q), _ptr(scales), _ptr(du), _ptr(g)), stream,
+          dg=dg, q=q, scales=scales, du=du, g=g)
+
+
+def act8_gemm_dw_scratch_bytes(dtype, tokens: int, n_out: int, n_in: int) -> int:
+    """dtype: the torch type of dy."""
+    import torch
+    dt = BF16 if dtype == torch.bfloat16 else FP32
+    return int(lib().merak_act8_gemm_dw_scratch_bytes(dt, tokens, n_out, n_in))
+
+
+def act8_gemm_dw(dy, q, scales, dw, scratch=None, accumulate=False, stream=None) -> None:
+    """dw [n_out, n_in] fp32 (= or +=) dy^T X, with dy [.., n_out] and X [.., n_in] from its
+    checkpoint; scratch of act8_gemm_dw_scratch_bytes(dy.dtype, tokens, n_out, n_in) bytes."""
+    import torch
+    what = "act8_gemm_dw"
+    dt = _element(what, dy)
+    tokens, n_in = _act8(what, q, scales)
+    _require(dw.dim() == 2 and dw.dtype == torch.float32 and dw.shape[1] == n_in, what, "dw is fp32 [n_out, n_in]")
+    n_out = dw.shape[0]
+    _require(dy.numel() == tokens * n_out and dy.shape[-1] == n_out, what, "dy is [tokens, n_out]")
+    sp = _scratch(what, scratch, act8_gemm_dw_scratch_bytes(dy.dtype, tokens, n_out, n_in))
+    _call(what, "merak_act8_gemm_dw",
+          lambda: (dt, tokens, n_out, n_in, _ptr(dy), _ptr(q), _ptr(scales), _ptr(dw), int(accumulate), sp), stream,
+          dy=dy, q=q, scales=scales, dw=dw, scratch=scratch)

@@ -1,0 +1,454 @@
+// Embedding lookup with scaling, and its gradient by sorted tokens.
+//
+//   y[t]  = scale * E[ids[t] - first]           (a row of zeros if that is no row of E)
+//   dE[v] (=|+=) scale * sum of dy[t] over the tokens t with ids[t] - first = v
+//
+// E is one tensor-parallel rank's share of the vocabulary (rows first ..
+// first + rows - 1), so ids of other ranks, and padding such as -1, contribute
+// nothing: the sum of the ranks' y is the whole lookup.
+//
+// Both directions move data and compute next to nothing.  The lookup reads the
+// tokens' rows and writes y.  The gradient reads dy once and writes dE once: the
+// tokens are sorted by row first (tokens of one row in their own order), so each
+// row's sum is formed in registers, in one fixed order and without
+// floating-point atomics, and rows without a token are written as zeros by the
+// same launch.
+#include <algorithm>
+
+#include "common.h"
+#include "kernels.h"
+
+namespace merak {
+
+// Row of the table that `id` names, or `rows` if none.
+template <typename I>
+__device__ __forceinline__ int table_row(I id, long long first, int rows) {
+  const unsigned long long r = (unsigned long long)(long long)id - (unsigned long long)first;
+  return r < (unsigned long long)rows ? (int)r : rows;
+}
+
+// ---------------------------------------------------------------------------
+// Forward: one 16-byte chunk of y per thread and step, consecutive threads on
+// consecutive chunks of y.
+// ---------------------------------------------------------------------------
+constexpr int kFwdUnroll = 4;
+
+template <typename T, typename I>
+__global__ void __launch_bounds__(256) embedding_fwd_kernel(int tokens, int hidden, int rows, long long first,
+                                                            float scale, const I* __restrict__ ids,
+                                                            const T* __restrict__ table, T* __restrict__ y) {
+  constexpr int EPC = 16 / sizeof(T);  // elements per chunk
+  const unsigned cpr = hidden / EPC;
+  const unsigned long long base = (unsigned long long)blockIdx.x * (256 * kFwdUnroll);
+  const unsigned t0 = (unsigned)(base / cpr), c0 = (unsigned)(base % cpr);
+  u32x4_t v[kFwdUnroll];
+  size_t at[kFwdUnroll];
+  bool live[kFwdUnroll];
+#pragma unroll
+  for (int u = 0; u < kFwdUnroll; ++u) {
+    const unsigned local = c0 + threadIdx.x + 256 * u;
+    const unsigned dt = local / cpr, c = local - dt * cpr;
+    const size_t t = (size_t)t0 + dt;
+    live[u] = t < (size_t)tokens;
+    at[u] = (t * cpr + c) * EPC;
+    v[u] = u32x4_t{0u, 0u, 0u, 0u};
+    if (live[u]) {
+      const int r = table_row(ids[t], first, rows);
+      if (r < rows) v[u] = *reinterpret_cast<const u32x4_t*>(table + ((size_t)r * cpr + c) * EPC);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kFwdUnroll; ++u) {
+    if (!live[u]) continue;
+    if constexpr (sizeof(T) == 2) {
+      float f[8];
+      unpack8(v[u], f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] *= scale;
+      store8(y + at[u], f);
+    } else {
+      const f32x4_t f = __builtin_bit_cast(f32x4_t, v[u]);
+      const float o[4] = {f[0] * scale, f[1] * scale, f[2] * scale, f[3] * scale};
+      store4(y + at[u], o);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Backward
+// ---------------------------------------------------------------------------
+constexpr int kDirect = 64;       // up to here one launch, without sorting
+constexpr int kSortBlock = 2048;  // tokens that are ranked against each other
+constexpr int kFillRows = 16;     // table rows that a workgroup clears
+constexpr int kSlab = 512;        // columns of a wave: 8 a lane
+constexpr int kMinChunk = 16, kMaxChunks = 1024;
+
+// Sorted positions per unit of work: at most kMaxChunks units, whole multiples
+// of 16 positions.
+static inline int chunk_len(int tokens) {
+  const int c = (tokens + kMaxChunks - 1) / kMaxChunks;
+  return std::max(kMinChunk, (c + 15) / 16 * 16);
+}
+
+// Rank of each token within its block of kSortBlock by (row, token): the number
+// of tokens of the block that come before it.  A workgroup ranks 64 tokens, each
+// of its four waves against a quarter of the block.  Comparing every pair is
+// kSortBlock comparisons a token with no dependence between them, in one launch;
+// 16384 tokens give every SIMD one wave.
+template <typename I>
+__global__ void __launch_bounds__(256) embedding_rank_kernel(int tokens, int rows, long long first,
+                                                             const I* __restrict__ ids, int* __restrict__ skey,
+                                                             int* __restrict__ stok) {
+  __shared__ __align__(16) unsigned key[kSortBlock];  // past the last token: above every row
+  __shared__ int cnt[4][64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int t0 = blockIdx.x * 64;                 // first token of this workgroup
+  const int b0 = t0 / kSortBlock * kSortBlock;    // first token of its block
+  const int slice = t0 - b0;
+  for (int j = threadIdx.x; j < kSortBlock; j += 256)
+    key[j] = b0 + j < tokens ? (unsigned)table_row(ids[b0 + j], first, rows) : 0xfffffffeu;
+  __syncthreads();
+  const unsigned k = key[slice + lane];
+  // tokens before the slice count if their row is not larger, tokens after it if smaller
+  constexpr int Q = kSortBlock / 4;
+  int n = 0;
+  for (int j = w * Q; j < (w + 1) * Q; j += 4) {
+    const unsigned* kj = key + j;
+    if (j < slice || j >= slice + 64) {
+      const unsigned thr = j < slice ? k + 1 : k;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) n += kj[e] < thr;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) n += kj[e] < (j + e < slice + lane ? k + 1 : k);
+    }
+  }
+  cnt[w][lane] = n;
+  __syncthreads();
+  if (w == 0 && t0 + lane < tokens) {
+    const int r = cnt[0][lane] + cnt[1][lane] + cnt[2][lane] + cnt[3][lane];
+    skey[b0 + r] = (int)k;
+    stok[b0 + r] = t0 + lane;
+  }
+}
+
+// Whole order from the sorted blocks: a token's position is the number of tokens
+// before it in each block, found by binary search.  A workgroup places 64 tokens,
+// its waves search every fourth block.
+__global__ void __launch_bounds__(256) embedding_merge_kernel(int tokens, const int* __restrict__ skey,
+                                                              const int* __restrict__ stok, int* __restrict__ gkey,
+                                                              int* __restrict__ gtok) {
+  __shared__ int cnt[4][64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int p = blockIdx.x * 64 + lane;
+  const int b = blockIdx.x * 64 / kSortBlock, nb = (tokens + kSortBlock - 1) / kSortBlock;
+  const int k = p < tokens ? skey[p] : 0;
+  int n = 0;
+  for (int o = w; o < nb; o += 4) {
+    if (o == b) {
+      n += p - b * kSortBlock;
+      continue;
+    }
+    const int* kb = skey + (size_t)o * kSortBlock;
+    const int m = min(kSortBlock, tokens - o * kSortBlock);
+    const int thr = o < b ? k + 1 : k;
+    int pos = 0;  // tokens known to come before
+#pragma unroll
+    for (int step = kSortBlock; step > 0; step >>= 1)
+      if (pos + step <= m && kb[pos + step - 1] < thr) pos += step;
+    n += pos;
+  }
+  cnt[w][lane] = n;
+  __syncthreads();
+  if (w == 0 && p < tokens) {
+    const int g = cnt[0][lane] + cnt[1][lane] + cnt[2][lane] + cnt[3][lane];
+    gkey[g] = k;
+    gtok[g] = stok[p];
+  }
+}
+
+// First sorted position whose row is not below r.
+__device__ __forceinline__ int lower_bound(const int* key, int n, int r) {
+  int lo = 0;
+  while (n > 0) {
+    const int half = n >> 1;
+    if (key[lo + half] < r) {
+      lo += half + 1;
+      n -= half + 1;
+    } else {
+      n = half;
+    }
+  }
+  return lo;
+}
+
+// 8 columns of a finished row.
+__device__ __forceinline__ void write_row(float* out, const float acc[8], float scale, int accumulate) {
+  float v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = acc[e] * scale;
+  if (accumulate) {
+    float o[8];
+    load8(out, o);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += o[e];
+  }
+  store8(out, v);
+}
+
+__device__ __forceinline__ void clear_row(float* row, int hidden, int lane) {
+  for (int c = lane * 4; c < hidden; c += 256) *reinterpret_cast<f32x4_t*>(row + c) = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+}
+
+struct EmbeddingSum {
+  int tokens, hidden, rows, chunk, accumulate;
+  float scale;
+  const int* key;   // [tokens] rows in order, `rows` for tokens without one
+  const int* tok;   // [tokens] the tokens in that order
+  float* part;      // [chunks][2][hidden]
+  float* out;       // [rows][hidden]
+  int sum_blocks;   // workgroups that sum; the rest clear rows
+};
+
+// Sums over runs of equal rows.  A wave takes `chunk` sorted positions and 512
+// columns and adds the tokens of a run in order.  A run within the chunk is
+// finished here.  Of a run that other chunks share, the chunk's part goes to
+// part[c][1] if the run begins in the chunk, else to part[c][0];
+// embedding_join_kernel adds them up.
+// The workgroups after those clear the rows that no token names.
+template <typename T>
+__global__ void __launch_bounds__(256) embedding_sum_kernel(EmbeddingSum a, const T* __restrict__ dy) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  if ((int)blockIdx.x >= a.sum_blocks) {
+    __shared__ int used[kFillRows];
+    const int r0 = (blockIdx.x - a.sum_blocks) * kFillRows;
+    if (threadIdx.x < kFillRows) {
+      const int r = r0 + threadIdx.x;
+      const int p = lower_bound(a.key, a.tokens, r);
+      used[threadIdx.x] = p < a.tokens && a.key[p] == r;
+    }
+    __syncthreads();
+    for (int i = w; i < kFillRows && r0 + i < a.rows; i += 4)
+      if (!used[i]) clear_row(a.out + (size_t)(r0 + i) * a.hidden, a.hidden, lane);
+    return;
+  }
+  const int slabs = (a.hidden + kSlab - 1) / kSlab;
+  const int unit = blockIdx.x * 4 + w;
+  const int c = unit / slabs, col = (unit % slabs) * kSlab + lane * 8;
+  const int lo = c * a.chunk, hi = min(lo + a.chunk, a.tokens);
+  if (lo >= a.tokens) return;
+  const bool live = col < a.hidden;
+  const int before = lo > 0 ? a.key[lo - 1] : -1;
+  const int after = hi < a.tokens ? a.key[hi] : -1;
+  int cur = -1;
+  float acc[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
+  float* head = a.part + ((size_t)c * 2) * a.hidden + col;
+  for (int base = lo; base < hi; base += 64) {
+    const int m = min(64, hi - base);
+    const int kk = lane < m ? a.key[base + lane] : a.rows;
+    const int tt = lane < m ? a.tok[base + lane] : 0;
+    constexpr int U = 4;
+    for (int i = 0; i < m; i += U) {
+      float v[U][8];
+      int k[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        k[u] = __builtin_amdgcn_readlane(kk, i + u);  // i + u < 64; lanes past m hold `rows`
+        const size_t t = (size_t)__builtin_amdgcn_readlane(tt, i + u);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[u][e] = 0.0f;
+        if (live && k[u] < a.rows) load8(dy + t * a.hidden + col, v[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (k[u] != cur) {
+          if (cur >= 0 && live) {
+            if (cur == before) store8(head, acc);
+            else write_row(a.out + (size_t)cur * a.hidden + col, acc, a.scale, a.accumulate);
+          }
+          cur = k[u] < a.rows ? k[u] : -1;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] += v[u][e];
+      }
+      if (k[U - 1] >= a.rows) break;  // only tokens without a row from here on
+    }
+  }
+  if (cur >= 0 && live) {
+    if (cur == before) store8(head, acc);
+    else if (cur == after) store8(head + a.hidden, acc);
+    else write_row(a.out + (size_t)cur * a.hidden + col, acc, a.scale, a.accumulate);
+  }
+}
+
+// Adds the parts of a run that spans chunks, for the chunk in which it begins:
+// four waves take every fourth part, and their sums are added in wave order.
+__global__ void __launch_bounds__(256) embedding_join_kernel(EmbeddingSum a) {
+  __shared__ float red[3][64][9];
+  const int slabs = (a.hidden + kSlab - 1) / kSlab;
+  const int c = blockIdx.x / slabs;
+  const int lo = c * a.chunk, hi = min(lo + a.chunk, a.tokens);
+  if (hi >= a.tokens) return;
+  const int k = a.key[hi - 1];
+  if (k >= a.rows || a.key[hi] != k || (lo > 0 && a.key[lo - 1] == k)) return;
+  const int end = lower_bound(a.key, a.tokens, k + 1) - 1;  // last position of the run
+  const int last = end / a.chunk;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int col = (blockIdx.x % slabs) * kSlab + lane * 8;
+  const bool live = col < a.hidden;
+  float acc[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
+  if (live) {
+#pragma unroll 4
+    for (int i = c + w; i <= last; i += 4) {
+      float v[8];
+      load8(a.part + ((size_t)i * 2 + (i == c)) * a.hidden + col, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] += v[e];
+    }
+  }
+  if (w > 0)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) red[w - 1][lane][e] = acc[e];
+  __syncthreads();
+  if (w == 0 && live) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] += red[i][lane][e];
+    write_row(a.out + (size_t)k * a.hidden + col, acc, a.scale, a.accumulate);
+  }
+}
+
+// Up to 64 tokens: every wave holds all rows in its lanes.  A wave per token and
+// 512 columns; the first token of a row adds the row's tokens in order.
+template <typename T, typename I>
+__global__ void __launch_bounds__(256) embedding_direct_kernel(EmbeddingSum a, long long first,
+                                                               const I* __restrict__ ids, const T* __restrict__ dy) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int key = lane < a.tokens ? table_row(ids[lane], first, a.rows) : a.rows;
+  if ((int)blockIdx.x >= a.sum_blocks) {
+    const int r0 = (blockIdx.x - a.sum_blocks) * kFillRows;
+    for (int i = w; i < kFillRows && r0 + i < a.rows; i += 4)
+      if (__ballot(key == r0 + i) == 0ull) clear_row(a.out + (size_t)(r0 + i) * a.hidden, a.hidden, lane);
+    return;
+  }
+  const int slabs = (a.hidden + kSlab - 1) / kSlab;
+  const int unit = blockIdx.x * 4 + w;
+  const int t = unit / slabs, col = (unit % slabs) * kSlab + lane * 8;
+  if (t >= a.tokens) return;
+  const int k = __builtin_amdgcn_readlane(key, t);
+  if (k >= a.rows) return;
+  unsigned long long run = __ballot(key == k);
+  if (__builtin_ctzll(run) != t || col >= a.hidden) return;
+  float acc[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
+  for (; run; run &= run - 1) {
+    float v[8];
+    load8(dy + (size_t)__builtin_ctzll(run) * a.hidden + col, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] += v[e];
+  }
+  write_row(a.out + (size_t)k * a.hidden + col, acc, a.scale, a.accumulate);
+}
+
+// ---------------------------------------------------------------------------
+// Host launchers
+// ---------------------------------------------------------------------------
+template <typename T, typename I>
+static hipError_t fwd_t(int tokens, int hidden, int rows, long long first, float scale, const void* ids,
+                        const void* table, void* y, hipStream_t s) {
+  const long long chunks = (long long)tokens * (hidden / (16 / (int)sizeof(T)));
+  const long long wg = (chunks + 256 * kFwdUnroll - 1) / (256 * kFwdUnroll);
+  if (wg > 0x7fffffffLL) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((embedding_fwd_kernel<T, I>), dim3((unsigned)wg), dim3(256), 0, s, tokens, hidden, rows, first,
+                     scale, (const I*)ids, (const T*)table, (T*)y);
+  return hipGetLastError();
+}
+
+hipError_t launch_embedding_fwd(int dtype, int id_type, int tokens, int hidden, int rows, long long first, float scale,
+                                const void* ids, const void* table, void* y, hipStream_t s) {
+  if (dtype == DT_BF16)
+    return id_type == ID_I32 ? fwd_t<bf16_t, int>(tokens, hidden, rows, first, scale, ids, table, y, s)
+                             : fwd_t<bf16_t, long long>(tokens, hidden, rows, first, scale, ids, table, y, s);
+  return id_type == ID_I32 ? fwd_t<float, int>(tokens, hidden, rows, first, scale, ids, table, y, s)
+                           : fwd_t<float, long long>(tokens, hidden, rows, first, scale, ids, table, y, s);
+}
+
+// Scratch: the sorted blocks' rows and tokens, the whole order's rows and
+// tokens, and the parts of runs that span chunks.
+static size_t order_bytes(int tokens) { return ((size_t)tokens * 4 + 255) / 256 * 256; }
+
+size_t embedding_scratch_bytes(int tokens, int hidden) {
+  if (tokens <= kDirect) return 0;
+  const int len = chunk_len(tokens);
+  const size_t chunks = ((size_t)tokens + len - 1) / len;
+  return 4 * order_bytes(tokens) + chunks * 2 * hidden * sizeof(float);
+}
+
+template <typename T, typename I>
+static hipError_t bwd_t(EmbeddingSum a, long long first, const void* ids, const void* dy, char* scratch,
+                        hipStream_t s) {
+  const long long slabs = (a.hidden + kSlab - 1) / kSlab;
+  const long long fill = a.accumulate ? 0 : ((long long)a.rows + kFillRows - 1) / kFillRows;
+  if (a.tokens <= kDirect) {
+    a.sum_blocks = (int)((a.tokens * slabs + 3) / 4);
+    hipLaunchKernelGGL((embedding_direct_kernel<T, I>), dim3((unsigned)(a.sum_blocks + fill)), dim3(256), 0, s, a,
+                       first, (const I*)ids, (const T*)dy);
+    return hipGetLastError();
+  }
+  const size_t ob = order_bytes(a.tokens);
+  int* gkey = (int*)scratch;
+  int* gtok = (int*)(scratch + ob);
+  int* skey = (int*)(scratch + 2 * ob);
+  int* stok = (int*)(scratch + 3 * ob);
+  const bool one = a.tokens <= kSortBlock;  // one block: its order is the whole order
+  const unsigned wg = (unsigned)(((long long)a.tokens + 63) / 64);
+  hipLaunchKernelGGL((embedding_rank_kernel<I>), dim3(wg), dim3(256), 0, s, a.tokens, a.rows, first, (const I*)ids,
+                     one ? gkey : skey, one ? gtok : stok);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (!one) {
+    hipLaunchKernelGGL(embedding_merge_kernel, dim3(wg), dim3(256), 0, s, a.tokens, skey, stok, gkey, gtok);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  a.chunk = chunk_len(a.tokens);
+  a.key = gkey;
+  a.tok = gtok;
+  a.part = (float*)(scratch + 4 * ob);
+  const long long units = (((long long)a.tokens + a.chunk - 1) / a.chunk) * slabs;
+  a.sum_blocks = (int)((units + 3) / 4);
+  hipLaunchKernelGGL(embedding_sum_kernel<T>, dim3((unsigned)(a.sum_blocks + fill)), dim3(256), 0, s, a,
+                     (const T*)dy);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(embedding_join_kernel, dim3((unsigned)units), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_embedding_bwd(int dtype, int id_type, int tokens, int hidden, int rows, long long first, float scale,
+                                const void* ids, const void* dy, float* dtable, int accumulate, void* scratch,
+                                hipStream_t s) {
+  EmbeddingSum a{};
+  a.tokens = tokens;
+  a.hidden = hidden;
+  a.rows = rows;
+  a.accumulate = accumulate;
+  a.scale = scale;
+  a.out = dtable;
+  char* sc = (char*)scratch;
+  if (dtype == DT_BF16)
+    return id_type == ID_I32 ? bwd_t<bf16_t, int>(a, first, ids, dy, sc, s)
+                             : bwd_t<bf16_t, long long>(a, first, ids, dy, sc, s);
+  return id_type == ID_I32 ? bwd_t<float, int>(a, first, ids, dy, sc, s)
+                           : bwd_t<float, long long>(a, first, ids, dy, sc, s);
+}
+
+}  // namespace merak

@@ -130,4 +130,47 @@ hipError_t launch_attention_fwd_d128(int B, int S, int H, int G, int mstride, co
 hipError_t launch_attention_bwd_d128(int B, int S, int H, int G, int mstride, const void* qkv, const void* o,
                                      const float* lse, const void* dout, void* dqkv, float* delta, hipStream_t st);
 
+// Element type of token ids.
+enum IdType { ID_I32 = 0, ID_I64 = 1 };
+
+// Embedding lookup and its gradient (embedding.hip).  scratch of the gradient:
+// embedding_scratch_bytes (0 for short calls, scratch may then be null).
+hipError_t launch_embedding_fwd(int dtype, int id_type, int tokens, int hidden, int rows, long long first, float scale,
+                                const void* ids, const void* table, void* y, hipStream_t stream);
+size_t embedding_scratch_bytes(int tokens, int hidden);
+hipError_t launch_embedding_bwd(int dtype, int id_type, int tokens, int hidden, int rows, long long first, float scale,
+                                const void* ids, const void* dy, float* dtable, int accumulate, void* scratch,
+                                hipStream_t stream);
+
+// Query/key norm with position rotation (qk_norm_rope.hip) on rows
+// [q_heads | kv_heads keys | kv_heads values][head_dim].
+struct QkShape {
+  int tokens, q_heads, kv_heads, head_dim;
+  int rope_dim, interleaved;
+  float eps;
+  const float* table;    // [table_rows][rope_dim / 2][2], null when rope_dim = 0
+  int table_rows;
+  const int* positions;  // [tokens], or null: token t is at t % seq_len
+  int seq_len;
+};
+hipError_t launch_rope_table(int positions, int rope_dim, double theta, float* table, hipStream_t stream);
+hipError_t launch_qk_norm_rope_fwd(int dtype, const QkShape& q, const void* in, const void* gq, const void* gk,
+                                   void* out, hipStream_t stream);
+size_t qk_norm_rope_scratch_elems(int tokens, int q_heads, int kv_heads, int head_dim);
+hipError_t launch_qk_norm_rope_bwd(int dtype, const QkShape& q, const void* dout, const void* in, const void* gq,
+                                   const void* gk, void* dx, float* dgq, float* dgk, int accumulate, float* part,
+                                   hipStream_t stream);
+
+// Activation checkpoints in 8 bits (act8.hip): codes q [rows][cols], scales
+// [rows][cols / 32]; cols % 32 == 0.
+hipError_t launch_act8_save(int dtype, int rows, int cols, const void* x, uint8_t* q, uint8_t* scales,
+                            hipStream_t stream);
+hipError_t launch_act8_restore(int dtype, int rows, int cols, const uint8_t* q, const uint8_t* scales, void* x,
+                               hipStream_t stream);
+hipError_t launch_act8_gelu_bwd(int dtype, int rows, int cols, const void* dg, const uint8_t* q, const uint8_t* scales,
+                                void* du, void* g, hipStream_t stream);
+size_t act8_gemm_dw_scratch_bytes(int dtype, int tokens, int n_out, int n_in);
+hipError_t launch_act8_gemm_dw(int dtype, int tokens, int n_out, int n_in, const void* dy, const uint8_t* q,
+                               const uint8_t* scales, float* dw, int accumulate, void* scratch, hipStream_t stream);
+
 }  // namespace merak
