@@ -401,50 +401,65 @@ def _require(ok: bool, what: str, why: str) -> None:
         raise ValueError(f"{what}: {why}")
 
 
-def _call(what: str, name: str, make_args, stream, **tensors) -> None:
-    """Call the entry point `name` with make_args() and the stream, after checking that the
-    tensors are dense and on one GPU.  The call goes to that GPU: its current stream
-    unless `stream` names another one of its streams."""
+def _call(what: str, fn: str, args, stream, names: str, *tensors) -> None:
+    """Call the entry point fn(*args, stream) after checking that the tensors (None: not given)
+    are dense and on one GPU.  The call goes to that GPU: its current stream unless `stream`
+    names another one of its streams.  (The checks cost a few tenths of a microsecond a tensor:
+    of a short call's time the host's part is the larger.)"""
     import torch
-    given = {k: t for k, t in tensors.items() if t is not None}
-    for k, t in given.items():
-        _require(t.is_contiguous(), what, f"{k} is not contiguous")
-    devices = {t.device for t in given.values()}
-    _require(len(devices) == 1 and next(iter(devices)).type == "cuda", what,
-             f"tensors are not on one GPU ({', '.join(f'{k}: {t.device}' for k, t in given.items())})")
-    device = devices.pop()
+    index = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and (t.get_device() != index or index < 0 or not t.is_contiguous()):
+            for name, u in zip(names.split(), tensors):
+                _require(u is None or u.is_contiguous(), what, f"{name} is not contiguous")
+            where = (f"{name}: {u.device}" for name, u in zip(names.split(), tensors) if u is not None)
+            raise ValueError(f"{what}: tensors are not on one GPU ({', '.join(where)})")
     if stream is None:
-        stream = torch.cuda.current_stream(device)
-    _require(stream.device == device, what, f"the stream is on {stream.device}, the tensors on {device}")
-    if torch.cuda.current_device() == device.index:
-        _check(getattr(lib(), name)(*make_args(), stream.cuda_stream), name)
+        handle = torch._C._cuda_getCurrentRawStream(index)  # a fifteenth of torch.cuda.current_stream's time
     else:
-        with torch.cuda.device(device):
-            _check(getattr(lib(), name)(*make_args(), stream.cuda_stream), name)
+        if stream.device.index != index:
+            raise ValueError(f"{what}: the stream is on {stream.device}, the tensors on cuda:{index}")
+        handle = stream.cuda_stream
+    entry = getattr(lib(), fn)
+    if torch.cuda.current_device() == index:
+        status = entry(*args, handle)
+    else:
+        with torch.cuda.device(index):
+            status = entry(*args, handle)
+    if status:
+        raise MerakError(status, fn)
 
 
 def _element(what: str, *tensors) -> int:
     """BF16 or FP32 of tensors that share that type."""
     import torch
     dt = tensors[0].dtype
-    _require(dt in (torch.bfloat16, torch.float32), what, f"element type {dt}: bf16 or fp32")
-    _require(all(t.dtype == dt for t in tensors), what, "element types differ")
-    return BF16 if dt == torch.bfloat16 else FP32
+    for t in tensors:
+        if t.dtype is not dt:
+            raise ValueError(f"{what}: element types differ")
+    if dt is torch.bfloat16:
+        return BF16
+    if dt is torch.float32:
+        return FP32
+    raise ValueError(f"{what}: element type {dt}: bf16 or fp32")
 
 
 def _scratch(what: str, scratch, nbytes: int):
     """Pointer of a scratch tensor of at least nbytes (None if it needs none)."""
     if nbytes == 0:
         return None
-    _require(scratch is not None and scratch.numel() * scratch.element_size() >= nbytes, what,
-             f"scratch of {nbytes} bytes needed")
+    if scratch is None or scratch.numel() * scratch.element_size() < nbytes:
+        raise ValueError(f"{what}: scratch of {nbytes} bytes needed")
     return scratch.data_ptr()
 
 
 def _id_type(what: str, ids) -> int:
     import torch
-    _require(ids.dtype in (torch.int32, torch.int64), what, f"ids of type {ids.dtype}: int32 or int64")
-    return I32 if ids.dtype == torch.int32 else I64
+    if ids.dtype is torch.int64:
+        return I64
+    if ids.dtype is torch.int32:
+        return I32
+    raise ValueError(f"{what}: ids of type {ids.dtype}: int32 or int64")
 
 
 def embedding_fwd(ids, table, y, scale=1.0, first_id=0, stream=None) -> None:
@@ -455,9 +470,9 @@ def embedding_fwd(ids, table, y, scale=1.0, first_id=0, stream=None) -> None:
     _require(table.dim() == 2, what, "table is [rows, hidden]")
     rows, hidden = table.shape
     _require(y.numel() == ids.numel() * hidden and y.shape[-1] == hidden, what, "y is one row for each id")
-    _call(what, "merak_embedding_fwd",
-          lambda: (dt, it, ids.numel(), hidden, rows, first_id, scale, _ptr(ids), _ptr(table), _ptr(y)), stream,
-          ids=ids, table=table, y=y)
+    _call(what, "merak_embedding_fwd", (dt, it, ids.numel(), hidden, rows, first_id, scale, _ptr(ids), _ptr(table),
+          _ptr(y)),
+          stream, "ids table y", ids, table, y)
 
 
 def embedding_scratch_bytes(tokens: int, hidden: int) -> int:
@@ -474,9 +489,9 @@ def embedding_bwd(ids, dy, dtable, scratch=None, scale=1.0, first_id=0, accumula
     rows, hidden = dtable.shape
     _require(dy.numel() == ids.numel() * hidden and dy.shape[-1] == hidden, what, "dy is one row for each id")
     sp = _scratch(what, scratch, embedding_scratch_bytes(ids.numel(), hidden))
-    _call(what, "merak_embedding_bwd",
-          lambda: (dt, it, ids.numel(), hidden, rows, first_id, scale, _ptr(ids), _ptr(dy), _ptr(dtable),
-                   int(accumulate), sp), stream, ids=ids, dy=dy, dtable=dtable, scratch=scratch)
+    _call(what, "merak_embedding_bwd", (dt, it, ids.numel(), hidden, rows, first_id, scale, _ptr(ids), _ptr(dy),
+          _ptr(dtable), int(accumulate), sp),
+          stream, "ids dy dtable scratch", ids, dy, dtable, scratch)
 
 
 def rope_table(table, theta=10000.0, stream=None) -> None:
@@ -486,8 +501,8 @@ def rope_table(table, theta=10000.0, stream=None) -> None:
     what = "rope_table"
     _require(table.dim() == 3 and table.shape[2] == 2 and table.dtype == torch.float32, what,
              "table is fp32 [positions, rope_dim / 2, 2]")
-    _call(what, "merak_rope_table", lambda: (table.shape[0], 2 * table.shape[1], theta, _ptr(table)), stream,
-          table=table)
+    _call(what, "merak_rope_table", (table.shape[0], 2 * table.shape[1], theta, _ptr(table)),
+          stream, "table", table)
 
 
 def _qk_args(what, qkv, q_gamma, k_gamma, table, positions, q_heads, kv_heads, seq_len, interleaved, eps):
@@ -522,9 +537,8 @@ def qk_norm_rope_fwd(qkv, q_gamma, k_gamma, table, out, q_heads, kv_heads, posit
     head, tail = _qk_args(what, qkv, q_gamma, k_gamma, table, positions, q_heads, kv_heads, seq_len, interleaved, eps)
     _element(what, qkv, out)
     _require(out.numel() == qkv.numel(), what, "out has qkv's size")
-    _call(what, "merak_qk_norm_rope_fwd",
-          lambda: (*head, _ptr(qkv), _ptr(q_gamma), _ptr(k_gamma), *tail, _ptr(out)), stream,
-          qkv=qkv, q_gamma=q_gamma, k_gamma=k_gamma, table=table, positions=positions, out=out)
+    _call(what, "merak_qk_norm_rope_fwd", (*head, _ptr(qkv), _ptr(q_gamma), _ptr(k_gamma), *tail, _ptr(out)),
+          stream, "qkv q_gamma k_gamma table positions out", qkv, q_gamma, k_gamma, table, positions, out)
 
 
 def qk_norm_rope_scratch_elems(tokens: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
@@ -545,11 +559,10 @@ def qk_norm_rope_bwd(dout, qkv, q_gamma, k_gamma, table, dqkv, dq_gamma, dk_gamm
     _require(all(g.dtype == torch.float32 and g.numel() == d for g in (dq_gamma, dk_gamma)), what,
              "dq_gamma and dk_gamma are fp32 [head_dim]")
     sp = _scratch(what, scratch, 4 * qk_norm_rope_scratch_elems(head[1], q_heads, kv_heads, d))
-    _call(what, "merak_qk_norm_rope_bwd",
-          lambda: (*head, _ptr(dout), _ptr(qkv), _ptr(q_gamma), _ptr(k_gamma), *tail, _ptr(dqkv), _ptr(dq_gamma),
-                   _ptr(dk_gamma), int(accumulate), sp), stream,
-          dout=dout, qkv=qkv, q_gamma=q_gamma, k_gamma=k_gamma, table=table, positions=positions, dqkv=dqkv,
-          dq_gamma=dq_gamma, dk_gamma=dk_gamma, scratch=scratch)
+    _call(what, "merak_qk_norm_rope_bwd", (*head, _ptr(dout), _ptr(qkv), _ptr(q_gamma), _ptr(k_gamma), *tail,
+          _ptr(dqkv), _ptr(dq_gamma), _ptr(dk_gamma), int(accumulate), sp),
+          stream, "dout qkv q_gamma k_gamma table positions dqkv dq_gamma dk_gamma scratch",
+          dout, qkv, q_gamma, k_gamma, table, positions, dqkv, dq_gamma, dk_gamma, scratch)
 
 
 def _act8(what, q, scales):
@@ -558,7 +571,7 @@ def _act8(what, q, scales):
     _require(q.dtype == torch.uint8 and scales.dtype == torch.uint8, what, "q and scales are uint8")
     _require(q.dim() >= 1 and q.shape[-1] > 0, what, "q is [rows, cols]")
     cols = q.shape[-1]
-    _require(cols % 32 == 0, what, f"cols {cols} is no multiple of 32")
+    _require(cols % 32 == 0, what, "cols is a multiple of 32")
     _require(scales.numel() * 32 == q.numel() and scales.shape[-1] * 32 == cols, what,
              "scales is [rows, cols / 32]")
     return q.numel() // cols, cols
@@ -570,8 +583,8 @@ def act8_save(x, q, scales, stream=None) -> None:
     dt = _element(what, x)
     rows, cols = _act8(what, q, scales)
     _require(x.numel() == q.numel() and x.shape[-1] == cols, what, "x has q's shape")
-    _call(what, "merak_act8_save", lambda: (dt, rows, cols, _ptr(x), _ptr(q), _ptr(scales)), stream,
-          x=x, q=q, scales=scales)
+    _call(what, "merak_act8_save", (dt, rows, cols, _ptr(x), _ptr(q), _ptr(scales)),
+          stream, "x q scales", x, q, scales)
 
 
 def act8_restore(q, scales, x, stream=None) -> None:
@@ -580,8 +593,8 @@ def act8_restore(q, scales, x, stream=None) -> None:
     dt = _element(what, x)
     rows, cols = _act8(what, q, scales)
     _require(x.numel() == q.numel() and x.shape[-1] == cols, what, "x has q's shape")
-    _call(what, "merak_act8_restore", lambda: (dt, rows, cols, _ptr(q), _ptr(scales), _ptr(x)), stream,
-          q=q, scales=scales, x=x)
+    _call(what, "merak_act8_restore", (dt, rows, cols, _ptr(q), _ptr(scales), _ptr(x)),
+          stream, "q scales x", q, scales, x)
 
 
 def act8_gelu_bwd(dg, q, scales, du, g=None, stream=None) -> None:
@@ -592,9 +605,8 @@ def act8_gelu_bwd(dg, q, scales, du, g=None, stream=None) -> None:
     rows, cols = _act8(what, q, scales)
     _require(all(t.numel() == q.numel() and t.shape[-1] == cols for t in (dg, *rest)), what,
              "dg, du and g have q's shape")
-    _call(what, "merak_act8_gelu_bwd",
-          lambda: (dt, rows, cols, _ptr(dg), _ptr(q), _ptr(scales), _ptr(du), _ptr(g)), stream,
-          dg=dg, q=q, scales=scales, du=du, g=g)
+    _call(what, "merak_act8_gelu_bwd", (dt, rows, cols, _ptr(dg), _ptr(q), _ptr(scales), _ptr(du), _ptr(g)),
+          stream, "dg q scales du g", dg, q, scales, du, g)
 
 
 def act8_gemm_dw_scratch_bytes(dtype, tokens: int, n_out: int, n_in: int) -> int:
@@ -615,6 +627,6 @@ def act8_gemm_dw(dy, q, scales, dw, scratch=None, accumulate=False, stream=None)
     n_out = dw.shape[0]
     _require(dy.numel() == tokens * n_out and dy.shape[-1] == n_out, what, "dy is [tokens, n_out]")
     sp = _scratch(what, scratch, act8_gemm_dw_scratch_bytes(dy.dtype, tokens, n_out, n_in))
-    _call(what, "merak_act8_gemm_dw",
-          lambda: (dt, tokens, n_out, n_in, _ptr(dy), _ptr(q), _ptr(scales), _ptr(dw), int(accumulate), sp), stream,
-          dy=dy, q=q, scales=scales, dw=dw, scratch=scratch)
+    _call(what, "merak_act8_gemm_dw", (dt, tokens, n_out, n_in, _ptr(dy), _ptr(q), _ptr(scales), _ptr(dw),
+          int(accumulate), sp),
+          stream, "dy q scales dw scratch", dy, q, scales, dw, scratch)

@@ -13,6 +13,7 @@
 // has 4 significant bits, so it is exact in bf16 too: the bf16 matrix instruction
 // takes it as it is.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
 #include "common.h"
@@ -60,6 +61,17 @@ __device__ __forceinline__ void decode4(uint32_t q, float scale, float v[4]) {
   v[3] = hi[1] * scale;
 }
 
+// Two codes of a word as bf16 (exact).
+template <bool HI>
+__device__ __forceinline__ uint32_t decode2_bf16(uint32_t w, float scale) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, HI));
+}
+
+__device__ __forceinline__ u32x4_t decode8_bf16(uint32_t lo, uint32_t hi, float scale) {
+  return u32x4_t{decode2_bf16<false>(lo, scale), decode2_bf16<true>(lo, scale), decode2_bf16<false>(hi, scale),
+                 decode2_bf16<true>(hi, scale)};
+}
+
 // Scale from its byte (10 .. 247 in a saved checkpoint).
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
@@ -91,10 +103,14 @@ __global__ void __launch_bounds__(256) act8_restore_kernel(long long chunks, con
   if (i >= chunks) return;
   const u32x2_t c = *reinterpret_cast<const u32x2_t*>(q + i * 8);
   const float s = scale_of(scales[i >> 2]);
-  float v[8];
-  decode4(c[0], s, v);
-  decode4(c[1], s, v + 4);
-  store8(x + i * 8, v);
+  if constexpr (sizeof(T) == 2) {
+    *reinterpret_cast<u32x4_t*>(x + i * 8) = decode8_bf16(c[0], c[1], s);
+  } else {
+    float v[8];
+    decode4(c[0], s, v);
+    decode4(c[1], s, v + 4);
+    store8(x + i * 8, v);
+  }
 }
 
 // GeLU (tanh form) and its derivative with s = sigmoid(w), w = 2 sqrt(2/pi) (u +
@@ -138,106 +154,244 @@ __global__ void __launch_bounds__(256) act8_gelu_bwd_kernel(long long chunks, co
 // ---------------------------------------------------------------------------
 // Weight gradient dW[n, m] (=|+=) sum over tokens t of dY[t, n] X[t, m], X in 8 bits.
 //
-// bf16: both operands are staged in LDS as they lie in memory, tokens by features,
-// and read by the transposing LDS read, as in the weight-gradient GEMM of gemm.hip;
-// X's codes become bf16 on the way into LDS.
+// bf16: v_mfma_f32_32x32x16_bf16, fp32 accumulators, 64 tokens a stage, two LDS
+// buffers.  Both operands lie in LDS as in memory, tokens by features (swizzled, see
+// gemm.hip), and are read by the transposing LDS read.  dY goes global -> LDS
+// directly.  X's codes go to registers a stage ahead, 16 codes of one scale block at
+// a time, and become bf16 on the way into LDS: eight conversions that take the scale
+// along for 16 values.  Converting there costs each value one conversion in a
+// workgroup; behind LDS every wave that shares a column would convert it again.
+//
+// Stage kt + 2 is filled in behind the barrier at the end of stage kt's reads, its
+// pieces (dY load, conversion and LDS write, load of stage kt + 3's codes) between
+// the MFMAs of the last sub-step.  Every wait is for the loads of a whole stage ago.
+// Buffers are addressed from each stage's first token, so operands may be of any
+// size; tokens past the end read as zeros.
 // ---------------------------------------------------------------------------
-constexpr int kDwTile = 128;
+struct DwArgs {
+  int tokens, n_out, n_in;
+  int per_split;  // tokens of a split, a multiple of 64 (or all)
+  int tiles;      // output tiles of a split
+  int accumulate;
+  const bf16_t* dy;
+  const uint8_t* q;
+  const uint8_t* scales;
+  float* out;     // splits = 1: dw; else the splits' sums [splits][n_out][n_in]
+};
 
-// 16 codes of one scale block as 16 bf16 values (exact).
-__device__ __forceinline__ void decode16(u32x4_t c, float scale, u32x4_t out[2]) {
-  float v[4];
+// Raw buffer of `rows` rows of `ld` bytes from p, empty if rows <= 0.
+__device__ __forceinline__ i32x4_t stage_rsrc(const void* p, int rows, size_t ld) {
+  return operand_rsrc_words(p, rows > 0 ? (uint32_t)(min(rows, kBK) * ld) : 0u);
+}
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t stage_buffer(const void* p, int rows, size_t ld) {
+  return operand_rsrc(p, rows > 0 ? (uint32_t)(min(rows, kBK) * ld) : 0u);
+}
+
+template <int BM, int BN, int WM, int WN>
+__global__ void __launch_bounds__(WM * WN * 64) act8_dw_kernel(DwArgs p) {
+  constexpr int NW = WM * WN, NT = NW * 64;
+  constexpr int WTM = BM / WM, WTN = BN / WN, TM = WTM / 32, TN = WTN / 32;
+  constexpr int A_BYTES = BM * 128, STAGE = (BM + BN) * 128;
+  constexpr int LA = BM / 8 / NW;         // dY loads of a wave and stage
+  constexpr int LB = BN * kBK / 16 / NT;  // runs of 16 codes of a thread and stage
+  constexpr int RPR = BN / 16, CPR = BN / 8;
+  extern __shared__ __align__(16) char smem[];
+
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / WN, wn = wave % WN;
+  // Each XCD takes neighbouring tiles, in groups of four tile rows.
+  const int id = xcd_remap(blockIdx.x, gridDim.x);
+  const int split = id / p.tiles, tile = id - split * p.tiles;
+  const int tiles_m = (p.n_out + BM - 1) / BM, tiles_n = (p.n_in + BN - 1) / BN;
+  constexpr int GM = 4;
+  const int group = tile / (GM * tiles_n), first_m = group * GM;
+  const int gsz = min(tiles_m - first_m, GM), in_group = tile - group * GM * tiles_n;
+  const int m0 = (first_m + in_group % gsz) * BM, n0 = (in_group / gsz) * BN;
+
+  const int k0 = split * p.per_split;
+  const int rows = min(p.per_split, p.tokens - k0);
+  const int KT = (rows + kBK - 1) / kBK;
+  const size_t lda = (size_t)p.n_out * 2, ldq = p.n_in, lds = p.n_in / kScaleBlock;
+  const char* pa = reinterpret_cast<const char*>(p.dy) + (size_t)k0 * lda;
+  const uint8_t* pq = p.q + (size_t)k0 * ldq;
+  const uint8_t* ps = p.scales + (size_t)k0 * lds;
+
+  TileLoader<true, BM, NW> la;
+  la.init(m0, p.n_out, wave, lane);
+  la.step = 0;  // the buffer's start moves instead
+  uint32_t qoff[LB], soff[LB], w0[LB];
+  bool swap[LB];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    decode4(c[i], scale, v);
-    out[i >> 1][2 * (i & 1)] = pack_bf16x2(v[0], v[1]);
-    out[i >> 1][2 * (i & 1) + 1] = pack_bf16x2(v[2], v[3]);
+  for (int u = 0; u < LB; ++u) {
+    const int i = threadIdx.x + NT * u, kr = i / RPR, run = i % RPR;
+    qoff[u] = (uint32_t)(kr * p.n_in + n0 + run * 16);
+    soff[u] = (uint32_t)(kr * (p.n_in / kScaleBlock) + (n0 + run * 16) / kScaleBlock);
+    // The run's two 16-byte chunks are neighbours in LDS; lanes 8 runs on write theirs in
+    // the other order, so that 16 lanes cover all 64 banks.
+    swap[u] = (run >> 3) & 1;
+    w0[u] = (uint32_t)(A_BYTES + kr * 2 * BN + ((run * 2 + 4 * (kr & 3)) % CPR) * 16);
+  }
+  FragReader<true, BM> fa;
+  FragReader<true, BN> fb;
+  fa.init(lane);
+  fb.init(lane);
+
+  f32x16_t acc[TN][TM];
+#pragma unroll
+  for (int j = 0; j < TN; ++j)
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[j][i][e] = 0.0f;
+
+  u32x4_t raw[LB];
+  uint32_t rs[LB];
+  bf16x8_t a0[TM], a1[TM], b0[TN], b1[TN];
+  auto load_codes = [&](int kt, int u) {  // run u of stage kt
+    const int left = rows - kt * kBK;
+    const __amdgpu_buffer_rsrc_t rq = stage_buffer(pq + (size_t)kt * kBK * ldq, left, ldq);
+    const __amdgpu_buffer_rsrc_t rc = stage_buffer(ps + (size_t)kt * kBK * lds, left, lds);
+    raw[u] = __builtin_amdgcn_raw_buffer_load_b128(rq, qoff[u], 0, 0);
+    rs[u] = __builtin_amdgcn_raw_buffer_load_b8(rc, soff[u], 0, 0);
+  };
+  auto write_codes = [&](char* st, int u, int half) {  // chunk `half` (in this lane's order) of run u
+    const float sc = scale_of(rs[u]);
+    const bool second = half ? !swap[u] : swap[u];
+    const u32x4_t v = decode8_bf16(second ? raw[u][2] : raw[u][0], second ? raw[u][3] : raw[u][1], sc);
+    *reinterpret_cast<u32x4_t*>(st + w0[u] + (second ? 16 : 0)) = v;
+  };
+  auto dy_rsrc = [&](int kt) { return stage_rsrc(pa + (size_t)kt * kBK * lda, rows - kt * kBK, lda); };
+  auto read_frags = [&](const char* st, int ks, bf16x8_t (&a)[TM], bf16x8_t (&b)[TN]) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i) a[i] = fa.read(st, wm * WTM + i * 32, ks);
+#pragma unroll
+    for (int j = 0; j < TN; ++j) b[j] = fb.read(st + A_BYTES, wn * WTN + j * 32, ks);
+  };
+  constexpr int NMF = TM * TN, NRD = 2 * (TM + TN), NIL = NRD > NMF ? NRD : NMF;
+  // reads of (st, ks) into set n, interleaved with the MFMAs of set c
+  auto step = [&](const char* st, int ks, bf16x8_t (&na)[TM], bf16x8_t (&nb)[TN], const bf16x8_t (&ca)[TM],
+                  const bf16x8_t (&cb)[TN]) {
+    read_frags(st, ks, na, nb);
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+        acc[j][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cb[j], ca[i], acc[j][i], 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < NIL; ++i) {
+      if (i < NMF) __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // one MFMA
+      if (i < NRD) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // one LDS read
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    char* st = smem + s * STAGE;
+#pragma unroll
+    for (int u = 0; u < LB; ++u) load_codes(s, u);
+    la.issue(dy_rsrc(s), st, wave);
+#pragma unroll
+    for (int u = 0; u < LB; ++u) {
+      write_codes(st, u, 0);
+      write_codes(st, u, 1);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < LB; ++u) load_codes(2, u);
+  wait_vm_barrier<0>();
+  read_frags(smem, 0, a0, b0);
+  __builtin_amdgcn_sched_barrier(0);
+
+  // Past the last stage the loads find empty buffers: they fetch nothing and write zeros.
+  for (int kt = 0; kt < KT; ++kt) {
+    char* st = smem + (kt & 1) * STAGE;
+    step(st, 1, a1, b1, a0, b0);
+    step(st, 2, a0, b0, a1, b1);
+    step(st, 3, a1, b1, a0, b0);
+    wait_vm_barrier<0>();  // stage kt + 1 is in LDS, the codes of kt + 2 in registers; all have read stage kt
+    const i32x4_t ra = dy_rsrc(kt + 2);
+    constexpr int NP = LA + 3 * LB;  // pieces of the refill
+    constexpr int PER = (NP + NMF - 1) / NMF;
+#pragma unroll
+    for (int u = 0; u < NMF; ++u) {
+      acc[u / TM][u % TM] =
+          __builtin_amdgcn_mfma_f32_32x32x16_bf16(b1[u / TM], a1[u % TM], acc[u / TM][u % TM], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int e = 0; e < PER; ++e) {
+        const int c = u * PER + e;
+        if (c < LA) {
+          la.issue_one(ra, st, wave, c);
+        } else if (c < NP) {
+          const int r = (c - LA) / 3, part = (c - LA) % 3;
+          if (part < 2) write_codes(st, r, part);
+          else load_codes(kt + 3, r);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    read_frags(smem + ((kt + 1) & 1) * STAGE, 0, a0, b0);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  wait_vm_barrier<0>();  // nothing is on its way into LDS any more
+
+  // acc[j][i][r]: output lane % 32, input (r / 4) * 8 + (lane / 32) * 4 + r % 4.  Through
+  // LDS, a 32-row slab of the wave's tile at a time, so that lanes write whole row segments.
+  constexpr int CLD = WTN + 4, CPW = WTN / 8, CPL = 32 * CPW / 64;
+  static_assert((size_t)NW * 32 * CLD * 4 <= 2 * STAGE, "epilogue staging fits in the operand buffers");
+  float* stg = reinterpret_cast<float*>(smem) + wave * 32 * CLD;
+  float* out = p.out + (size_t)split * p.n_out * p.n_in;
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<f32x4_t*>(stg + (lane & 31) * CLD + j * 32 + g * 8 + (lane >> 5) * 4) =
+            f32x4_t{acc[j][i][4 * g], acc[j][i][4 * g + 1], acc[j][i][4 * g + 2], acc[j][i][4 * g + 3]};
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the staging slab is this wave's own
+#pragma unroll
+    for (int u = 0; u < CPL; ++u) {
+      const int c = lane + 64 * u, r = c / CPW, cc = c % CPW;
+      const int m = m0 + wm * WTM + i * 32 + r, n = n0 + wn * WTN + cc * 8;
+      if (m < p.n_out && n < p.n_in) {
+        float v[8];
+        load8(stg + r * CLD + cc * 8, v);
+        float* o = out + (size_t)m * p.n_in + n;
+        if (p.accumulate) {
+          float w[8];
+          load8(o, w);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] += w[e];
+        }
+        store8(o, v);
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   }
 }
 
-__global__ void __launch_bounds__(256) act8_dw_bf16_kernel(int tokens, int n_out, int n_in,
-                                                           const bf16_t* __restrict__ dy,
-                                                           const uint8_t* __restrict__ q,
-                                                           const uint8_t* __restrict__ scales, float* __restrict__ dw,
-                                                           int accumulate) {
-  constexpr int R = kDwTile, CPR = R / 8;
-  __shared__ __align__(16) char smem[2 * R * 128];
-  char* sa = smem;            // dY [64 tokens][128 outputs] bf16
-  char* sb = smem + R * 128;  // X  [64 tokens][128 inputs] bf16
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int wm = wave >> 1, wn = wave & 1;
-  const int tiles_n = (n_in + R - 1) / R;
-  const int m0 = (blockIdx.x / tiles_n) * R, n0 = (blockIdx.x % tiles_n) * R;
-  FragReader<true, R> fr;
-  fr.init(lane);
-  f32x16_t acc[2][2];
+// dw (=|+=) the splits' sums, in split order.
+__global__ void __launch_bounds__(256) act8_dw_join_kernel(long long chunks, int splits, const float* __restrict__ part,
+                                                           float* __restrict__ dw, int accumulate) {
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= chunks) return;
+  f32x4_t s = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int k = 0; k < splits; ++k) {
+    const f32x4_t v = reinterpret_cast<const f32x4_t*>(part)[k * chunks + i];
 #pragma unroll
-  for (int j = 0; j < 2; ++j)
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) acc[j][i][e] = 0.0f;
-  const u32x4_t zero = {0u, 0u, 0u, 0u};
-  for (int k0 = 0; k0 < tokens; k0 += kBK) {
-    __syncthreads();  // the stage before has been read
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {  // dY: 64 x 16 chunks of 8 outputs
-      const int i = threadIdx.x + 256 * u, kr = i / CPR, ch = i % CPR;
-      const int t = k0 + kr, m = m0 + ch * 8;
-      const u32x4_t v = t < tokens && m < n_out
-                            ? *reinterpret_cast<const u32x4_t*>(dy + (size_t)t * n_out + m) : zero;
-      *reinterpret_cast<u32x4_t*>(sa + kr * 2 * R + ((ch + 4 * (kr & 3)) % CPR) * 16) = v;
-    }
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {  // X: 64 x 8 runs of 16 codes
-      const int i = threadIdx.x + 256 * u, kr = i / (R / 16), run = i % (R / 16);
-      const int t = k0 + kr, n = n0 + run * 16;
-      u32x4_t v[2] = {zero, zero};
-      if (t < tokens && n < n_in) {
-        const u32x4_t c = *reinterpret_cast<const u32x4_t*>(q + (size_t)t * n_in + n);
-        decode16(c, scale_of(scales[(size_t)t * (n_in / kScaleBlock) + n / kScaleBlock]), v);
-      }
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-        *reinterpret_cast<u32x4_t*>(sb + kr * 2 * R + ((run * 2 + e + 4 * (kr & 3)) % CPR) * 16) = v[e];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int ks = 0; ks < kBK / 16; ++ks) {
-      bf16x8_t a[2], b[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        a[i] = fr.read(sa, wm * 64 + i * 32, ks);
-        b[i] = fr.read(sb, wn * 64 + i * 32, ks);
-      }
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-          acc[j][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[j], a[i], acc[j][i], 0, 0, 0);
-    }
+    for (int e = 0; e < 4; ++e) s[e] += v[e];
   }
-  // acc[j][i][r]: output lane % 32, input (r / 4) * 8 + (lane / 32) * 4 + r % 4
+  f32x4_t* o = reinterpret_cast<f32x4_t*>(dw) + i;
+  if (accumulate) {
+    const f32x4_t v = *o;
 #pragma unroll
-  for (int j = 0; j < 2; ++j)
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int m = m0 + wm * 64 + i * 32 + (lane & 31);
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int n = n0 + wn * 64 + j * 32 + g * 8 + (lane >> 5) * 4;
-        if (m >= n_out || n >= n_in) continue;
-        float v[4] = {acc[j][i][4 * g], acc[j][i][4 * g + 1], acc[j][i][4 * g + 2], acc[j][i][4 * g + 3]};
-        float* out = dw + (size_t)m * n_in + n;
-        if (accumulate) {
-          float o[4];
-          load4(out, o);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] += o[e];
-        }
-        store4(out, v);
-      }
-    }
+    for (int e = 0; e < 4; ++e) s[e] = v[e] + s[e];
+  }
+  *o = s;
 }
 
 // fp32 check mode, on the fp32 matrix instruction (32 x 32 x 2): 64 x 64 tiles, four
@@ -335,23 +489,64 @@ hipError_t launch_act8_gelu_bwd(int dtype, int rows, int cols, const void* dg, c
   return hipGetLastError();
 }
 
+// Tile and split of the bf16 weight gradient.
+struct DwPlan {
+  bool large;  // 256 x 256 tiles, else 128 x 128
+  int tiles, splits, per_split;
+};
+
+static DwPlan dw_plan(int tokens, int n_out, int n_in) {
+  auto tiles = [&](int t) { return (long long)((n_out + t - 1) / t) * ((n_in + t - 1) / t); };
+  DwPlan p;
+  p.large = tiles(256) >= 160;
+  p.tiles = (int)tiles(p.large ? 256 : 128);
+  const int stages = (tokens + kBK - 1) / kBK;
+  int splits = 1;
+  if (!p.large) splits = (int)std::min<long long>(std::max<long long>(512 / p.tiles, 1), (stages + 7) / 8);
+  const int per = (stages + splits - 1) / splits;
+  p.splits = (stages + per - 1) / per;
+  p.per_split = per * kBK;
+  return p;
+}
+
 size_t act8_gemm_dw_scratch_bytes(int dtype, int tokens, int n_out, int n_in) {
-  (void)dtype; (void)tokens; (void)n_out; (void)n_in;
-  return 0;
+  if (dtype != DT_BF16) return 0;
+  const DwPlan p = dw_plan(tokens, n_out, n_in);
+  return p.splits > 1 ? (size_t)p.splits * n_out * n_in * sizeof(float) : 0;
+}
+
+template <int BM, int BN, int WM, int WN>
+static hipError_t run_dw(const DwArgs& a, int splits, hipStream_t s) {
+  constexpr size_t lds = 2 * (BM + BN) * 128;
+  static_assert(lds <= 160 * 1024, "LDS budget");
+  auto kern = act8_dw_kernel<BM, BN, WM, WN>;
+  static std::atomic<uint64_t> lds_set{0};
+  const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(kern), lds, lds_set);
+  if (e != hipSuccess) return e;
+  const long long wg = (long long)a.tiles * splits;
+  if (wg > 0x7fffffffLL) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(kern, dim3((unsigned)wg), dim3(WM * WN * 64), lds, s, a);
+  return hipGetLastError();
 }
 
 hipError_t launch_act8_gemm_dw(int dtype, int tokens, int n_out, int n_in, const void* dy, const uint8_t* q,
                                const uint8_t* scales, float* dw, int accumulate, void* scratch, hipStream_t s) {
-  (void)scratch;
-  const long long tile = dtype == DT_BF16 ? kDwTile : 64;
-  const long long wg = ((n_out + tile - 1) / tile) * ((n_in + tile - 1) / tile);
+  if (dtype == DT_BF16) {
+    const DwPlan p = dw_plan(tokens, n_out, n_in);
+    const bool split = p.splits > 1;
+    const DwArgs a{tokens, n_out, n_in, p.per_split, p.tiles, split ? 0 : accumulate, (const bf16_t*)dy, q, scales,
+                   split ? (float*)scratch : dw};
+    hipError_t e = p.large ? run_dw<256, 256, 2, 4>(a, p.splits, s) : run_dw<128, 128, 2, 2>(a, p.splits, s);
+    if (e != hipSuccess || !split) return e;
+    const long long chunks = (long long)n_out * n_in / 4;
+    hipLaunchKernelGGL(act8_dw_join_kernel, dim3((unsigned)((chunks + 255) / 256)), dim3(256), 0, s, chunks, p.splits,
+                       (const float*)scratch, dw, accumulate);
+    return hipGetLastError();
+  }
+  const long long wg = ((n_out + 63LL) / 64) * ((n_in + 63LL) / 64);
   if (wg > 0x7fffffffLL) return hipErrorInvalidValue;
-  if (dtype == DT_BF16)
-    hipLaunchKernelGGL(act8_dw_bf16_kernel, dim3((unsigned)wg), dim3(256), 0, s, tokens, n_out, n_in,
-                       (const bf16_t*)dy, q, scales, dw, accumulate);
-  else
-    hipLaunchKernelGGL(act8_dw_f32_kernel, dim3((unsigned)wg), dim3(256), 0, s, tokens, n_out, n_in, (const float*)dy,
-                       q, scales, dw, accumulate);
+  hipLaunchKernelGGL(act8_dw_f32_kernel, dim3((unsigned)wg), dim3(256), 0, s, tokens, n_out, n_in, (const float*)dy, q,
+                     scales, dw, accumulate);
   return hipGetLastError();
 }
 
