@@ -162,9 +162,11 @@ __global__ void __launch_bounds__(256) act8_gelu_bwd_kernel(long long chunks, co
 // along for 16 values.  Converting there costs each value one conversion in a
 // workgroup; behind LDS every wave that shares a column would convert it again.
 //
-// Stage kt + 2 is filled in behind the barrier at the end of stage kt's reads, its
-// pieces (dY load, conversion and LDS write, load of stage kt + 3's codes) between
-// the MFMAs of the last sub-step.  Every wait is for the loads of a whole stage ago.
+// A stage has four sub-steps; each reads the next one's fragments between its MFMAs.
+// Behind the barrier at the end of stage kt's reads its buffer is refilled with
+// stage kt + 2, piece by piece between the MFMAs too: dY's loads and the loads of the
+// codes of stage kt + 3 in the last sub-step, the conversions in the next two.  Every
+// wait is for the loads of a whole stage ago.
 // Buffers are addressed from each stage's first token, so operands may be of any
 // size; tokens past the end read as zeros.
 // ---------------------------------------------------------------------------
@@ -246,95 +248,95 @@ __global__ void __launch_bounds__(WM * WN * 64) act8_dw_kernel(DwArgs p) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[j][i][e] = 0.0f;
 
-  u32x4_t raw[LB];
-  uint32_t rs[LB];
-  bf16x8_t a0[TM], a1[TM], b0[TN], b1[TN];
-  auto load_codes = [&](int kt, int u) {  // run u of stage kt
+  // The codes of the next stage to convert, and of the one after it (on their way).
+  struct Codes {
+    u32x4_t q[LB];
+    uint32_t s[LB];
+  } now, next;
+  bf16x8_t a0[TM], a1[TM], b0[TN], b1[TN];  // two fragment sets
+  auto load_codes = [&](Codes& c, int kt, int u) {  // run u of stage kt
     const int left = rows - kt * kBK;
     const __amdgpu_buffer_rsrc_t rq = stage_buffer(pq + (size_t)kt * kBK * ldq, left, ldq);
     const __amdgpu_buffer_rsrc_t rc = stage_buffer(ps + (size_t)kt * kBK * lds, left, lds);
-    raw[u] = __builtin_amdgcn_raw_buffer_load_b128(rq, qoff[u], 0, 0);
-    rs[u] = __builtin_amdgcn_raw_buffer_load_b8(rc, soff[u], 0, 0);
+    c.q[u] = __builtin_amdgcn_raw_buffer_load_b128(rq, qoff[u], 0, 0);
+    c.s[u] = __builtin_amdgcn_raw_buffer_load_b8(rc, soff[u], 0, 0);
   };
   auto write_codes = [&](char* st, int u, int half) {  // chunk `half` (in this lane's order) of run u
-    const float sc = scale_of(rs[u]);
+    const float sc = scale_of(now.s[u]);
     const bool second = half ? !swap[u] : swap[u];
-    const u32x4_t v = decode8_bf16(second ? raw[u][2] : raw[u][0], second ? raw[u][3] : raw[u][1], sc);
+    const u32x4_t v = decode8_bf16(second ? now.q[u][2] : now.q[u][0], second ? now.q[u][3] : now.q[u][1], sc);
     *reinterpret_cast<u32x4_t*>(st + w0[u] + (second ? 16 : 0)) = v;
   };
   auto dy_rsrc = [&](int kt) { return stage_rsrc(pa + (size_t)kt * kBK * lda, rows - kt * kBK, lda); };
-  auto read_frags = [&](const char* st, int ks, bf16x8_t (&a)[TM], bf16x8_t (&b)[TN]) {
-#pragma unroll
-    for (int i = 0; i < TM; ++i) a[i] = fa.read(st, wm * WTM + i * 32, ks);
-#pragma unroll
-    for (int j = 0; j < TN; ++j) b[j] = fb.read(st + A_BYTES, wn * WTN + j * 32, ks);
-  };
-  constexpr int NMF = TM * TN, NRD = 2 * (TM + TN), NIL = NRD > NMF ? NRD : NMF;
-  // reads of (st, ks) into set n, interleaved with the MFMAs of set c
+  // A sub-step: the MFMAs of set c, each followed by the read of one fragment of (st, ks)
+  // into set n and by piece(u), in that order.
+  constexpr int NMF = TM * TN;
+  constexpr int RPM = (TM + TN + NMF - 1) / NMF;  // fragment reads behind an MFMA
   auto step = [&](const char* st, int ks, bf16x8_t (&na)[TM], bf16x8_t (&nb)[TN], const bf16x8_t (&ca)[TM],
-                  const bf16x8_t (&cb)[TN]) {
-    read_frags(st, ks, na, nb);
-#pragma unroll
-    for (int j = 0; j < TN; ++j)
-#pragma unroll
-      for (int i = 0; i < TM; ++i)
-        acc[j][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cb[j], ca[i], acc[j][i], 0, 0, 0);
-#pragma unroll
-    for (int i = 0; i < NIL; ++i) {
-      if (i < NMF) __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // one MFMA
-      if (i < NRD) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // one LDS read
-    }
-    __builtin_amdgcn_sched_barrier(0);
-  };
-
-#pragma unroll
-  for (int s = 0; s < 2; ++s) {
-    char* st = smem + s * STAGE;
-#pragma unroll
-    for (int u = 0; u < LB; ++u) load_codes(s, u);
-    la.issue(dy_rsrc(s), st, wave);
-#pragma unroll
-    for (int u = 0; u < LB; ++u) {
-      write_codes(st, u, 0);
-      write_codes(st, u, 1);
-    }
-  }
-#pragma unroll
-  for (int u = 0; u < LB; ++u) load_codes(2, u);
-  wait_vm_barrier<0>();
-  read_frags(smem, 0, a0, b0);
-  __builtin_amdgcn_sched_barrier(0);
-
-  // Past the last stage the loads find empty buffers: they fetch nothing and write zeros.
-  for (int kt = 0; kt < KT; ++kt) {
-    char* st = smem + (kt & 1) * STAGE;
-    step(st, 1, a1, b1, a0, b0);
-    step(st, 2, a0, b0, a1, b1);
-    step(st, 3, a1, b1, a0, b0);
-    wait_vm_barrier<0>();  // stage kt + 1 is in LDS, the codes of kt + 2 in registers; all have read stage kt
-    const i32x4_t ra = dy_rsrc(kt + 2);
-    constexpr int NP = LA + 3 * LB;  // pieces of the refill
-    constexpr int PER = (NP + NMF - 1) / NMF;
+                  const bf16x8_t (&cb)[TN], auto piece) {
 #pragma unroll
     for (int u = 0; u < NMF; ++u) {
       acc[u / TM][u % TM] =
-          __builtin_amdgcn_mfma_f32_32x32x16_bf16(b1[u / TM], a1[u % TM], acc[u / TM][u % TM], 0, 0, 0);
+          __builtin_amdgcn_mfma_f32_32x32x16_bf16(cb[u / TM], ca[u % TM], acc[u / TM][u % TM], 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int e = 0; e < RPM; ++e) {
+        const int f = u * RPM + e;
+        if (f < TN) nb[f] = fb.read(st + A_BYTES, wn * WTN + f * 32, ks);
+        else if (f < TN + TM) na[f - TN] = fa.read(st, wm * WTM + (f - TN) * 32, ks);
+      }
+      piece(u);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  auto nothing = [](int) {};
+
+#pragma unroll
+  for (int u = 0; u < LB; ++u) load_codes(now, 0, u);
+  la.issue(dy_rsrc(0), smem, wave);
+#pragma unroll
+  for (int u = 0; u < LB; ++u) {
+    write_codes(smem, u, 0);
+    write_codes(smem, u, 1);
+  }
+#pragma unroll
+  for (int u = 0; u < LB; ++u) load_codes(next, 1, u);
+  wait_vm_barrier<0>();
+  now = next;
+#pragma unroll
+  for (int u = 0; u < LB; ++u) load_codes(next, 2, u);
+  la.issue(dy_rsrc(1), smem + STAGE, wave);
+#pragma unroll
+  for (int j = 0; j < TN; ++j) b0[j] = fb.read(smem + A_BYTES, wn * WTN + j * 32, 0);
+#pragma unroll
+  for (int i = 0; i < TM; ++i) a0[i] = fa.read(smem, wm * WTM + i * 32, 0);
+  __builtin_amdgcn_sched_barrier(0);
+
+  // Past the last stage the loads find empty buffers: they fetch nothing and write zeros.
+  constexpr int CONV = 2 * LB;  // chunks to convert, half of them in each of two sub-steps
+  for (int kt = 0; kt < KT; ++kt) {
+    char* st = smem + (kt & 1) * STAGE;
+    char* other = smem + ((kt + 1) & 1) * STAGE;
+    auto convert = [&](int first, int u) {
+      constexpr int EVERY = NMF / (CONV / 2);
+      static_assert(NMF % (CONV / 2) == 0, "conversions spread evenly over the MFMAs");
+      if (u % EVERY == 0) write_codes(other, (first + u / EVERY) / 2, (first + u / EVERY) % 2);
+    };
+    step(st, 1, a1, b1, a0, b0, [&](int u) { convert(0, u); });
+    step(st, 2, a0, b0, a1, b1, [&](int u) { convert(CONV / 2, u); });
+    step(st, 3, a1, b1, a0, b0, nothing);
+    wait_vm_barrier<0>();  // stage kt + 1 is in LDS, `next` is there, and all have read stage kt
+    now = next;
+    const i32x4_t ra = dy_rsrc(kt + 2);
+    constexpr int NP = LA + LB, PER = (NP + NMF - 1) / NMF;
+    step(other, 0, a0, b0, a1, b1, [&](int u) {
 #pragma unroll
       for (int e = 0; e < PER; ++e) {
         const int c = u * PER + e;
-        if (c < LA) {
-          la.issue_one(ra, st, wave, c);
-        } else if (c < NP) {
-          const int r = (c - LA) / 3, part = (c - LA) % 3;
-          if (part < 2) write_codes(st, r, part);
-          else load_codes(kt + 3, r);
-        }
+        if (c < LA) la.issue_one(ra, st, wave, c);
+        else if (c < NP) load_codes(next, kt + 3, c - LA);
       }
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    read_frags(smem + ((kt + 1) & 1) * STAGE, 0, a0, b0);
-    __builtin_amdgcn_sched_barrier(0);
+    });
   }
   wait_vm_barrier<0>();  // nothing is on its way into LDS any more
 

@@ -15,9 +15,16 @@
 // the raw rows is kept for it.  Statistics and sums are fp32, outputs are rounded
 // once.
 //
-// Bound by memory.  A group of 8, 16 or 32 lanes owns a head, 8 features a lane,
-// so a wave moves 8, 4 or 2 neighbouring heads at a time; the two halves of a pair
-// meet by a lane exchange.
+// Bound by memory.  G lanes own a head, CH chunks of 8 features each; a workgroup holds
+// 256 / G heads of one kind (queries or keys, so one gain) at a time, and others copy
+// the values.  How the chunks lie on the lanes, so that loads cover whole segments and
+// the two members of a pair meet cheaply:
+//   64, 128, 256 features: two chunks a lane, half a head apart; pairs of a fully
+//     rotated head lie in one lane;
+//   96: three neighbouring chunks on each of four lanes, pairs in lanes that differ in
+//     one bit;
+//   any other head, or any other number of rotated features: one chunk a lane, pairs
+//     anywhere in the group.
 #include <algorithm>
 #include <cmath>
 
@@ -50,182 +57,341 @@ struct QkArgs {
   const float* table;
 };
 
+// The value of the lane whose number differs in bit(s) X.
+template <int X>
+__device__ __forceinline__ float xor_lane(float v) {
+  const int i = __float_as_int(v);
+  if constexpr (X == 1) return __int_as_float(__builtin_amdgcn_update_dpp(0, i, 0xB1, 0xf, 0xf, true));  // quad [1,0,3,2]
+  else if constexpr (X == 2) return __int_as_float(__builtin_amdgcn_update_dpp(0, i, 0x4E, 0xf, 0xf, true));  // [2,3,0,1]
+  else if constexpr (X == 8) return __int_as_float(__builtin_amdgcn_update_dpp(0, i, 0x128, 0xf, 0xf, true));  // row_ror:8
+  else return __int_as_float(__builtin_amdgcn_ds_swizzle(i, 0x1f | (X << 10)));  // 4, 16: xor within 32 lanes
+}
+
 template <int G>
 __device__ __forceinline__ float group_sum(float v) {
-#pragma unroll
-  for (int off = G / 2; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+  if constexpr (G > 1) v += xor_lane<1>(v);
+  if constexpr (G > 2) v += xor_lane<2>(v);
+  if constexpr (G > 4) v += xor_lane<4>(v);
+  if constexpr (G > 8) v += xor_lane<8>(v);
+  if constexpr (G > 16) v += xor_lane<16>(v);
   return v;
 }
 
-// Rotation of the 8 features of chunk c by the token's angles, forward (dir = 1)
-// or back (dir = -1).  `base` is the group's first lane.  A position outside the
-// table rotates by NaN.
-template <bool INTER>
-__device__ __forceinline__ void rotate8(const QkArgs& a, int pos, int c, int base, float dir, float z[8]) {
-  const int pc = a.rope >> 4;  // chunks of half the rotated features
+// How the two members of a pair meet: neighbours (interleaved), in a lane's two chunks, in
+// lanes that differ in one bit, or anywhere in the group.
+enum { INTERLEAVED = 0, IN_LANE = -2, ANYWHERE = -1 };  // else the bit
+
+// Chunk i of lane j.
+template <int G, int CH>
+__device__ __forceinline__ int chunk_of(int j, int i) {
+  return CH == 2 ? j + G * i : j * CH + i;
+}
+
+// Rotation of a lane's features by its token's angles, forward (dir = 1) or back
+// (dir = -1).  The lane is the group's j-th, `base` its first lane.  A position outside
+// the table rotates by NaN.
+template <int G, int CH, int MODE>
+__device__ __forceinline__ void rotate(const QkArgs& a, int pos, int j, int base, float dir, float (&z)[CH][8]) {
   const bool in = pos >= 0 && pos < a.table_rows;
-  const bool rot = c < 2 * pc;
-  if constexpr (INTER) {
-    if (!rot) return;
-    const float* cs = a.table + ((size_t)(in ? pos : 0) * (a.rope >> 1) + c * 4) * 2;
-    float t[8];
-    load8(cs, t);
+  const float* row = a.table + (size_t)(in ? pos : 0) * a.rope;  // rope / 2 pairs of floats
+  if constexpr (MODE == INTERLEAVED) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float co = in ? t[2 * e] : NAN, si = (in ? t[2 * e + 1] : NAN) * dir;
-      const float x = z[2 * e], y = z[2 * e + 1];
-      z[2 * e] = x * co - y * si;
-      z[2 * e + 1] = y * co + x * si;
+    for (int i = 0; i < CH; ++i) {
+      const int c = chunk_of<G, CH>(j, i);
+      if (c * 8 >= a.rope) continue;
+      float t[8];
+      load8(row + c * 8, t);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float co = in ? t[2 * e] : NAN, si = (in ? t[2 * e + 1] : NAN) * dir;
+        const float x = z[i][2 * e], y = z[i][2 * e + 1];
+        z[i][2 * e] = x * co - y * si;
+        z[i][2 * e + 1] = y * co + x * si;
+      }
     }
-  } else {
-    const bool low = c < pc;
-    const int other = rot ? base + (low ? c + pc : c - pc) : base;
-    float p[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) p[e] = __shfl(z[e], other, 64);
-    if (!rot) return;
-    const float* cs = a.table + ((size_t)(in ? pos : 0) * (a.rope >> 1) + (low ? c : c - pc) * 8) * 2;
+  } else if constexpr (MODE == IN_LANE) {
+    static_assert(CH == 2, "the lane's chunks are half a head apart");
     float t[16];
-    load8(cs, t);
-    load8(cs + 8, t + 8);
-    const float sign = low ? -dir : dir;
+    load8(row + j * 16, t);
+    load8(row + j * 16 + 8, t + 8);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float co = in ? t[2 * e] : NAN, si = (in ? t[2 * e + 1] : NAN) * sign;
-      z[e] = z[e] * co + p[e] * si;
+      const float co = in ? t[2 * e] : NAN, si = (in ? t[2 * e + 1] : NAN) * dir;
+      const float x = z[0][e], y = z[1][e];
+      z[0][e] = x * co - y * si;
+      z[1][e] = y * co + x * si;
+    }
+  } else {
+    constexpr int ROT = CH == 2 ? 1 : CH;    // chunks of a lane that are rotated (CH = 2: the lower half of a head)
+    const int lanes = (a.rope >> 4) / ROT;   // lanes that hold the pairs' first members
+    const bool low = j < lanes, rot = j < 2 * lanes;
+    const float sign = low ? -dir : dir;
+    const float* cs = row + (low ? j : j - lanes) * ROT * 16;
+#pragma unroll
+    for (int i = 0; i < ROT; ++i) {
+      float p[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if constexpr (MODE > 0) p[e] = xor_lane<(MODE > 0 ? MODE : 1)>(z[i][e]);
+        else p[e] = __shfl(z[i][e], rot ? base + (low ? j + lanes : j - lanes) : base, 64);
+      }
+      if (!rot) continue;
+      float t[16];
+      load8(cs + i * 16, t);
+      load8(cs + i * 16 + 8, t + 8);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float co = in ? t[2 * e] : NAN, si = (in ? t[2 * e + 1] : NAN) * sign;
+        z[i][e] = z[i][e] * co + p[e] * si;
+      }
     }
   }
 }
 
-__device__ __forceinline__ int position_of(const QkArgs& a, int t) {
-  return a.positions ? a.positions[t] : t % a.seq_len;
+__device__ __forceinline__ int position_of(const QkArgs& a, unsigned t) {
+  return a.positions ? a.positions[t] : (int)(t % (unsigned)a.seq_len);
 }
 
-// One head per group of G lanes and step.  `copy`: also move the value heads
-// (out is not in).
-template <typename T, int G, bool INTER>
-__global__ void __launch_bounds__(256) qk_fwd_kernel(QkArgs a, int copy, const T* in, const T* __restrict__ gq,
-                                                     const T* __restrict__ gk, T* out) {
-  const int lane = threadIdx.x & 63, j = lane & (G - 1), base = lane - j;
-  const int row_heads = a.q_heads + 2 * a.kv_heads, qk = a.q_heads + a.kv_heads;
-  const int heads = copy ? row_heads : qk;
-  const long long slot = ((long long)blockIdx.x * 256 + threadIdx.x) / G;
-  const long long t = slot / heads;
-  if (t >= a.tokens) return;  // whole groups leave: the exchanges below stay within a group
-  const int h = (int)(slot - t * heads);
-  const bool live = j * 8 < a.d;
-  const size_t at = ((size_t)t * row_heads + h) * a.d + j * 8;
-  float x[8];
+// Workgroups of a launch: for queries, for keys, for copying values.
+struct QkGrid {
+  int q, k, v;
+};
+
+constexpr int kCopyUnroll = 4;  // 16-byte chunks of the values a thread moves
+
+// Copy of the value heads by workgroup b.
+template <typename T>
+__device__ __forceinline__ void copy_values(const QkArgs& a, unsigned b, const T* in, T* out) {
+  constexpr unsigned EPC = 16 / sizeof(T);
+  const unsigned per = a.kv_heads * a.d / EPC;  // chunks of a row's values
+  const size_t row = (size_t)(a.q_heads + 2 * a.kv_heads) * a.d, skip = (size_t)(a.q_heads + a.kv_heads) * a.d;
+  const unsigned long long first = (unsigned long long)b * (256 * kCopyUnroll);
+  const unsigned t0 = (unsigned)(first / per), c0 = (unsigned)(first % per);
+  u32x4_t v[kCopyUnroll];
+  size_t at[kCopyUnroll];
+  bool live[kCopyUnroll];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = 0.0f;
-  if (live) load8(in + at, x);
-  if (h >= qk) {
-    if (live) store8(out + at, x);
+  for (int u = 0; u < kCopyUnroll; ++u) {
+    const unsigned local = c0 + threadIdx.x + 256 * u, dt = local / per;
+    live[u] = (unsigned long long)t0 + dt < (unsigned)a.tokens;
+    at[u] = ((size_t)t0 + dt) * row + skip + (size_t)(local - dt * per) * EPC;
+    if (live[u]) v[u] = *reinterpret_cast<const u32x4_t*>(in + at[u]);
+  }
+#pragma unroll
+  for (int u = 0; u < kCopyUnroll; ++u)
+    if (live[u]) *reinterpret_cast<u32x4_t*>(out + at[u]) = v[u];
+}
+
+// The heads of one kind, numbered through all tokens: token and head of number
+// first + i, first a workgroup's first.
+struct HeadRange {
+  int heads, head0;
+  unsigned t0, h0;
+  __device__ __forceinline__ HeadRange(int heads, int head0, unsigned long long first)
+      : heads(heads), head0(head0), t0((unsigned)(first / heads)), h0((unsigned)(first % heads)) {}
+  // Element of the head in a row-major [tokens][row heads][d]; *t is its token.
+  __device__ __forceinline__ size_t at(unsigned i, const QkArgs& a, unsigned* t) const {
+    const unsigned local = h0 + i, dt = local / (unsigned)heads;
+    *t = t0 + dt;
+    return ((size_t)*t * (a.q_heads + 2 * a.kv_heads) + head0 + (local - dt * heads)) * a.d;
+  }
+};
+
+// Lane j's chunks of a head at p.
+template <int G, int CH, typename T>
+__device__ __forceinline__ void load_chunks(const T* p, int j, int d, float (&v)[CH][8]) {
+#pragma unroll
+  for (int i = 0; i < CH; ++i) {
+    const int c = chunk_of<G, CH>(j, i) * 8;
+    if (CH > 1 || c < d) {  // (a head fills its lanes where they hold more than one chunk)
+      load8(p + c, v[i]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] = 0.0f;
+    }
+  }
+}
+
+template <int G, int CH, typename T>
+__device__ __forceinline__ void store_chunks(T* p, int j, int d, const float (&v)[CH][8]) {
+#pragma unroll
+  for (int i = 0; i < CH; ++i) {
+    const int c = chunk_of<G, CH>(j, i) * 8;
+    if (CH > 1 || c < d) store8(p + c, v[i]);
+  }
+}
+
+template <typename T, int G, int CH, int MODE>
+__global__ void __launch_bounds__(256) qk_fwd_kernel(QkArgs a, QkGrid grid, const T* in, const T* __restrict__ gq,
+                                                     const T* __restrict__ gk, T* out) {
+  if ((int)blockIdx.x >= grid.q + grid.k) {
+    copy_values(a, blockIdx.x - grid.q - grid.k, in, out);
     return;
   }
+  const bool keys = (int)blockIdx.x >= grid.q;
+  const unsigned b = blockIdx.x - (keys ? grid.q : 0);
+  const HeadRange range(keys ? a.kv_heads : a.q_heads, keys ? a.q_heads : 0, (unsigned long long)b * (256 / G));
+  const int lane = threadIdx.x & 63, j = lane & (G - 1), base = lane - j;
+  unsigned t;
+  const size_t at = range.at(threadIdx.x / G, a, &t);
+  if (t >= (unsigned)a.tokens) return;  // whole groups leave: the exchanges stay within a group
+  float x[CH][8], g[CH][8];
+  load_chunks<G, CH>(in + at, j, a.d, x);
+  const int pos = a.rope ? position_of(a, t) : 0;
+  load_chunks<G, CH>(keys ? gk : gq, j, a.d, g);
   float s = 0.0f;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) s += x[e] * x[e];
+  for (int i = 0; i < CH; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s += x[i][e] * x[i][e];
   const float rstd = 1.0f / sqrtf(group_sum<G>(s) / (float)a.d + a.eps);
-  float g[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) g[e] = 0.0f;
-  if (live) load8((h < a.q_heads ? gq : gk) + j * 8, g);
+  for (int i = 0; i < CH; ++i)
 #pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = x[e] * rstd * g[e];
-  if (a.rope) rotate8<INTER>(a, position_of(a, (int)t), j, base, 1.0f, x);
-  if (live) store8(out + at, x);
+    for (int e = 0; e < 8; ++e) x[i][e] = x[i][e] * rstd * g[i][e];
+  if (a.rope) rotate<G, CH, MODE>(a, pos, j, base, 1.0f, x);
+  store_chunks<G, CH>(out + at, j, a.d, x);
 }
 
-// Gradient: workgroups step through the heads, each lane keeping the sums of its
-// 8 gain columns for queries and for keys; the workgroup's sums go to
-// part[query or key][workgroup][d], and launch_reduce_partials adds those in order.
-template <typename T, int G, bool INTER>
-__global__ void __launch_bounds__(256) qk_bwd_kernel(QkArgs a, int copy, const T* dout, const T* __restrict__ in,
+// Gradient: the workgroups of a kind step through its heads, each lane keeping the sums
+// of its gain columns; a workgroup's sums go to part[workgroup][d], queries' first, and
+// qk_gain_kernel adds those in order.
+template <typename T, int G, int CH, int MODE>
+__global__ void __launch_bounds__(256) qk_bwd_kernel(QkArgs a, QkGrid grid, const T* dout, const T* __restrict__ in,
                                                      const T* __restrict__ gq, const T* __restrict__ gk, T* dx,
                                                      float* __restrict__ part) {
-  __shared__ float red[2][4][G * 8];
+  if ((int)blockIdx.x >= grid.q + grid.k) {
+    copy_values(a, blockIdx.x - grid.q - grid.k, dout, dx);
+    return;
+  }
+  __shared__ float red[4][G * CH * 8];
+  const bool keys = (int)blockIdx.x >= grid.q;
+  const unsigned b = blockIdx.x - (keys ? grid.q : 0), blocks = keys ? grid.k : grid.q;
+  const int heads = keys ? a.kv_heads : a.q_heads;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, j = lane & (G - 1), base = lane - j;
-  const int row_heads = a.q_heads + 2 * a.kv_heads, qk = a.q_heads + a.kv_heads;
-  const int heads = copy ? row_heads : qk;
-  const bool live = j * 8 < a.d;
-  const long long slots = (long long)a.tokens * heads, stride = (long long)gridDim.x * (256 / G);
-  float sq[8], sk[8];
+  float g[CH][8], sum[CH][8];
+  load_chunks<G, CH>(keys ? gk : gq, j, a.d, g);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) sq[e] = sk[e] = 0.0f;
-  for (long long slot = ((long long)blockIdx.x * 256 + threadIdx.x) / G; slot < slots; slot += stride) {
-    const long long t = slot / heads;
-    const int h = (int)(slot - t * heads);
-    const size_t at = ((size_t)t * row_heads + h) * a.d + j * 8;
-    float dz[8], x[8], g[8];
+  for (int i = 0; i < CH; ++i)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) dz[e] = x[e] = g[e] = 0.0f;
-    if (live) load8(dout + at, dz);
-    if (h >= qk) {
-      if (live) store8(dx + at, dz);
-      continue;
-    }
-    if (live) {
-      load8(in + at, x);
-      load8((h < a.q_heads ? gq : gk) + j * 8, g);
-    }
-    if (a.rope) rotate8<INTER>(a, position_of(a, (int)t), j, base, -1.0f, dz);
+    for (int e = 0; e < 8; ++e) sum[i][e] = 0.0f;
+  const unsigned long long total = (unsigned long long)a.tokens * heads;
+  for (unsigned long long first = (unsigned long long)b * (256 / G); first < total;
+       first += (unsigned long long)blocks * (256 / G)) {
+    const HeadRange range(heads, keys ? a.q_heads : 0, first);
+    unsigned t;
+    const size_t at = range.at(threadIdx.x / G, a, &t);
+    if (t >= (unsigned)a.tokens) continue;
+    float dz[CH][8], x[CH][8];
+    load_chunks<G, CH>(dout + at, j, a.d, dz);
+    load_chunks<G, CH>(in + at, j, a.d, x);
+    if (a.rope) rotate<G, CH, MODE>(a, position_of(a, t), j, base, -1.0f, dz);
     float s = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s += x[e] * x[e];
+    for (int i = 0; i < CH; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s += x[i][e] * x[i][e];
     const float rstd = 1.0f / sqrtf(group_sum<G>(s) / (float)a.d + a.eps);
     float m = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      x[e] *= rstd;
-      const float c = dz[e] * x[e];
-      if (h < a.q_heads) sq[e] += c;
-      else sk[e] += c;
-      dz[e] *= g[e];
-      m += dz[e] * x[e];
-    }
+    for (int i = 0; i < CH; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        x[i][e] *= rstd;
+        sum[i][e] += dz[i][e] * x[i][e];
+        dz[i][e] *= g[i][e];
+        m += dz[i][e] * x[i][e];
+      }
     m = group_sum<G>(m) / (float)a.d;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) dz[e] = rstd * (dz[e] - x[e] * m);
-    if (live) store8(dx + at, dz);
+    for (int i = 0; i < CH; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) dz[i][e] = rstd * (dz[i][e] - x[i][e] * m);
+    store_chunks<G, CH>(dx + at, j, a.d, dz);
   }
   // the wave's groups, then the four waves in order
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
+  for (int i = 0; i < CH; ++i)
 #pragma unroll
-    for (int off = G; off < 64; off <<= 1) {
-      sq[e] += __shfl_xor(sq[e], off, 64);
-      sk[e] += __shfl_xor(sk[e], off, 64);
+    for (int e = 0; e < 8; ++e) {
+#pragma unroll
+      for (int off = G; off < 64; off <<= 1) sum[i][e] += __shfl_xor(sum[i][e], off, 64);
+      if (lane < G) red[w][chunk_of<G, CH>(j, i) * 8 + e] = sum[i][e];
     }
-    if (lane < G) {
-      red[0][w][j * 8 + e] = sq[e];
-      red[1][w][j * 8 + e] = sk[e];
-    }
-  }
   __syncthreads();
-  for (int i = threadIdx.x; i < 2 * a.d; i += 256) {
-    const int which = i >= a.d, c = i - which * a.d;
-    const float v = red[which][0][c] + red[which][1][c] + red[which][2][c] + red[which][3][c];
-    part[((size_t)which * gridDim.x + blockIdx.x) * a.d + c] = v;
+  for (int i = threadIdx.x; i < a.d; i += 256)
+    part[(size_t)blockIdx.x * a.d + i] = red[0][i] + red[1][i] + red[2][i] + red[3][i];
+}
+
+// Gain gradients from the workgroups' sums, 16 columns of one gain a workgroup: 64
+// threads a column take every 64th sum (8 in flight), and are added in order.  (One
+// column a lane with 16 waves, the way the other column sums end, took 17 us for
+// 1024 sums.)
+__global__ void __launch_bounds__(1024) qk_gain_kernel(int d, QkGrid grid, const float* __restrict__ part,
+                                                       float* __restrict__ dgq, float* __restrict__ dgk,
+                                                       int accumulate) {
+  __shared__ float red[64][17];
+  const int per = (d + 15) / 16;  // workgroups of a gain
+  const bool keys = (int)blockIdx.x >= per;
+  const int col = (blockIdx.x - (keys ? per : 0)) * 16 + (threadIdx.x & 15), slice = threadIdx.x >> 4;
+  const int n = keys ? grid.k : grid.q;
+  const float* p = part + (size_t)(keys ? grid.q : 0) * d;
+  float s = 0.0f;
+  if (col < d) {
+#pragma unroll 8
+    for (int i = slice; i < n; i += 64) s += p[(size_t)i * d + col];
+  }
+  red[slice][threadIdx.x & 15] = s;
+  __syncthreads();
+  if (threadIdx.x < 16 && col < d) {
+    float v = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 64; ++i) v += red[i][threadIdx.x];
+    float* o = (keys ? dgk : dgq) + col;
+    *o = accumulate ? *o + v : v;
   }
 }
 
 // ---------------------------------------------------------------------------
 // Host launchers
 // ---------------------------------------------------------------------------
-constexpr int kBwdBlocks = 1024;
+// Lanes of a head, chunks of a lane and how its pairs meet (see the top).
+struct QkLanes {
+  int G, CH, mode;
+};
 
-static inline int group_lanes(int d) { return d <= 64 ? 8 : d <= 128 ? 16 : 32; }
+static QkLanes lanes_of(const QkShape& q) {
+  const int n = q.head_dim / 8;  // chunks
+  const bool one = q.interleaved || q.rope_dim == 0;
+  const bool full = q.rope_dim == q.head_dim, half = 2 * q.rope_dim == q.head_dim;
+  if (one || full || half) {
+    if (n == 8 || n == 16 || n == 32) return {n / 2, 2, one ? INTERLEAVED : full ? IN_LANE : n / 4};
+    if (n == 12) return {4, 3, one ? INTERLEAVED : full ? 2 : 1};
+  }
+  return {n <= 8 ? 8 : n <= 16 ? 16 : 32, 1, one ? INTERLEAVED : ANYWHERE};
+}
 
-// Workgroups of the gradient: the same for a size whether the values are copied or not.
-static inline int bwd_blocks(int tokens, int q_heads, int kv_heads, int d) {
-  const long long per = 256 / group_lanes(d);
-  const long long need = ((long long)tokens * (q_heads + kv_heads) + per - 1) / per;
-  return (int)std::min<long long>(need, kBwdBlocks);
+static long long heads_blocks(long long tokens, int heads, int G) { return (tokens * heads + 256 / G - 1) / (256 / G); }
+
+static long long copy_blocks(const QkShape& q, size_t esz) {
+  const long long chunks = (long long)q.tokens * q.kv_heads * q.head_dim * (long long)esz / 16;
+  return (chunks + 256 * kCopyUnroll - 1) / (256 * kCopyUnroll);
+}
+
+// Workgroups of the gradient's two kinds: as many as the chip holds at once (four a CU;
+// three with three chunks a lane, by their registers) shared out by the kinds' heads, or
+// one for each 32 heads if that is fewer.
+static void bwd_blocks(int tokens, int q_heads, int kv_heads, int d, int* bq, int* bk) {
+  const long long all = d == 96 ? 768 : 1024;
+  const long long share = std::max(1LL, all * q_heads / (q_heads + kv_heads));
+  *bq = (int)std::min(heads_blocks(tokens, q_heads, 8), share);
+  *bk = (int)std::min(heads_blocks(tokens, kv_heads, 8), std::max(1LL, all - share));
 }
 
 size_t qk_norm_rope_scratch_elems(int tokens, int q_heads, int kv_heads, int d) {
-  return (size_t)2 * bwd_blocks(tokens, q_heads, kv_heads, d) * d;
+  int bq, bk;
+  bwd_blocks(tokens, q_heads, kv_heads, d, &bq, &bk);
+  return (size_t)(bq + bk) * d;
 }
 
 hipError_t launch_rope_table(int positions, int rope_dim, double theta, float* table, hipStream_t s) {
@@ -241,71 +407,83 @@ static QkArgs qk_args(const QkShape& q) {
                 q.eps, q.positions, q.table};
 }
 
-template <typename T, int G>
-static hipError_t fwd_t(const QkShape& q, const void* in, const void* gq, const void* gk, void* out, hipStream_t s) {
-  const int copy = in != out;
-  const int heads = q.q_heads + q.kv_heads + (copy ? q.kv_heads : 0);
-  const long long wg = ((long long)q.tokens * heads * G + 255) / 256;
-  if (wg > 0x7fffffffLL) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)wg);
-  if (q.interleaved)
-    hipLaunchKernelGGL((qk_fwd_kernel<T, G, true>), grid, dim3(256), 0, s, qk_args(q), copy, (const T*)in,
-                       (const T*)gq, (const T*)gk, (T*)out);
-  else
-    hipLaunchKernelGGL((qk_fwd_kernel<T, G, false>), grid, dim3(256), 0, s, qk_args(q), copy, (const T*)in,
-                       (const T*)gq, (const T*)gk, (T*)out);
-  return hipGetLastError();
+struct QkCall {
+  const QkShape& q;
+  const void *dout, *in, *gq, *gk;  // dout: gradient only
+  void* out;
+  float* part;
+  hipStream_t s;
+};
+
+struct Fwd {
+  template <typename T, int G, int CH, int MODE>
+  static hipError_t run(const QkCall& c) {
+    const QkShape& q = c.q;
+    const long long bq = heads_blocks(q.tokens, q.q_heads, G), bk = heads_blocks(q.tokens, q.kv_heads, G);
+    const long long bv = c.in != c.out ? copy_blocks(q, sizeof(T)) : 0;
+    if (bq + bk + bv > 0x7fffffffLL) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((qk_fwd_kernel<T, G, CH, MODE>), dim3((unsigned)(bq + bk + bv)), dim3(256), 0, c.s, qk_args(q),
+                       QkGrid{(int)bq, (int)bk, (int)bv}, (const T*)c.in, (const T*)c.gq, (const T*)c.gk, (T*)c.out);
+    return hipGetLastError();
+  }
+};
+
+struct Bwd {
+  template <typename T, int G, int CH, int MODE>
+  static hipError_t run(const QkCall& c) {
+    const QkShape& q = c.q;
+    int bq, bk;
+    bwd_blocks(q.tokens, q.q_heads, q.kv_heads, q.head_dim, &bq, &bk);
+    const long long bv = c.dout != c.out ? copy_blocks(q, sizeof(T)) : 0;
+    if (bq + bk + bv > 0x7fffffffLL) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((qk_bwd_kernel<T, G, CH, MODE>), dim3((unsigned)(bq + bk + bv)), dim3(256), 0, c.s, qk_args(q),
+                       QkGrid{bq, bk, (int)bv}, (const T*)c.dout, (const T*)c.in, (const T*)c.gq, (const T*)c.gk,
+                       (T*)c.out, c.part);
+    return hipGetLastError();
+  }
+};
+
+template <typename P, typename T, int G, int CH>
+static hipError_t run_mode(const QkCall& c, int mode) {
+  if (mode == INTERLEAVED) return P::template run<T, G, CH, INTERLEAVED>(c);
+  if constexpr (CH == 1) {
+    return P::template run<T, G, CH, ANYWHERE>(c);
+  } else if constexpr (CH == 2) {
+    if (mode == IN_LANE) return P::template run<T, G, CH, IN_LANE>(c);
+    return P::template run<T, G, CH, G / 2>(c);
+  } else {
+    if (mode == 2) return P::template run<T, G, CH, 2>(c);
+    return P::template run<T, G, CH, 1>(c);
+  }
 }
 
-template <typename T>
-static hipError_t fwd_dispatch(const QkShape& q, const void* in, const void* gq, const void* gk, void* out,
-                               hipStream_t s) {
-  switch (group_lanes(q.head_dim)) {
-    case 8: return fwd_t<T, 8>(q, in, gq, gk, out, s);
-    case 16: return fwd_t<T, 16>(q, in, gq, gk, out, s);
-    default: return fwd_t<T, 32>(q, in, gq, gk, out, s);
-  }
+template <typename P, typename T>
+static hipError_t run_lanes(const QkCall& c) {
+  const QkLanes l = lanes_of(c.q);
+  if (l.CH == 2) return l.G == 4 ? run_mode<P, T, 4, 2>(c, l.mode) : l.G == 8 ? run_mode<P, T, 8, 2>(c, l.mode)
+                                                                             : run_mode<P, T, 16, 2>(c, l.mode);
+  if (l.CH == 3) return run_mode<P, T, 4, 3>(c, l.mode);
+  return l.G == 8 ? run_mode<P, T, 8, 1>(c, l.mode) : l.G == 16 ? run_mode<P, T, 16, 1>(c, l.mode)
+                                                                : run_mode<P, T, 32, 1>(c, l.mode);
 }
 
 hipError_t launch_qk_norm_rope_fwd(int dtype, const QkShape& q, const void* in, const void* gq, const void* gk,
                                    void* out, hipStream_t s) {
-  return dtype == DT_BF16 ? fwd_dispatch<bf16_t>(q, in, gq, gk, out, s) : fwd_dispatch<float>(q, in, gq, gk, out, s);
-}
-
-template <typename T, int G>
-static hipError_t bwd_t(const QkShape& q, const void* dout, const void* in, const void* gq, const void* gk, void* dx,
-                        float* part, hipStream_t s) {
-  const int copy = dout != dx;
-  const dim3 grid(bwd_blocks(q.tokens, q.q_heads, q.kv_heads, q.head_dim));
-  if (q.interleaved)
-    hipLaunchKernelGGL((qk_bwd_kernel<T, G, true>), grid, dim3(256), 0, s, qk_args(q), copy, (const T*)dout,
-                       (const T*)in, (const T*)gq, (const T*)gk, (T*)dx, part);
-  else
-    hipLaunchKernelGGL((qk_bwd_kernel<T, G, false>), grid, dim3(256), 0, s, qk_args(q), copy, (const T*)dout,
-                       (const T*)in, (const T*)gq, (const T*)gk, (T*)dx, part);
-  return hipGetLastError();
-}
-
-template <typename T>
-static hipError_t bwd_dispatch(const QkShape& q, const void* dout, const void* in, const void* gq, const void* gk,
-                               void* dx, float* part, hipStream_t s) {
-  switch (group_lanes(q.head_dim)) {
-    case 8: return bwd_t<T, 8>(q, dout, in, gq, gk, dx, part, s);
-    case 16: return bwd_t<T, 16>(q, dout, in, gq, gk, dx, part, s);
-    default: return bwd_t<T, 32>(q, dout, in, gq, gk, dx, part, s);
-  }
+  const QkCall c{q, nullptr, in, gq, gk, out, nullptr, s};
+  return dtype == DT_BF16 ? run_lanes<Fwd, bf16_t>(c) : run_lanes<Fwd, float>(c);
 }
 
 hipError_t launch_qk_norm_rope_bwd(int dtype, const QkShape& q, const void* dout, const void* in, const void* gq,
                                    const void* gk, void* dx, float* dgq, float* dgk, int accumulate, float* part,
                                    hipStream_t s) {
-  hipError_t e = dtype == DT_BF16 ? bwd_dispatch<bf16_t>(q, dout, in, gq, gk, dx, part, s)
-                                  : bwd_dispatch<float>(q, dout, in, gq, gk, dx, part, s);
+  const QkCall c{q, dout, in, gq, gk, dx, part, s};
+  hipError_t e = dtype == DT_BF16 ? run_lanes<Bwd, bf16_t>(c) : run_lanes<Bwd, float>(c);
   if (e != hipSuccess) return e;
-  const int n = bwd_blocks(q.tokens, q.q_heads, q.kv_heads, q.head_dim);
-  const ReduceJob jobs[2] = {{n, q.head_dim, part, dgq, accumulate},
-                             {n, q.head_dim, part + (size_t)n * q.head_dim, dgk, accumulate}};
-  return launch_reduce_partials_batch(jobs, 2, s);
+  int bq, bk;
+  bwd_blocks(q.tokens, q.q_heads, q.kv_heads, q.head_dim, &bq, &bk);
+  hipLaunchKernelGGL(qk_gain_kernel, dim3(2 * ((q.head_dim + 15) / 16)), dim3(1024), 0, s, q.head_dim,
+                     QkGrid{bq, bk, 0}, part, dgq, dgk, accumulate);
+  return hipGetLastError();
 }
 
 }  // namespace merak

@@ -367,7 +367,7 @@ def test_act8_gelu_backward_of_nan_is_nan():
 
 
 DW = [(1, 8, 32), (2, 64, 64), (63, 72, 96), (64, 128, 128), (65, 136, 160), (333, 264, 288), (130, 520, 32),
-      (1000, 256, 640), (5000, 64, 64), (129, 1000, 1056)]
+      (1000, 256, 640), (5000, 64, 64), (129, 1000, 1056), (1, 4104, 2592), (200, 4104, 2592), (700, 3848, 2688)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
