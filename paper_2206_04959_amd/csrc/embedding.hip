@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(256) embedding_fwd_kernel(int tokens, int hidd
 // ---------------------------------------------------------------------------
 // Backward
 // ---------------------------------------------------------------------------
-constexpr int kDirect = 64;       // up to here one launch, without sorting
+constexpr int kDirect = 256;      // up to here one launch, without sorting
 constexpr int kSortBlock = 2048;  // tokens that are ranked against each other
 constexpr int kFillRows = 16;     // table rows that a workgroup clears
 constexpr int kSlab = 512;        // columns of a wave: 8 a lane
@@ -90,43 +90,67 @@ static inline int chunk_len(int tokens) {
   return std::max(kMinChunk, (c + 15) / 16 * 16);
 }
 
-// Rank of each token within its block of kSortBlock by (row, token): the number
-// of tokens of the block that come before it.  A workgroup ranks 64 tokens, each
-// of its four waves against a quarter of the block.  Comparing every pair is
-// kSortBlock comparisons a token with no dependence between them, in one launch;
-// 16384 tokens give every SIMD one wave.
+// Rank of each token within its block of kSortBlock by (row, token): the number of
+// tokens of the block that come before it.  A workgroup ranks 64 tokens, each of its
+// eight waves against an eighth of the block.  Comparing every pair costs two
+// instructions a pair and no dependence between them, in one launch; the keys go
+// through LDS as four-key reads that all lanes share.
+constexpr int kRankWaves = 8;
+
 template <typename I>
-__global__ void __launch_bounds__(256) embedding_rank_kernel(int tokens, int rows, long long first,
-                                                             const I* __restrict__ ids, int* __restrict__ skey,
-                                                             int* __restrict__ stok) {
+__global__ void __launch_bounds__(64 * kRankWaves) embedding_rank_kernel(int tokens, int rows, long long first,
+                                                                         const I* __restrict__ ids,
+                                                                         int* __restrict__ skey,
+                                                                         int* __restrict__ stok) {
+  constexpr int NT = 64 * kRankWaves, PER = kSortBlock / NT, Q = kSortBlock / kRankWaves;
   __shared__ __align__(16) unsigned key[kSortBlock];  // past the last token: above every row
-  __shared__ int cnt[4][64];
+  __shared__ int cnt[kRankWaves][64];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int t0 = blockIdx.x * 64;                 // first token of this workgroup
-  const int b0 = t0 / kSortBlock * kSortBlock;    // first token of its block
-  const int slice = t0 - b0;
-  for (int j = threadIdx.x; j < kSortBlock; j += 256)
-    key[j] = b0 + j < tokens ? (unsigned)table_row(ids[b0 + j], first, rows) : 0xfffffffeu;
+  const int t0 = blockIdx.x * 64;               // first token of this workgroup
+  const int b0 = t0 / kSortBlock * kSortBlock;  // first token of its block
+  const int slice = t0 - b0, m = min(kSortBlock, tokens - b0);
+  I id[PER];
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    const int j = threadIdx.x + NT * u;
+    id[u] = j < m ? ids[b0 + j] : (I)0;
+  }
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    const int j = threadIdx.x + NT * u;
+    key[j] = j < m ? (unsigned)table_row(id[u], first, rows) : 0xfffffffeu;
+  }
   __syncthreads();
   const unsigned k = key[slice + lane];
-  // tokens before the slice count if their row is not larger, tokens after it if smaller
-  constexpr int Q = kSortBlock / 4;
+  // A token before the slice counts if its row is not larger, one after it if smaller.
   int n = 0;
-  for (int j = w * Q; j < (w + 1) * Q; j += 4) {
-    const unsigned* kj = key + j;
-    if (j < slice || j >= slice + 64) {
-      const unsigned thr = j < slice ? k + 1 : k;
+  auto count = [&](int lo, int hi, unsigned thr) {  // multiples of 64
+    for (int j = lo; j < hi; j += 16) {
+      u32x4_t v[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) n += kj[e] < thr;
-    } else {
+      for (int u = 0; u < 4; ++u) v[u] = *reinterpret_cast<const u32x4_t*>(key + j + 4 * u);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) n += kj[e] < (j + e < slice + lane ? k + 1 : k);
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) n += v[u][e] < thr;
+    }
+  };
+  const int lo = w * Q, hi = min(lo + Q, (m + 63) & ~63);
+  count(lo, min(hi, slice), k + 1);
+  count(max(lo, slice + 64), hi, k);
+  if (slice >= lo && slice < hi) {
+    for (int j = 0; j < 64; j += 4) {
+      const u32x4_t v = *reinterpret_cast<const u32x4_t*>(key + slice + j);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) n += v[e] < (j + e < lane ? k + 1 : k);
     }
   }
   cnt[w][lane] = n;
   __syncthreads();
   if (w == 0 && t0 + lane < tokens) {
-    const int r = cnt[0][lane] + cnt[1][lane] + cnt[2][lane] + cnt[3][lane];
+    int r = 0;
+#pragma unroll
+    for (int i = 0; i < kRankWaves; ++i) r += cnt[i][lane];
     skey[b0 + r] = (int)k;
     stok[b0 + r] = t0 + lane;
   }
@@ -134,21 +158,23 @@ __global__ void __launch_bounds__(256) embedding_rank_kernel(int tokens, int row
 
 // Whole order from the sorted blocks: a token's position is the number of tokens
 // before it in each block, found by binary search.  A workgroup places 64 tokens,
-// its waves search every fourth block.
-__global__ void __launch_bounds__(256) embedding_merge_kernel(int tokens, const int* __restrict__ skey,
-                                                              const int* __restrict__ stok, int* __restrict__ gkey,
-                                                              int* __restrict__ gtok) {
-  __shared__ int cnt[4][64];
+// its 16 waves search every 16th block: a search is a chain of 12 loads, so they are
+// spread wide.
+constexpr int kMergeWaves = 16;
+
+__global__ void __launch_bounds__(64 * kMergeWaves) embedding_merge_kernel(int tokens, const int* __restrict__ skey,
+                                                                           const int* __restrict__ stok,
+                                                                           int* __restrict__ gkey,
+                                                                           int* __restrict__ gtok) {
+  __shared__ int cnt[kMergeWaves][64];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int p = blockIdx.x * 64 + lane;
   const int b = blockIdx.x * 64 / kSortBlock, nb = (tokens + kSortBlock - 1) / kSortBlock;
   const int k = p < tokens ? skey[p] : 0;
-  int n = 0;
-  for (int o = w; o < nb; o += 4) {
-    if (o == b) {
-      n += p - b * kSortBlock;
-      continue;
-    }
+  const int t = p < tokens ? stok[p] : 0;
+  int n = w == b % kMergeWaves ? p - b * kSortBlock : 0;  // those of its own block
+  for (int o = w; o < nb; o += kMergeWaves) {
+    if (o == b) continue;
     const int* kb = skey + (size_t)o * kSortBlock;
     const int m = min(kSortBlock, tokens - o * kSortBlock);
     const int thr = o < b ? k + 1 : k;
@@ -161,9 +187,11 @@ __global__ void __launch_bounds__(256) embedding_merge_kernel(int tokens, const 
   cnt[w][lane] = n;
   __syncthreads();
   if (w == 0 && p < tokens) {
-    const int g = cnt[0][lane] + cnt[1][lane] + cnt[2][lane] + cnt[3][lane];
+    int g = 0;
+#pragma unroll
+    for (int i = 0; i < kMergeWaves; ++i) g += cnt[i][lane];
     gkey[g] = k;
-    gtok[g] = stok[p];
+    gtok[g] = t;
   }
 }
 
@@ -218,7 +246,7 @@ struct EmbeddingSum {
 // The workgroups after those clear the rows that no token names.
 template <typename T>
 __global__ void __launch_bounds__(256) embedding_sum_kernel(EmbeddingSum a, const T* __restrict__ dy) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if ((int)blockIdx.x >= a.sum_blocks) {
     __shared__ int used[kFillRows];
     const int r0 = (blockIdx.x - a.sum_blocks) * kFillRows;
@@ -286,9 +314,11 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(EmbeddingSum a, cons
 }
 
 // Adds the parts of a run that spans chunks, for the chunk in which it begins:
-// four waves take every fourth part, and their sums are added in wave order.
-__global__ void __launch_bounds__(256) embedding_join_kernel(EmbeddingSum a) {
-  __shared__ float red[3][64][9];
+// eight waves take every eighth part, and their sums are added in wave order.
+constexpr int kJoinWaves = 8;
+
+__global__ void __launch_bounds__(64 * kJoinWaves) embedding_join_kernel(EmbeddingSum a) {
+  __shared__ float red[kJoinWaves - 1][64][9];
   const int slabs = (a.hidden + kSlab - 1) / kSlab;
   const int c = blockIdx.x / slabs;
   const int lo = c * a.chunk, hi = min(lo + a.chunk, a.tokens);
@@ -297,15 +327,15 @@ __global__ void __launch_bounds__(256) embedding_join_kernel(EmbeddingSum a) {
   if (k >= a.rows || a.key[hi] != k || (lo > 0 && a.key[lo - 1] == k)) return;
   const int end = lower_bound(a.key, a.tokens, k + 1) - 1;  // last position of the run
   const int last = end / a.chunk;
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = (blockIdx.x % slabs) * kSlab + lane * 8;
   const bool live = col < a.hidden;
   float acc[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
   if (live) {
-#pragma unroll 4
-    for (int i = c + w; i <= last; i += 4) {
+#pragma unroll 8
+    for (int i = c + w; i <= last; i += kJoinWaves) {
       float v[8];
       load8(a.part + ((size_t)i * 2 + (i == c)) * a.hidden + col, v);
 #pragma unroll
@@ -318,44 +348,79 @@ __global__ void __launch_bounds__(256) embedding_join_kernel(EmbeddingSum a) {
   __syncthreads();
   if (w == 0 && live) {
 #pragma unroll
-    for (int i = 0; i < 3; ++i)
+    for (int i = 0; i < kJoinWaves - 1; ++i)
 #pragma unroll
       for (int e = 0; e < 8; ++e) acc[e] += red[i][lane][e];
     write_row(a.out + (size_t)k * a.hidden + col, acc, a.scale, a.accumulate);
   }
 }
 
-// Up to 64 tokens: every wave holds all rows in its lanes.  A wave per token and
-// 512 columns; the first token of a row adds the row's tokens in order.
+// Up to kDirect tokens: every wave holds all rows in its lanes, four a lane.  A wave per
+// token and 512 columns; the first token of a row adds the row's tokens in order.
 template <typename T, typename I>
 __global__ void __launch_bounds__(256) embedding_direct_kernel(EmbeddingSum a, long long first,
                                                                const I* __restrict__ ids, const T* __restrict__ dy) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int key = lane < a.tokens ? table_row(ids[lane], first, a.rows) : a.rows;
+  constexpr int KG = kDirect / 64;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int key[KG];
+#pragma unroll
+  for (int g = 0; g < KG; ++g) {
+    const int t = 64 * g + lane;
+    key[g] = t < a.tokens ? table_row(ids[t], first, a.rows) : a.rows;
+  }
   if ((int)blockIdx.x >= a.sum_blocks) {
     const int r0 = (blockIdx.x - a.sum_blocks) * kFillRows;
-    for (int i = w; i < kFillRows && r0 + i < a.rows; i += 4)
-      if (__ballot(key == r0 + i) == 0ull) clear_row(a.out + (size_t)(r0 + i) * a.hidden, a.hidden, lane);
+    for (int i = w; i < kFillRows && r0 + i < a.rows; i += 4) {
+      bool used = false;
+#pragma unroll
+      for (int g = 0; g < KG; ++g) used |= key[g] == r0 + i;
+      if (__ballot(used) == 0ull) clear_row(a.out + (size_t)(r0 + i) * a.hidden, a.hidden, lane);
+    }
     return;
   }
   const int slabs = (a.hidden + kSlab - 1) / kSlab;
   const int unit = blockIdx.x * 4 + w;
   const int t = unit / slabs, col = (unit % slabs) * kSlab + lane * 8;
   if (t >= a.tokens) return;
-  const int k = __builtin_amdgcn_readlane(key, t);
+  int k = a.rows;
+#pragma unroll
+  for (int g = 0; g < KG; ++g)
+    if (t >> 6 == g) k = __builtin_amdgcn_readlane(key[g], t & 63);
   if (k >= a.rows) return;
-  unsigned long long run = __ballot(key == k);
-  if (__builtin_ctzll(run) != t || col >= a.hidden) return;
+  unsigned long long run[KG];
+  int head = -1;  // the row's first token
+#pragma unroll
+  for (int g = KG - 1; g >= 0; --g) {
+    run[g] = __ballot(key[g] == k);
+    if (run[g]) head = 64 * g + __builtin_ctzll(run[g]);
+  }
+  if (head != t) return;
+  const bool live = col < a.hidden;
   float acc[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
-  for (; run; run &= run - 1) {
-    float v[8];
-    load8(dy + (size_t)__builtin_ctzll(run) * a.hidden + col, v);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] += v[e];
+  for (int g = 0; g < KG; ++g) {
+    unsigned long long r = run[g];
+    while (r) {
+      constexpr int U = 8;  // rows in flight
+      float v[U][8];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[u][e] = 0.0f;
+        if (r) {
+          if (live) load8(dy + (size_t)(64 * g + __builtin_ctzll(r)) * a.hidden + col, v[u]);
+          r &= r - 1;
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] += v[u][e];
+    }
   }
-  write_row(a.out + (size_t)k * a.hidden + col, acc, a.scale, a.accumulate);
+  if (live) write_row(a.out + (size_t)k * a.hidden + col, acc, a.scale, a.accumulate);
 }
 
 // ---------------------------------------------------------------------------
@@ -410,12 +475,12 @@ static hipError_t bwd_t(EmbeddingSum a, long long first, const void* ids, const 
   int* stok = (int*)(scratch + 3 * ob);
   const bool one = a.tokens <= kSortBlock;  // one block: its order is the whole order
   const unsigned wg = (unsigned)(((long long)a.tokens + 63) / 64);
-  hipLaunchKernelGGL((embedding_rank_kernel<I>), dim3(wg), dim3(256), 0, s, a.tokens, a.rows, first, (const I*)ids,
+  hipLaunchKernelGGL((embedding_rank_kernel<I>), dim3(wg), dim3(64 * kRankWaves), 0, s, a.tokens, a.rows, first, (const I*)ids,
                      one ? gkey : skey, one ? gtok : stok);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (!one) {
-    hipLaunchKernelGGL(embedding_merge_kernel, dim3(wg), dim3(256), 0, s, a.tokens, skey, stok, gkey, gtok);
+    hipLaunchKernelGGL(embedding_merge_kernel, dim3(wg), dim3(64 * kMergeWaves), 0, s, a.tokens, skey, stok, gkey, gtok);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -429,7 +494,7 @@ static hipError_t bwd_t(EmbeddingSum a, long long first, const void* ids, const 
                      (const T*)dy);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(embedding_join_kernel, dim3((unsigned)units), dim3(256), 0, s, a);
+  hipLaunchKernelGGL(embedding_join_kernel, dim3((unsigned)units), dim3(64 * kJoinWaves), 0, s, a);
   return hipGetLastError();
 }
 

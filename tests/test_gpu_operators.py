@@ -98,7 +98,7 @@ def test_embedding_forward(dtype, tokens, hidden, rows, first, ids_type):
 
 
 EMBED_BWD = [(1, 8, 1, 0), (2, 1600, 5, 0), (63, 72, 40, 7), (64, 520, 33, 100), (65, 64, 40, 7), (200, 1000, 17, 0),
-             (2047, 40, 300, 0), (2048, 16, 60, 9), (2049, 16, 3000, 0), (5003, 24, 100, 50), (17000, 8, 90, 0)]
+             (255, 24, 90, 5), (256, 520, 7, 0), (257, 8, 200, 0), (2047, 40, 300, 0), (2048, 16, 60, 9), (2049, 16, 3000, 0), (5003, 24, 100, 50), (17000, 8, 90, 0), (33000, 8, 9, 3)]
 
 
 @pytest.mark.parametrize("pattern", ["mixed", "same", "none", "falling", "few"])
