@@ -14,6 +14,7 @@
 // floating-point atomics, and rows without a token are written as zeros by the
 // same launch.
 #include <algorithm>
+#include <atomic>
 
 #include "common.h"
 #include "kernels.h"
@@ -82,6 +83,7 @@ constexpr int kSortBlock = 2048;  // tokens that are ranked against each other
 constexpr int kFillRows = 16;     // table rows that a workgroup clears
 constexpr int kSlab = 512;        // columns of a wave: 8 a lane
 constexpr int kMinChunk = 16, kMaxChunks = 1024;
+constexpr int kWhole = 32;        // a run of up to this many tokens is never split
 
 // Sorted positions per unit of work: at most kMaxChunks units, whole multiples
 // of 16 positions.
@@ -92,16 +94,18 @@ static inline int chunk_len(int tokens) {
 
 // Rank of each token within its block of kSortBlock by (row, token): the number of
 // tokens of the block that come before it.  A workgroup ranks 64 tokens, each of its
-// eight waves against an eighth of the block.  Comparing every pair costs two
+// 16 waves against 128 of the block.  Comparing every pair costs two
 // instructions a pair and no dependence between them, in one launch; the keys go
 // through LDS as four-key reads that all lanes share.
-constexpr int kRankWaves = 8;
+constexpr int kRankWaves = 16;
 
 template <typename I>
 __global__ void __launch_bounds__(64 * kRankWaves) embedding_rank_kernel(int tokens, int rows, long long first,
                                                                          const I* __restrict__ ids,
                                                                          int* __restrict__ skey,
-                                                                         int* __restrict__ stok) {
+                                                                         int* __restrict__ stok,
+                                                                         int* __restrict__ split) {
+  if (blockIdx.x == 0 && threadIdx.x == 0) *split = 0;  // for embedding_sum_kernel
   constexpr int NT = 64 * kRankWaves, PER = kSortBlock / NT, Q = kSortBlock / kRankWaves;
   __shared__ __align__(16) unsigned key[kSortBlock];  // past the last token: above every row
   __shared__ int cnt[kRankWaves][64];
@@ -125,12 +129,12 @@ __global__ void __launch_bounds__(64 * kRankWaves) embedding_rank_kernel(int tok
   // A token before the slice counts if its row is not larger, one after it if smaller.
   int n = 0;
   auto count = [&](int lo, int hi, unsigned thr) {  // multiples of 64
-    for (int j = lo; j < hi; j += 16) {
-      u32x4_t v[4];
+    for (int j = lo; j < hi; j += 32) {
+      u32x4_t v[8];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) v[u] = *reinterpret_cast<const u32x4_t*>(key + j + 4 * u);
+      for (int u = 0; u < 8; ++u) v[u] = *reinterpret_cast<const u32x4_t*>(key + j + 4 * u);
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
+      for (int u = 0; u < 8; ++u)
 #pragma unroll
         for (int e = 0; e < 4; ++e) n += v[u][e] < thr;
     }
@@ -139,6 +143,7 @@ __global__ void __launch_bounds__(64 * kRankWaves) embedding_rank_kernel(int tok
   count(lo, min(hi, slice), k + 1);
   count(max(lo, slice + 64), hi, k);
   if (slice >= lo && slice < hi) {
+#pragma unroll
     for (int j = 0; j < 64; j += 4) {
       const u32x4_t v = *reinterpret_cast<const u32x4_t*>(key + slice + j);
 #pragma unroll
@@ -157,55 +162,69 @@ __global__ void __launch_bounds__(64 * kRankWaves) embedding_rank_kernel(int tok
 }
 
 // Whole order from the sorted blocks: a token's position is the number of tokens
-// before it in each block, found by binary search.  A workgroup places 64 tokens,
-// its 16 waves search every 16th block: a search is a chain of 12 loads, so they are
-// spread wide.
+// before it in each block, found by binary search.  A workgroup places 64 tokens;
+// each of its waves (one a block, at most 16) brings a block's keys into LDS and
+// searches there: twelve dependent loads from L2 instead took 4 of 5 us.
 constexpr int kMergeWaves = 16;
 
 __global__ void __launch_bounds__(64 * kMergeWaves) embedding_merge_kernel(int tokens, const int* __restrict__ skey,
                                                                            const int* __restrict__ stok,
                                                                            int* __restrict__ gkey,
                                                                            int* __restrict__ gtok) {
-  __shared__ int cnt[kMergeWaves][64];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  extern __shared__ __align__(16) int block_keys[];  // [waves][kSortBlock], then the counts [waves][64]
+  const int waves = blockDim.x >> 6;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int* mine = block_keys + w * kSortBlock;
+  int* cnt = block_keys + waves * kSortBlock;
   const int p = blockIdx.x * 64 + lane;
   const int b = blockIdx.x * 64 / kSortBlock, nb = (tokens + kSortBlock - 1) / kSortBlock;
   const int k = p < tokens ? skey[p] : 0;
   const int t = p < tokens ? stok[p] : 0;
-  int n = w == b % kMergeWaves ? p - b * kSortBlock : 0;  // those of its own block
-  for (int o = w; o < nb; o += kMergeWaves) {
+  int n = w == b % waves ? p - b * kSortBlock : 0;  // those of its own block
+  for (int o = w; o < nb; o += waves) {
     if (o == b) continue;
     const int* kb = skey + (size_t)o * kSortBlock;
     const int m = min(kSortBlock, tokens - o * kSortBlock);
+    constexpr int L = kSortBlock / 256;
+    u32x4_t v[L];
+#pragma unroll
+    for (int u = 0; u < L; ++u) {
+      const int j = 256 * u + lane * 4;  // skey holds whole blocks: keys past m are read and not used
+      v[u] = *reinterpret_cast<const u32x4_t*>(kb + j);
+    }
+#pragma unroll
+    for (int u = 0; u < L; ++u) *reinterpret_cast<u32x4_t*>(mine + 256 * u + lane * 4) = v[u];
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the keys are this wave's own
     const int thr = o < b ? k + 1 : k;
     int pos = 0;  // tokens known to come before
 #pragma unroll
     for (int step = kSortBlock; step > 0; step >>= 1)
-      if (pos + step <= m && kb[pos + step - 1] < thr) pos += step;
+      if (pos + step <= m && mine[pos + step - 1] < thr) pos += step;
     n += pos;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   }
-  cnt[w][lane] = n;
+  cnt[w * 64 + lane] = n;
   __syncthreads();
   if (w == 0 && p < tokens) {
     int g = 0;
-#pragma unroll
-    for (int i = 0; i < kMergeWaves; ++i) g += cnt[i][lane];
+    for (int i = 0; i < waves; ++i) g += cnt[i * 64 + lane];
     gkey[g] = k;
     gtok[g] = t;
   }
 }
 
-// First sorted position whose row is not below r.
-__device__ __forceinline__ int lower_bound(const int* key, int n, int r) {
+// First sorted position whose row is not below r, by 16 neighbouring lanes together: they
+// probe 16 places at a time, so 2^14 keys take four dependent loads.
+__device__ __forceinline__ int lower_bound16(const int* key, int n, int r, int lane) {
   int lo = 0;
-  while (n > 0) {
-    const int half = n >> 1;
-    if (key[lo + half] < r) {
-      lo += half + 1;
-      n -= half + 1;
-    } else {
-      n = half;
-    }
+  while (n > 0) {  // the same for the 16 lanes
+    const int step = (n + 15) >> 4, at = (lane & 15) * step;
+    const unsigned long long votes = __ballot(at < n && key[lo + at] < r);
+    const int below = __builtin_popcount((unsigned)(votes >> (lane & 48)) & 0xffffu);  // probes below r come first
+    if (below == 0) return lo;
+    const int from = (below - 1) * step + 1, to = min(below * step, n);
+    lo += from;
+    n = to - from;
   }
   return lo;
 }
@@ -234,15 +253,36 @@ struct EmbeddingSum {
   const int* key;   // [tokens] rows in order, `rows` for tokens without one
   const int* tok;   // [tokens] the tokens in that order
   float* part;      // [chunks][2][hidden]
+  int* split;       // split[0]: how many runs are split, then the chunks in which they begin
   float* out;       // [rows][hidden]
   int sum_blocks;   // workgroups that sum; the rest clear rows
 };
 
-// Sums over runs of equal rows.  A wave takes `chunk` sorted positions and 512
-// columns and adds the tokens of a run in order.  A run within the chunk is
-// finished here.  Of a run that other chunks share, the chunk's part goes to
-// part[c][1] if the run begins in the chunk, else to part[c][0];
-// embedding_join_kernel adds them up.
+// Tokens of the run across the border at sorted position p > 0, counted to both sides of
+// it and up to kWhole each (0, 0: no run crosses it).  k: the lane's key, at p - 32 + lane.
+struct Across {
+  int before, after;
+  __device__ __forceinline__ bool whole() const { return before + after <= kWhole; }
+};
+
+__device__ __forceinline__ int key_at(const EmbeddingSum& a, int p) { return p >= 0 && p < a.tokens ? a.key[p] : -1; }
+
+__device__ __forceinline__ Across run_across(const EmbeddingSum& a, int p, int k) {
+  static_assert(kWhole == 32, "a half of the wave looks at each side");
+  const int here = __builtin_amdgcn_readlane(k, 32);
+  const unsigned long long same = __ballot(k == here && here < a.rows && p > 0 && p < a.tokens);
+  const unsigned lo = ~(unsigned)same, hi = ~(unsigned)(same >> 32);
+  const int before = lo ? __builtin_clz(lo) : 32;
+  if (before == 0) return {0, 0};
+  return {before, hi ? __builtin_ctz(hi) : 32};
+}
+
+// Sums over runs of equal rows.  A wave takes 512 columns of the runs that begin in
+// `chunk` sorted positions, and adds the tokens of a run in order.  A run of up to kWhole
+// tokens is finished by the chunk in which it begins, wherever it ends.  Of a longer
+// one that crosses chunks each chunk adds its own positions, into part[c][1] if the run
+// begins in the chunk, else into part[c][0]; the chunk in which it begins is noted, and
+// embedding_join_kernel adds the parts.
 // The workgroups after those clear the rows that no token names.
 template <typename T>
 __global__ void __launch_bounds__(256) embedding_sum_kernel(EmbeddingSum a, const T* __restrict__ dy) {
@@ -250,11 +290,10 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(EmbeddingSum a, cons
   if ((int)blockIdx.x >= a.sum_blocks) {
     __shared__ int used[kFillRows];
     const int r0 = (blockIdx.x - a.sum_blocks) * kFillRows;
-    if (threadIdx.x < kFillRows) {
-      const int r = r0 + threadIdx.x;
-      const int p = lower_bound(a.key, a.tokens, r);
-      used[threadIdx.x] = p < a.tokens && a.key[p] == r;
-    }
+    static_assert(kFillRows * 16 == 256, "16 lanes look for a row");
+    const int r = r0 + (threadIdx.x >> 4);
+    const int p = lower_bound16(a.key, a.tokens, r, lane);
+    if ((lane & 15) == 0) used[threadIdx.x >> 4] = p < a.tokens && a.key[p] == r;
     __syncthreads();
     for (int i = w; i < kFillRows && r0 + i < a.rows; i += 4)
       if (!used[i]) clear_row(a.out + (size_t)(r0 + i) * a.hidden, a.hidden, lane);
@@ -262,96 +301,124 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(EmbeddingSum a, cons
   }
   const int slabs = (a.hidden + kSlab - 1) / kSlab;
   const int unit = blockIdx.x * 4 + w;
-  const int c = unit / slabs, col = (unit % slabs) * kSlab + lane * 8;
+  const int c = unit / slabs, slab = unit % slabs, col = slab * kSlab + lane * 8;
   const int lo = c * a.chunk, hi = min(lo + a.chunk, a.tokens);
   if (lo >= a.tokens) return;
   const bool live = col < a.hidden;
-  const int before = lo > 0 ? a.key[lo - 1] : -1;
-  const int after = hi < a.tokens ? a.key[hi] : -1;
+  // All keys that the borders and the first 64 positions need, in one step: every load
+  // here waits for another kernel's stores.
+  const int k_lo = key_at(a, lo - 32 + lane), k_hi = key_at(a, hi - 32 + lane);
+  int k_here = key_at(a, lo + lane), t_here = lo + lane < a.tokens ? a.tok[lo + lane] : 0;
+  const Across first = run_across(a, lo, k_lo), last = run_across(a, hi, k_hi);
+  const int begin = first.whole() ? lo + first.after : lo;
+  if (begin >= hi) return;  // all of it belongs to a run that began before
+  const int end = last.whole() ? hi + last.after : hi;
+  // a split run's row at either end
+  const int before = first.before && !first.whole() ? __builtin_amdgcn_readlane(k_lo, 32) : -1;
+  const int after = last.before && !last.whole() ? __builtin_amdgcn_readlane(k_hi, 32) : -1;
   int cur = -1;
   float acc[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
   float* head = a.part + ((size_t)c * 2) * a.hidden + col;
-  for (int base = lo; base < hi; base += 64) {
-    const int m = min(64, hi - base);
-    const int kk = lane < m ? a.key[base + lane] : a.rows;
-    const int tt = lane < m ? a.tok[base + lane] : 0;
-    constexpr int U = 4;
-    for (int i = 0; i < m; i += U) {
-      float v[U][8];
-      int k[U];
+  for (int base = lo; base < end; base += 64) {
+    if (base > lo) {
+      k_here = key_at(a, base + lane);
+      t_here = base + lane < a.tokens ? a.tok[base + lane] : 0;
+    }
+    const int m = min(64, end - base);
+    constexpr int U = sizeof(T) == 2 ? 16 : 8;  // rows in flight
+    constexpr int W = sizeof(T) / 2;            // 16-byte pieces of 8 columns
+    for (int i = base == lo ? begin - lo : 0; i < m; i += U) {
+      u32x4_t v[U][W];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        k[u] = __builtin_amdgcn_readlane(kk, i + u);  // i + u < 64; lanes past m hold `rows`
-        const size_t t = (size_t)__builtin_amdgcn_readlane(tt, i + u);
+        if (i + u >= m || __builtin_amdgcn_readlane(k_here, (i + u) & 63) >= a.rows) break;  // no more rows
+        const T* p = dy + (size_t)__builtin_amdgcn_readlane(t_here, (i + u) & 63) * a.hidden + col;
+        if (live) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[u][e] = 0.0f;
-        if (live && k[u] < a.rows) load8(dy + t * a.hidden + col, v[u]);
+          for (int e = 0; e < W; ++e) v[u][e] = reinterpret_cast<const u32x4_t*>(p)[e];
+        }
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        if (k[u] != cur) {
+        if (i + u >= m) break;
+        const int k = __builtin_amdgcn_readlane(k_here, (i + u) & 63);
+        if (k != cur) {
           if (cur >= 0 && live) {
             if (cur == before) store8(head, acc);
             else write_row(a.out + (size_t)cur * a.hidden + col, acc, a.scale, a.accumulate);
           }
-          cur = k[u] < a.rows ? k[u] : -1;
+          cur = k < a.rows ? k : -1;
 #pragma unroll
           for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
         }
+        if (cur < 0) break;  // only tokens without a row from here on
+        float f[8];
+        if constexpr (W == 1) {
+          unpack8(v[u][0], f);
+        } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] += v[u][e];
+          for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(v[u][e >> 2][e & 3]);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] += f[e];
       }
-      if (k[U - 1] >= a.rows) break;  // only tokens without a row from here on
     }
   }
-  if (cur >= 0 && live) {
-    if (cur == before) store8(head, acc);
-    else if (cur == after) store8(head + a.hidden, acc);
-    else write_row(a.out + (size_t)cur * a.hidden + col, acc, a.scale, a.accumulate);
+  if (cur < 0) return;
+  if (cur == before) {
+    if (live) store8(head, acc);
+  } else if (cur == after) {
+    if (live) store8(head + a.hidden, acc);
+    if (slab == 0 && lane == 0) a.split[1 + atomicAdd(a.split, 1)] = c;
+  } else if (live) {
+    write_row(a.out + (size_t)cur * a.hidden + col, acc, a.scale, a.accumulate);
   }
 }
 
-// Adds the parts of a run that spans chunks, for the chunk in which it begins:
-// eight waves take every eighth part, and their sums are added in wave order.
-constexpr int kJoinWaves = 8;
+// Adds the parts of the split runs: a workgroup takes a run and 512 columns at a time, its
+// 16 waves every 16th part, and their sums are added in wave order.  (The runs are
+// listed in any order; each one's sum has its own.)
+constexpr int kJoinWaves = 16, kJoinBlocks = 128;
 
 __global__ void __launch_bounds__(64 * kJoinWaves) embedding_join_kernel(EmbeddingSum a) {
+  static_assert(64 * kJoinWaves >= kMaxChunks, "a thread a chunk");
   __shared__ float red[kJoinWaves - 1][64][9];
   const int slabs = (a.hidden + kSlab - 1) / kSlab;
-  const int c = blockIdx.x / slabs;
-  const int lo = c * a.chunk, hi = min(lo + a.chunk, a.tokens);
-  if (hi >= a.tokens) return;
-  const int k = a.key[hi - 1];
-  if (k >= a.rows || a.key[hi] != k || (lo > 0 && a.key[lo - 1] == k)) return;
-  const int end = lower_bound(a.key, a.tokens, k + 1) - 1;  // last position of the run
-  const int last = end / a.chunk;
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int col = (blockIdx.x % slabs) * kSlab + lane * 8;
-  const bool live = col < a.hidden;
-  float acc[8];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int items = a.split[0] * slabs;
+  for (int item = blockIdx.x; item < items; item += kJoinBlocks) {
+    const int c = a.split[1 + item / slabs];
+    const int k = a.key[(c + 1) * a.chunk - 1];
+    // the chunks after c that begin inside the run (there are at most kMaxChunks)
+    const long long at = (long long)(c + 1 + (int)threadIdx.x) * a.chunk;
+    const int last = c + __syncthreads_count(at < a.tokens && a.key[at] == k);
+    const int col = (item % slabs) * kSlab + lane * 8;
+    const bool live = col < a.hidden;
+    float acc[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
-  if (live) {
+    for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
+    if (live) {
 #pragma unroll 8
-    for (int i = c + w; i <= last; i += kJoinWaves) {
-      float v[8];
-      load8(a.part + ((size_t)i * 2 + (i == c)) * a.hidden + col, v);
+      for (int i = c + w; i <= last; i += kJoinWaves) {
+        float v[8];
+        load8(a.part + ((size_t)i * 2 + (i == c)) * a.hidden + col, v);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] += v[e];
+        for (int e = 0; e < 8; ++e) acc[e] += v[e];
+      }
     }
-  }
-  if (w > 0)
+    if (w > 0)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) red[w - 1][lane][e] = acc[e];
-  __syncthreads();
-  if (w == 0 && live) {
+      for (int e = 0; e < 8; ++e) red[w - 1][lane][e] = acc[e];
+    __syncthreads();
+    if (w == 0 && live) {
+      for (int i = 0; i < kJoinWaves - 1; ++i)
 #pragma unroll
-    for (int i = 0; i < kJoinWaves - 1; ++i)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] += red[i][lane][e];
-    write_row(a.out + (size_t)k * a.hidden + col, acc, a.scale, a.accumulate);
+        for (int e = 0; e < 8; ++e) acc[e] += red[i][lane][e];
+      write_row(a.out + (size_t)k * a.hidden + col, acc, a.scale, a.accumulate);
+    }
+    __syncthreads();
   }
 }
 
@@ -446,15 +513,16 @@ hipError_t launch_embedding_fwd(int dtype, int id_type, int tokens, int hidden, 
                            : fwd_t<float, long long>(tokens, hidden, rows, first, scale, ids, table, y, s);
 }
 
-// Scratch: the sorted blocks' rows and tokens, the whole order's rows and
-// tokens, and the parts of runs that span chunks.
-static size_t order_bytes(int tokens) { return ((size_t)tokens * 4 + 255) / 256 * 256; }
+// Scratch: the sorted blocks' rows and tokens, the whole order's rows and tokens, the
+// list of split runs, and their parts.
+// (The orders are held in whole blocks: embedding_merge_kernel reads them so.)
+static size_t order_bytes(int tokens) { return ((size_t)tokens + kSortBlock - 1) / kSortBlock * kSortBlock * 4; }
 
 size_t embedding_scratch_bytes(int tokens, int hidden) {
   if (tokens <= kDirect) return 0;
   const int len = chunk_len(tokens);
   const size_t chunks = ((size_t)tokens + len - 1) / len;
-  return 4 * order_bytes(tokens) + chunks * 2 * hidden * sizeof(float);
+  return 4 * order_bytes(tokens) + order_bytes(1 + kMaxChunks) + chunks * 2 * hidden * sizeof(float);
 }
 
 template <typename T, typename I>
@@ -473,28 +541,35 @@ static hipError_t bwd_t(EmbeddingSum a, long long first, const void* ids, const 
   int* gtok = (int*)(scratch + ob);
   int* skey = (int*)(scratch + 2 * ob);
   int* stok = (int*)(scratch + 3 * ob);
+  a.split = (int*)(scratch + 4 * ob);
   const bool one = a.tokens <= kSortBlock;  // one block: its order is the whole order
   const unsigned wg = (unsigned)(((long long)a.tokens + 63) / 64);
   hipLaunchKernelGGL((embedding_rank_kernel<I>), dim3(wg), dim3(64 * kRankWaves), 0, s, a.tokens, a.rows, first, (const I*)ids,
-                     one ? gkey : skey, one ? gtok : stok);
+                     one ? gkey : skey, one ? gtok : stok, a.split);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (!one) {
-    hipLaunchKernelGGL(embedding_merge_kernel, dim3(wg), dim3(64 * kMergeWaves), 0, s, a.tokens, skey, stok, gkey, gtok);
+    const int waves = std::min(kMergeWaves, (a.tokens + kSortBlock - 1) / kSortBlock);
+    const size_t lds = (size_t)waves * (kSortBlock + 64) * sizeof(int);
+    static std::atomic<uint64_t> lds_set{0};
+    e = allow_dynamic_lds(reinterpret_cast<const void*>(embedding_merge_kernel),
+                          (size_t)kMergeWaves * (kSortBlock + 64) * sizeof(int), lds_set);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(embedding_merge_kernel, dim3(wg), dim3(64 * waves), lds, s, a.tokens, skey, stok, gkey, gtok);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   a.chunk = chunk_len(a.tokens);
   a.key = gkey;
   a.tok = gtok;
-  a.part = (float*)(scratch + 4 * ob);
+  a.part = (float*)(scratch + 4 * ob + order_bytes(1 + kMaxChunks));
   const long long units = (((long long)a.tokens + a.chunk - 1) / a.chunk) * slabs;
   a.sum_blocks = (int)((units + 3) / 4);
   hipLaunchKernelGGL(embedding_sum_kernel<T>, dim3((unsigned)(a.sum_blocks + fill)), dim3(256), 0, s, a,
                      (const T*)dy);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(embedding_join_kernel, dim3((unsigned)units), dim3(64 * kJoinWaves), 0, s, a);
+  hipLaunchKernelGGL(embedding_join_kernel, dim3(kJoinBlocks), dim3(64 * kJoinWaves), 0, s, a);
   return hipGetLastError();
 }
 
