@@ -396,31 +396,29 @@ def attention_bwd(qkv, o, lse, dout, dqkv, delta, batch, seq, heads, head_dim, s
 I32, I64 = 0, 1
 
 
-def _require(ok: bool, what: str, why: str) -> None:
-    if not ok:
-        raise ValueError(f"{what}: {why}")
-
-
 def _call(what: str, fn: str, args, stream, names: str, *tensors) -> None:
     """Call the entry point fn(*args, stream) after checking that the tensors (None: not given)
     are dense and on one GPU.  The call goes to that GPU: its current stream unless `stream`
-    names another one of its streams.  (The checks cost a few tenths of a microsecond a tensor:
-    of a short call's time the host's part is the larger.)"""
+    names another one of its streams.  (A short call's time is mostly the host's, so the checks
+    are kept to a tenth of a microsecond or two each.)"""
     import torch
     index = tensors[0].get_device()
     for t in tensors:
-        if t is not None and (t.get_device() != index or index < 0 or not t.is_contiguous()):
-            for name, u in zip(names.split(), tensors):
-                _require(u is None or u.is_contiguous(), what, f"{name} is not contiguous")
-            where = (f"{name}: {u.device}" for name, u in zip(names.split(), tensors) if u is not None)
-            raise ValueError(f"{what}: tensors are not on one GPU ({', '.join(where)})")
+        if t is not None and (t.get_device() != index or not t.is_contiguous()):
+            index = -1
+    if index < 0:
+        for name, t in zip(names.split(), tensors):
+            if t is not None and not t.is_contiguous():
+                raise ValueError(f"{what}: {name} is not contiguous")
+        where = ", ".join(f"{name}: {t.device}" for name, t in zip(names.split(), tensors) if t is not None)
+        raise ValueError(f"{what}: tensors are not on one GPU ({where})")
     if stream is None:
         handle = torch._C._cuda_getCurrentRawStream(index)  # a fifteenth of torch.cuda.current_stream's time
+    elif stream.device.index != index:
+        raise ValueError(f"{what}: the stream is on {stream.device}, the tensors on cuda:{index}")
     else:
-        if stream.device.index != index:
-            raise ValueError(f"{what}: the stream is on {stream.device}, the tensors on cuda:{index}")
         handle = stream.cuda_stream
-    entry = getattr(lib(), fn)
+    entry = getattr(_lib or lib(), fn)
     if torch.cuda.current_device() == index:
         status = entry(*args, handle)
     else:
@@ -442,6 +440,13 @@ def _element(what: str, *tensors) -> int:
     if dt is torch.float32:
         return FP32
     raise ValueError(f"{what}: element type {dt}: bf16 or fp32")
+
+
+def _count(what: str, ids) -> int:
+    n = ids.numel()
+    if n > 1 << 30:  # (as an argument of the entry point a larger one would wrap)
+        raise ValueError(f"{what}: {n} ids")
+    return n
 
 
 def _scratch(what: str, scratch, nbytes: int):
@@ -467,12 +472,14 @@ def embedding_fwd(ids, table, y, scale=1.0, first_id=0, stream=None) -> None:
     ids int32 or int64 of any shape, table [rows, hidden], y ids.shape + [hidden]."""
     what = "embedding_fwd"
     dt, it = _element(what, table, y), _id_type(what, ids)
-    _require(table.dim() == 2, what, "table is [rows, hidden]")
+    if table.dim() != 2:
+        raise ValueError(f"{what}: table is [rows, hidden]")
     rows, hidden = table.shape
-    _require(y.numel() == ids.numel() * hidden and y.shape[-1] == hidden, what, "y is one row for each id")
-    _call(what, "merak_embedding_fwd", (dt, it, ids.numel(), hidden, rows, first_id, scale, _ptr(ids), _ptr(table),
-          _ptr(y)),
-          stream, "ids table y", ids, table, y)
+    tokens = _count(what, ids)
+    if y.numel() != tokens * hidden or y.shape[-1] != hidden:
+        raise ValueError(f"{what}: y is one row for each id")
+    _call(what, "merak_embedding_fwd", (dt, it, tokens, hidden, rows, first_id, scale, ids.data_ptr(),
+                                        table.data_ptr(), y.data_ptr()), stream, "ids table y", ids, table, y)
 
 
 def embedding_scratch_bytes(tokens: int, hidden: int) -> int:
@@ -485,24 +492,31 @@ def embedding_bwd(ids, dy, dtable, scratch=None, scale=1.0, first_id=0, accumula
     import torch
     what = "embedding_bwd"
     dt, it = _element(what, dy), _id_type(what, ids)
-    _require(dtable.dim() == 2 and dtable.dtype == torch.float32, what, "dtable is fp32 [rows, hidden]")
+    if dtable.dim() != 2 or dtable.dtype is not torch.float32:
+        raise ValueError(f"{what}: dtable is fp32 [rows, hidden]")
     rows, hidden = dtable.shape
-    _require(dy.numel() == ids.numel() * hidden and dy.shape[-1] == hidden, what, "dy is one row for each id")
-    sp = _scratch(what, scratch, embedding_scratch_bytes(ids.numel(), hidden))
-    _call(what, "merak_embedding_bwd", (dt, it, ids.numel(), hidden, rows, first_id, scale, _ptr(ids), _ptr(dy),
-          _ptr(dtable), int(accumulate), sp),
-          stream, "ids dy dtable scratch", ids, dy, dtable, scratch)
+    tokens = _count(what, ids)
+    if dy.numel() != tokens * hidden or dy.shape[-1] != hidden:
+        raise ValueError(f"{what}: dy is one row for each id")
+    sp = _scratch(what, scratch, embedding_scratch_bytes(tokens, hidden))
+    _call(what, "merak_embedding_bwd", (dt, it, tokens, hidden, rows, first_id, scale, ids.data_ptr(), dy.data_ptr(),
+                                        dtable.data_ptr(), int(accumulate), sp), stream,
+          "ids dy dtable scratch", ids, dy, dtable, scratch)
 
 
 def rope_table(table, theta=10000.0, stream=None) -> None:
     """Fill table fp32 [positions, rope_dim / 2, 2] with the cosines and sines of
     position * theta^(-2 i / rope_dim)."""
+    positions, rope = _table("rope_table", table)
+    _call("rope_table", "merak_rope_table", (positions, rope, theta, table.data_ptr()), stream, "table", table)
+
+
+def _table(what: str, table):
+    """(positions, rotated features) of a rotation table."""
     import torch
-    what = "rope_table"
-    _require(table.dim() == 3 and table.shape[2] == 2 and table.dtype == torch.float32, what,
-             "table is fp32 [positions, rope_dim / 2, 2]")
-    _call(what, "merak_rope_table", (table.shape[0], 2 * table.shape[1], theta, _ptr(table)),
-          stream, "table", table)
+    if table.dim() != 3 or table.shape[2] != 2 or table.dtype is not torch.float32:
+        raise ValueError(f"{what}: table is fp32 [positions, rope_dim / 2, 2]")
+    return table.shape[0], 2 * table.shape[1]
 
 
 def _qk_args(what, qkv, q_gamma, k_gamma, table, positions, q_heads, kv_heads, seq_len, interleaved, eps):
@@ -510,22 +524,25 @@ def _qk_args(what, qkv, q_gamma, k_gamma, table, positions, q_heads, kv_heads, s
     import torch
     dt = _element(what, qkv, q_gamma, k_gamma)
     d = q_gamma.numel()
-    _require(k_gamma.numel() == d, what, "q_gamma and k_gamma hold one head's features")
-    row = (q_heads + 2 * kv_heads) * d
-    _require(q_heads > 0 and kv_heads > 0 and row > 0 and qkv.numel() % row == 0, what,
-             "qkv is [tokens, q_heads + 2 * kv_heads, head_dim]")
-    tokens, rope, rows = qkv.numel() // row, 0, 0
-    if table is not None:
-        _require(table.dim() == 3 and table.shape[2] == 2 and table.dtype == torch.float32, what,
-                 "table is fp32 [positions, rope_dim / 2, 2]")
-        rope, rows = 2 * table.shape[1], table.shape[0]
-        if positions is not None:
-            _require(positions.dtype == torch.int32 and positions.numel() == tokens, what,
-                     "positions is int32, one for each token")
-        else:
-            _require(seq_len is not None, what, "positions or seq_len needed")
+    if k_gamma.numel() != d:
+        raise ValueError(f"{what}: q_gamma and k_gamma hold one head's features")
+    row, n = (q_heads + 2 * kv_heads) * d, qkv.numel()
+    if q_heads <= 0 or kv_heads <= 0 or row <= 0 or n % row != 0:
+        raise ValueError(f"{what}: qkv is [tokens, q_heads + 2 * kv_heads, head_dim]")
+    tokens = n // row
+    if table is None:
+        return (dt, tokens, q_heads, kv_heads, d, 0, int(interleaved), eps), (None, 0, None, 0)
+    rows, rope = _table(what, table)
+    if positions is not None:
+        if positions.dtype is not torch.int32 or positions.numel() != tokens:
+            raise ValueError(f"{what}: positions is int32, one for each token")
+        place = positions.data_ptr()
+    else:
+        if seq_len is None:
+            raise ValueError(f"{what}: positions or seq_len needed")
+        place = None
     return ((dt, tokens, q_heads, kv_heads, d, rope, int(interleaved), eps),
-            (_ptr(table), rows, _ptr(positions), int(seq_len or 0)))
+            (table.data_ptr(), rows, place, seq_len or 0))
 
 
 def qk_norm_rope_fwd(qkv, q_gamma, k_gamma, table, out, q_heads, kv_heads, positions=None, seq_len=None,
@@ -535,10 +552,11 @@ def qk_norm_rope_fwd(qkv, q_gamma, k_gamma, table, out, q_heads, kv_heads, posit
     table the heads are only normalised; without positions token t is at t % seq_len."""
     what = "qk_norm_rope_fwd"
     head, tail = _qk_args(what, qkv, q_gamma, k_gamma, table, positions, q_heads, kv_heads, seq_len, interleaved, eps)
-    _element(what, qkv, out)
-    _require(out.numel() == qkv.numel(), what, "out has qkv's size")
-    _call(what, "merak_qk_norm_rope_fwd", (*head, _ptr(qkv), _ptr(q_gamma), _ptr(k_gamma), *tail, _ptr(out)),
-          stream, "qkv q_gamma k_gamma table positions out", qkv, q_gamma, k_gamma, table, positions, out)
+    if out.dtype is not qkv.dtype or out.numel() != qkv.numel():
+        raise ValueError(f"{what}: out has qkv's type and size")
+    _call(what, "merak_qk_norm_rope_fwd", (*head, qkv.data_ptr(), q_gamma.data_ptr(), k_gamma.data_ptr(), *tail,
+                                           out.data_ptr()), stream,
+          "qkv q_gamma k_gamma table positions out", qkv, q_gamma, k_gamma, table, positions, out)
 
 
 def qk_norm_rope_scratch_elems(tokens: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
@@ -553,28 +571,36 @@ def qk_norm_rope_bwd(dout, qkv, q_gamma, k_gamma, table, dqkv, dq_gamma, dk_gamm
     import torch
     what = "qk_norm_rope_bwd"
     head, tail = _qk_args(what, qkv, q_gamma, k_gamma, table, positions, q_heads, kv_heads, seq_len, interleaved, eps)
-    _element(what, qkv, dout, dqkv)
-    _require(dout.numel() == qkv.numel() and dqkv.numel() == qkv.numel(), what, "dout and dqkv have qkv's size")
+    n = qkv.numel()
+    if dout.dtype is not qkv.dtype or dqkv.dtype is not qkv.dtype or dout.numel() != n or dqkv.numel() != n:
+        raise ValueError(f"{what}: dout and dqkv have qkv's type and size")
     d = q_gamma.numel()
-    _require(all(g.dtype == torch.float32 and g.numel() == d for g in (dq_gamma, dk_gamma)), what,
-             "dq_gamma and dk_gamma are fp32 [head_dim]")
+    for g in (dq_gamma, dk_gamma):
+        if g.dtype is not torch.float32 or g.numel() != d:
+            raise ValueError(f"{what}: dq_gamma and dk_gamma are fp32 [head_dim]")
     sp = _scratch(what, scratch, 4 * qk_norm_rope_scratch_elems(head[1], q_heads, kv_heads, d))
-    _call(what, "merak_qk_norm_rope_bwd", (*head, _ptr(dout), _ptr(qkv), _ptr(q_gamma), _ptr(k_gamma), *tail,
-          _ptr(dqkv), _ptr(dq_gamma), _ptr(dk_gamma), int(accumulate), sp),
-          stream, "dout qkv q_gamma k_gamma table positions dqkv dq_gamma dk_gamma scratch",
+    _call(what, "merak_qk_norm_rope_bwd", (*head, dout.data_ptr(), qkv.data_ptr(), q_gamma.data_ptr(),
+                                           k_gamma.data_ptr(), *tail, dqkv.data_ptr(), dq_gamma.data_ptr(),
+                                           dk_gamma.data_ptr(), int(accumulate), sp), stream,
+          "dout qkv q_gamma k_gamma table positions dqkv dq_gamma dk_gamma scratch",
           dout, qkv, q_gamma, k_gamma, table, positions, dqkv, dq_gamma, dk_gamma, scratch)
 
 
 def _act8(what, q, scales):
     """(rows, cols) of a checkpoint."""
     import torch
-    _require(q.dtype == torch.uint8 and scales.dtype == torch.uint8, what, "q and scales are uint8")
-    _require(q.dim() >= 1 and q.shape[-1] > 0, what, "q is [rows, cols]")
-    cols = q.shape[-1]
-    _require(cols % 32 == 0, what, "cols is a multiple of 32")
-    _require(scales.numel() * 32 == q.numel() and scales.shape[-1] * 32 == cols, what,
-             "scales is [rows, cols / 32]")
-    return q.numel() // cols, cols
+    if q.dtype is not torch.uint8 or scales.dtype is not torch.uint8:
+        raise ValueError(f"{what}: q and scales are uint8")
+    cols, n = q.shape[-1], q.numel()
+    if cols <= 0 or cols % 32 or scales.shape[-1] * 32 != cols or scales.numel() * 32 != n:
+        raise ValueError(f"{what}: q is [rows, cols] and scales [rows, cols / 32], cols a multiple of 32")
+    return n // cols, cols
+
+
+def _like(what, q, names, *tensors) -> None:
+    for t in tensors:
+        if t.numel() != q.numel() or t.shape[-1] != q.shape[-1]:
+            raise ValueError(f"{what}: {names} q's shape")
 
 
 def act8_save(x, q, scales, stream=None) -> None:
@@ -582,9 +608,9 @@ def act8_save(x, q, scales, stream=None) -> None:
     what = "act8_save"
     dt = _element(what, x)
     rows, cols = _act8(what, q, scales)
-    _require(x.numel() == q.numel() and x.shape[-1] == cols, what, "x has q's shape")
-    _call(what, "merak_act8_save", (dt, rows, cols, _ptr(x), _ptr(q), _ptr(scales)),
-          stream, "x q scales", x, q, scales)
+    _like(what, q, "x has", x)
+    _call(what, "merak_act8_save", (dt, rows, cols, x.data_ptr(), q.data_ptr(), scales.data_ptr()), stream,
+          "x q scales", x, q, scales)
 
 
 def act8_restore(q, scales, x, stream=None) -> None:
@@ -592,21 +618,20 @@ def act8_restore(q, scales, x, stream=None) -> None:
     what = "act8_restore"
     dt = _element(what, x)
     rows, cols = _act8(what, q, scales)
-    _require(x.numel() == q.numel() and x.shape[-1] == cols, what, "x has q's shape")
-    _call(what, "merak_act8_restore", (dt, rows, cols, _ptr(q), _ptr(scales), _ptr(x)),
-          stream, "q scales x", q, scales, x)
+    _like(what, q, "x has", x)
+    _call(what, "merak_act8_restore", (dt, rows, cols, q.data_ptr(), scales.data_ptr(), x.data_ptr()), stream,
+          "q scales x", q, scales, x)
 
 
 def act8_gelu_bwd(dg, q, scales, du, g=None, stream=None) -> None:
     """du = dg * GeLU'(u) and, if given, g = GeLU(u), with u from its checkpoint; du may be dg."""
     what = "act8_gelu_bwd"
-    rest = (du,) if g is None else (du, g)
-    dt = _element(what, dg, *rest)
+    given = (dg, du) if g is None else (dg, du, g)
+    dt = _element(what, *given)
     rows, cols = _act8(what, q, scales)
-    _require(all(t.numel() == q.numel() and t.shape[-1] == cols for t in (dg, *rest)), what,
-             "dg, du and g have q's shape")
-    _call(what, "merak_act8_gelu_bwd", (dt, rows, cols, _ptr(dg), _ptr(q), _ptr(scales), _ptr(du), _ptr(g)),
-          stream, "dg q scales du g", dg, q, scales, du, g)
+    _like(what, q, "dg, du and g have", *given)
+    _call(what, "merak_act8_gelu_bwd", (dt, rows, cols, dg.data_ptr(), q.data_ptr(), scales.data_ptr(), du.data_ptr(),
+                                        _ptr(g)), stream, "dg q scales du g", dg, q, scales, du, g)
 
 
 def act8_gemm_dw_scratch_bytes(dtype, tokens: int, n_out: int, n_in: int) -> int:
@@ -623,10 +648,12 @@ def act8_gemm_dw(dy, q, scales, dw, scratch=None, accumulate=False, stream=None)
     what = "act8_gemm_dw"
     dt = _element(what, dy)
     tokens, n_in = _act8(what, q, scales)
-    _require(dw.dim() == 2 and dw.dtype == torch.float32 and dw.shape[1] == n_in, what, "dw is fp32 [n_out, n_in]")
+    if dw.dim() != 2 or dw.dtype is not torch.float32 or dw.shape[1] != n_in:
+        raise ValueError(f"{what}: dw is fp32 [n_out, n_in]")
     n_out = dw.shape[0]
-    _require(dy.numel() == tokens * n_out and dy.shape[-1] == n_out, what, "dy is [tokens, n_out]")
+    if dy.numel() != tokens * n_out or dy.shape[-1] != n_out:
+        raise ValueError(f"{what}: dy is [tokens, n_out]")
     sp = _scratch(what, scratch, act8_gemm_dw_scratch_bytes(dy.dtype, tokens, n_out, n_in))
-    _call(what, "merak_act8_gemm_dw", (dt, tokens, n_out, n_in, _ptr(dy), _ptr(q), _ptr(scales), _ptr(dw),
-          int(accumulate), sp),
-          stream, "dy q scales dw scratch", dy, q, scales, dw, scratch)
+    _call(what, "merak_act8_gemm_dw", (dt, tokens, n_out, n_in, dy.data_ptr(), q.data_ptr(), scales.data_ptr(),
+                                       dw.data_ptr(), int(accumulate), sp), stream,
+          "dy q scales dw scratch", dy, q, scales, dw, scratch)

@@ -229,6 +229,17 @@ __device__ __forceinline__ int lower_bound16(const int* key, int n, int r, int l
   return lo;
 }
 
+// 8 columns of a row of T from their 16-byte pieces.
+template <typename T>
+__device__ __forceinline__ void unpack_row(const u32x4_t (&v)[sizeof(T) / 2], float f[8]) {
+  if constexpr (sizeof(T) == 2) {
+    unpack8(v[0], f);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(v[e >> 2][e & 3]);
+  }
+}
+
 // 8 columns of a finished row.
 __device__ __forceinline__ void write_row(float* out, const float acc[8], float scale, int accumulate) {
   float v[8];
@@ -355,12 +366,7 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(EmbeddingSum a, cons
         }
         if (cur < 0) break;  // only tokens without a row from here on
         float f[8];
-        if constexpr (W == 1) {
-          unpack8(v[u][0], f);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(v[u][e >> 2][e & 3]);
-        }
+        unpack_row<T>(v[u], f);
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[e] += f[e];
       }
@@ -470,21 +476,29 @@ __global__ void __launch_bounds__(256) embedding_direct_kernel(EmbeddingSum a, l
   for (int g = 0; g < KG; ++g) {
     unsigned long long r = run[g];
     while (r) {
-      constexpr int U = 8;  // rows in flight
-      float v[U][8];
+      constexpr int U = sizeof(T) == 2 ? 16 : 8;  // rows in flight
+      constexpr int W = sizeof(T) / 2;            // 16-byte pieces of 8 columns
+      u32x4_t v[U][W];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[u][e] = 0.0f;
+        for (int e = 0; e < W; ++e) v[u][e] = u32x4_t{0u, 0u, 0u, 0u};
         if (r) {
-          if (live) load8(dy + (size_t)(64 * g + __builtin_ctzll(r)) * a.hidden + col, v[u]);
+          const T* p = dy + (size_t)(64 * g + __builtin_ctzll(r)) * a.hidden + col;
+          if (live) {
+#pragma unroll
+            for (int e = 0; e < W; ++e) v[u][e] = reinterpret_cast<const u32x4_t*>(p)[e];
+          }
           r &= r - 1;
         }
       }
 #pragma unroll
-      for (int u = 0; u < U; ++u)
+      for (int u = 0; u < U; ++u) {
+        float f[8];
+        unpack_row<T>(v[u], f);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] += v[u][e];
+        for (int e = 0; e < 8; ++e) acc[e] += f[e];
+      }
     }
   }
   if (live) write_row(a.out + (size_t)k * a.hidden + col, acc, a.scale, a.accumulate);
