@@ -161,6 +161,9 @@ __global__ void __launch_bounds__(256) act8_gelu_bwd_kernel(long long chunks, co
 // a time, and become bf16 on the way into LDS: eight conversions that take the scale
 // along for 16 values.  Converting there costs each value one conversion in a
 // workgroup; behind LDS every wave that shares a column would convert it again.
+// Even so the conversions and their LDS writes take a fifth of a large product's time,
+// so there (dw_plan) X is restored once into scratch instead and goes global -> LDS
+// directly too.
 //
 // A stage has four sub-steps; each reads the next one's fragments between its MFMAs.
 // Behind the barrier at the end of stage kt's reads its buffer is refilled with
@@ -176,8 +179,9 @@ struct DwArgs {
   int tiles;      // output tiles of a split
   int accumulate;
   const bf16_t* dy;
-  const uint8_t* q;
+  const uint8_t* q;       // X: codes and scales, or
   const uint8_t* scales;
+  const bf16_t* x;        // its values
   float* out;     // splits = 1: dw; else the splits' sums [splits][n_out][n_in]
 };
 
@@ -190,14 +194,16 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t stage_buffer(const void* p, in
   return operand_rsrc(p, rows > 0 ? (uint32_t)(min(rows, kBK) * ld) : 0u);
 }
 
-template <int BM, int BN, int WM, int WN>
+template <int BM, int BN, int WM, int WN, bool CODES>
 __global__ void __launch_bounds__(WM * WN * 64) act8_dw_kernel(DwArgs p) {
   constexpr int NW = WM * WN, NT = NW * 64;
   constexpr int WTM = BM / WM, WTN = BN / WN, TM = WTM / 32, TN = WTN / 32;
   constexpr int A_BYTES = BM * 128, STAGE = (BM + BN) * 128;
   constexpr int LA = BM / 8 / NW;         // dY loads of a wave and stage
-  constexpr int LB = BN * kBK / 16 / NT;  // runs of 16 codes of a thread and stage
+  // X: runs of 16 codes of a thread and stage, or loads of a wave
+  constexpr int LB = CODES ? BN * kBK / 16 / NT : BN / 8 / NW;
   constexpr int RPR = BN / 16, CPR = BN / 8;
+  static_assert(!CODES || (LB * NT * 16 == BN * kBK && CPR % 16 == 0), "whole runs, slots in pairs");
   extern __shared__ __align__(16) char smem[];
 
   const int lane = threadIdx.x & 63;
@@ -215,25 +221,29 @@ __global__ void __launch_bounds__(WM * WN * 64) act8_dw_kernel(DwArgs p) {
   const int k0 = split * p.per_split;
   const int rows = min(p.per_split, p.tokens - k0);
   const int KT = (rows + kBK - 1) / kBK;
-  const size_t lda = (size_t)p.n_out * 2, ldq = p.n_in, lds = p.n_in / kScaleBlock;
+  const size_t lda = (size_t)p.n_out * 2, ldx = (size_t)p.n_in * 2, ldq = p.n_in, lds = p.n_in / kScaleBlock;
   const char* pa = reinterpret_cast<const char*>(p.dy) + (size_t)k0 * lda;
+  const char* px = reinterpret_cast<const char*>(p.x) + (size_t)k0 * ldx;
   const uint8_t* pq = p.q + (size_t)k0 * ldq;
   const uint8_t* ps = p.scales + (size_t)k0 * lds;
 
   TileLoader<true, BM, NW> la;
+  TileLoader<true, BN, NW> lb;
   la.init(m0, p.n_out, wave, lane);
-  la.step = 0;  // the buffer's start moves instead
+  la.step = lb.step = 0;  // the buffers' starts move instead
+  if constexpr (!CODES) {
+    lb.init(n0, p.n_in, wave, lane);
+    lb.step = 0;
+  }
   uint32_t qoff[LB], soff[LB], w0[LB];
-  bool swap[LB];
+  if constexpr (CODES) {
 #pragma unroll
-  for (int u = 0; u < LB; ++u) {
-    const int i = threadIdx.x + NT * u, kr = i / RPR, run = i % RPR;
-    qoff[u] = (uint32_t)(kr * p.n_in + n0 + run * 16);
-    soff[u] = (uint32_t)(kr * (p.n_in / kScaleBlock) + (n0 + run * 16) / kScaleBlock);
-    // The run's two 16-byte chunks are neighbours in LDS; lanes 8 runs on write theirs in
-    // the other order, so that 16 lanes cover all 64 banks.
-    swap[u] = (run >> 3) & 1;
-    w0[u] = (uint32_t)(A_BYTES + kr * 2 * BN + ((run * 2 + 4 * (kr & 3)) % CPR) * 16);
+    for (int u = 0; u < LB; ++u) {
+      const int i = threadIdx.x + NT * u, kr = i / RPR, run = i % RPR;
+      qoff[u] = (uint32_t)(kr * p.n_in + n0 + run * 16);
+      soff[u] = (uint32_t)(kr * (p.n_in / kScaleBlock) + (n0 + run * 16) / kScaleBlock);
+      w0[u] = (uint32_t)(A_BYTES + kr * 2 * BN + ((run * 2 + 4 * (kr & 3)) % CPR) * 16);
+    }
   }
   FragReader<true, BM> fa;
   FragReader<true, BN> fb;
@@ -261,12 +271,11 @@ __global__ void __launch_bounds__(WM * WN * 64) act8_dw_kernel(DwArgs p) {
     c.q[u] = __builtin_amdgcn_raw_buffer_load_b128(rq, qoff[u], 0, 0);
     c.s[u] = __builtin_amdgcn_raw_buffer_load_b8(rc, soff[u], 0, 0);
   };
-  auto write_codes = [&](char* st, int u, int half) {  // chunk `half` (in this lane's order) of run u
-    const float sc = scale_of(now.s[u]);
-    const bool second = half ? !swap[u] : swap[u];
-    const u32x4_t v = decode8_bf16(second ? now.q[u][2] : now.q[u][0], second ? now.q[u][3] : now.q[u][1], sc);
-    *reinterpret_cast<u32x4_t*>(st + w0[u] + (second ? 16 : 0)) = v;
+  auto write_codes = [&](char* st, int u, int half) {  // half a run; its two chunks are neighbours in LDS
+    *reinterpret_cast<u32x4_t*>(st + w0[u] + 16 * half) =
+        decode8_bf16(now.q[u][2 * half], now.q[u][2 * half + 1], scale_of(now.s[u]));
   };
+  auto x_rsrc = [&](int kt) { return stage_rsrc(px + (size_t)kt * kBK * ldx, rows - kt * kBK, ldx); };
   auto dy_rsrc = [&](int kt) { return stage_rsrc(pa + (size_t)kt * kBK * lda, rows - kt * kBK, lda); };
   // A sub-step: the MFMAs of set c, each followed by the read of one fragment of (st, ks)
   // into set n and by piece(u), in that order.
@@ -291,20 +300,29 @@ __global__ void __launch_bounds__(WM * WN * 64) act8_dw_kernel(DwArgs p) {
   };
   auto nothing = [](int) {};
 
+  if constexpr (CODES) {
 #pragma unroll
-  for (int u = 0; u < LB; ++u) load_codes(now, 0, u);
-  la.issue(dy_rsrc(0), smem, wave);
+    for (int u = 0; u < LB; ++u) load_codes(now, 0, u);
+    la.issue(dy_rsrc(0), smem, wave);
 #pragma unroll
-  for (int u = 0; u < LB; ++u) {
-    write_codes(smem, u, 0);
-    write_codes(smem, u, 1);
+    for (int u = 0; u < LB; ++u) {
+      write_codes(smem, u, 0);
+      write_codes(smem, u, 1);
+    }
+#pragma unroll
+    for (int u = 0; u < LB; ++u) load_codes(next, 1, u);
+  } else {
+    la.issue(dy_rsrc(0), smem, wave);
+    lb.issue(x_rsrc(0), smem + A_BYTES, wave);
   }
-#pragma unroll
-  for (int u = 0; u < LB; ++u) load_codes(next, 1, u);
   wait_vm_barrier<0>();
-  now = next;
+  if constexpr (CODES) {
+    now = next;
 #pragma unroll
-  for (int u = 0; u < LB; ++u) load_codes(next, 2, u);
+    for (int u = 0; u < LB; ++u) load_codes(next, 2, u);
+  } else {
+    lb.issue(x_rsrc(1), smem + STAGE + A_BYTES, wave);
+  }
   la.issue(dy_rsrc(1), smem + STAGE, wave);
 #pragma unroll
   for (int j = 0; j < TN; ++j) b0[j] = fb.read(smem + A_BYTES, wn * WTN + j * 32, 0);
@@ -313,28 +331,34 @@ __global__ void __launch_bounds__(WM * WN * 64) act8_dw_kernel(DwArgs p) {
   __builtin_amdgcn_sched_barrier(0);
 
   // Past the last stage the loads find empty buffers: they fetch nothing and write zeros.
-  constexpr int CONV = 2 * LB;  // chunks to convert, half of them in each of two sub-steps
+  constexpr int CONV = 2 * LB;  // half runs to convert, half of them in each of two sub-steps
   for (int kt = 0; kt < KT; ++kt) {
     char* st = smem + (kt & 1) * STAGE;
     char* other = smem + ((kt + 1) & 1) * STAGE;
     auto convert = [&](int first, int u) {
-      constexpr int EVERY = NMF / (CONV / 2);
-      static_assert(NMF % (CONV / 2) == 0, "conversions spread evenly over the MFMAs");
-      if (u % EVERY == 0) write_codes(other, (first + u / EVERY) / 2, (first + u / EVERY) % 2);
+      if constexpr (CODES) {
+        constexpr int EVERY = NMF / (CONV / 2);
+        static_assert(NMF % (CONV / 2) == 0, "conversions spread evenly over the MFMAs");
+        if (u % EVERY == 0) write_codes(other, (first + u / EVERY) / 2, (first + u / EVERY) % 2);
+      }
     };
     step(st, 1, a1, b1, a0, b0, [&](int u) { convert(0, u); });
     step(st, 2, a0, b0, a1, b1, [&](int u) { convert(CONV / 2, u); });
     step(st, 3, a1, b1, a0, b0, nothing);
     wait_vm_barrier<0>();  // stage kt + 1 is in LDS, `next` is there, and all have read stage kt
-    now = next;
-    const i32x4_t ra = dy_rsrc(kt + 2);
+    if constexpr (CODES) now = next;
+    const i32x4_t ra = dy_rsrc(kt + 2), rx = x_rsrc(CODES ? 0 : kt + 2);
     constexpr int NP = LA + LB, PER = (NP + NMF - 1) / NMF;
     step(other, 0, a0, b0, a1, b1, [&](int u) {
 #pragma unroll
       for (int e = 0; e < PER; ++e) {
         const int c = u * PER + e;
-        if (c < LA) la.issue_one(ra, st, wave, c);
-        else if (c < NP) load_codes(next, kt + 3, c - LA);
+        if (c < LA) {
+          la.issue_one(ra, st, wave, c);
+        } else if (c < NP) {
+          if constexpr (CODES) load_codes(next, kt + 3, c - LA);
+          else lb.issue_one(rx, st + A_BYTES, wave, c - LA);
+        }
       }
     });
   }
@@ -376,17 +400,37 @@ __global__ void __launch_bounds__(WM * WN * 64) act8_dw_kernel(DwArgs p) {
   }
 }
 
-// dw (=|+=) the splits' sums, in split order.
+// dw (=|+=) the splits' sums.  SLICES threads of a workgroup share a chunk of four columns:
+// each adds a part of the splits in order, and the parts are added in order.
+template <int SLICES>
 __global__ void __launch_bounds__(256) act8_dw_join_kernel(long long chunks, int splits, const float* __restrict__ part,
                                                            float* __restrict__ dw, int accumulate) {
-  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-  if (i >= chunks) return;
+  constexpr int CPB = 256 / SLICES;
+  __shared__ f32x4_t red[SLICES > 1 ? 256 : 1];
+  const int c = threadIdx.x % CPB, sl = threadIdx.x / CPB;
+  const long long i = (long long)blockIdx.x * CPB + c;
+  const bool live = i < chunks;
+  const int per = (splits + SLICES - 1) / SLICES, end = min(splits, (sl + 1) * per);
   f32x4_t s = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int k = 0; k < splits; ++k) {
-    const f32x4_t v = reinterpret_cast<const f32x4_t*>(part)[k * chunks + i];
+  if (live) {
+#pragma unroll 8
+    for (int k = sl * per; k < end; ++k) {
+      const f32x4_t v = reinterpret_cast<const f32x4_t*>(part)[k * chunks + i];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) s[e] += v[e];
+      for (int e = 0; e < 4; ++e) s[e] += v[e];
+    }
   }
+  if constexpr (SLICES > 1) {
+    red[threadIdx.x] = s;
+    __syncthreads();
+    if (sl > 0) return;
+    for (int k = 1; k < SLICES; ++k) {
+      const f32x4_t v = red[k * CPB + c];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] += v[e];
+    }
+  }
+  if (!live) return;
   f32x4_t* o = reinterpret_cast<f32x4_t*>(dw) + i;
   if (accumulate) {
     const f32x4_t v = *o;
@@ -396,50 +440,70 @@ __global__ void __launch_bounds__(256) act8_dw_join_kernel(long long chunks, int
   *o = s;
 }
 
+// Many splits (16 and more, of small outputs) share a chunk among eight threads: 128 splits
+// of 64 x 64, added by one thread each, took 40 us.
+static hipError_t launch_dw_join(long long elems, int splits, const float* part, float* dw, int accumulate,
+                                 hipStream_t s) {
+  const long long chunks = elems / 4;
+  if (splits >= 16)
+    hipLaunchKernelGGL(act8_dw_join_kernel<8>, dim3((unsigned)((chunks + 31) / 32)), dim3(256), 0, s, chunks, splits,
+                       part, dw, accumulate);
+  else
+    hipLaunchKernelGGL(act8_dw_join_kernel<1>, dim3((unsigned)((chunks + 255) / 256)), dim3(256), 0, s, chunks, splits,
+                       part, dw, accumulate);
+  return hipGetLastError();
+}
+
 // fp32 check mode, on the fp32 matrix instruction (32 x 32 x 2): 64 x 64 tiles, four
-// waves of 32 x 32, 32 tokens a stage.
-__global__ void __launch_bounds__(256) act8_dw_f32_kernel(int tokens, int n_out, int n_in, const float* __restrict__ dy,
-                                                          const uint8_t* __restrict__ q,
-                                                          const uint8_t* __restrict__ scales, float* __restrict__ dw,
-                                                          int accumulate) {
-  constexpr int R = 64, KB = 32;
+// waves of 32 x 32, 32 tokens a stage, the next stage's operands on their way to
+// registers meanwhile.
+constexpr int kDwTileF32 = 64, kStageF32 = 32;
+
+__global__ void __launch_bounds__(256) act8_dw_f32_kernel(DwArgs p, const float* __restrict__ dy) {
+  constexpr int R = kDwTileF32, KB = kStageF32;
   __shared__ __align__(16) float sa[KB][R];
   __shared__ __align__(16) float sb[KB][R];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, hf = lane >> 5;
   const int wm = wave >> 1, wn = wave & 1;
-  const int tiles_n = (n_in + R - 1) / R;
-  const int m0 = (blockIdx.x / tiles_n) * R, n0 = (blockIdx.x % tiles_n) * R;
+  const int split = blockIdx.x / p.tiles, tile = blockIdx.x - split * p.tiles;
+  const int tiles_n = (p.n_in + R - 1) / R;
+  const int m0 = (tile / tiles_n) * R, n0 = (tile % tiles_n) * R;
+  const int first = split * p.per_split, end = min(p.tokens, first + p.per_split);
+  const int kr = threadIdx.x >> 3, c8 = (threadIdx.x & 7) * 8;
   f32x16_t acc;
 #pragma unroll
   for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
-  for (int k0 = 0; k0 < tokens; k0 += KB) {
-    __syncthreads();
-    const int kr = threadIdx.x >> 3, c8 = (threadIdx.x & 7) * 8;
-    const int t = k0 + kr;
-    float a[8], b[8];
+  float a[8], b[8];
+  auto fetch = [&](int t) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) a[e] = b[e] = 0.0f;
-    if (t < tokens && m0 + c8 < n_out) load8(dy + (size_t)t * n_out + m0 + c8, a);
-    if (t < tokens && n0 + c8 < n_in) {
-      const u32x2_t c = *reinterpret_cast<const u32x2_t*>(q + (size_t)t * n_in + n0 + c8);
-      const float s = scale_of(scales[(size_t)t * (n_in / kScaleBlock) + (n0 + c8) / kScaleBlock]);
+    if (t < end && m0 + c8 < p.n_out) load8(dy + (size_t)t * p.n_out + m0 + c8, a);
+    if (t < end && n0 + c8 < p.n_in) {
+      const u32x2_t c = *reinterpret_cast<const u32x2_t*>(p.q + (size_t)t * p.n_in + n0 + c8);
+      const float s = scale_of(p.scales[(size_t)t * (p.n_in / kScaleBlock) + (n0 + c8) / kScaleBlock]);
       decode4(c[0], s, b);
       decode4(c[1], s, b + 4);
     }
+  };
+  fetch(first + kr);
+  for (int k0 = first; k0 < end; k0 += KB) {
+    __syncthreads();  // the stage before has been read
     store8(&sa[kr][c8], a);
     store8(&sb[kr][c8], b);
     __syncthreads();
+    fetch(k0 + KB + kr);
 #pragma unroll
     for (int k = 0; k < KB; k += 2)
       acc = __builtin_amdgcn_mfma_f32_32x32x2f32(sa[k + hf][wm * 32 + l32], sb[k + hf][wn * 32 + l32], acc, 0, 0, 0);
   }
   // acc[r]: output (r / 4) * 8 + 4 * hf + r % 4, input l32
+  float* dw = p.out + (size_t)split * p.n_out * p.n_in;
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
     const int m = m0 + wm * 32 + (r >> 2) * 8 + hf * 4 + (r & 3), n = n0 + wn * 32 + l32;
-    if (m >= n_out || n >= n_in) continue;
-    float* out = dw + (size_t)m * n_in + n;
-    *out = accumulate ? *out + acc[r] : acc[r];
+    if (m >= p.n_out || n >= p.n_in) continue;
+    float* out = dw + (size_t)m * p.n_in + n;
+    *out = p.accumulate ? *out + acc[r] : acc[r];
   }
 }
 
@@ -491,37 +555,95 @@ hipError_t launch_act8_gelu_bwd(int dtype, int rows, int cols, const void* dg, c
   return hipGetLastError();
 }
 
-// Tile and split of the bf16 weight gradient.
+// How the bf16 weight gradient is cut up: tiles of bm x bn, token splits, and whether X is
+// restored to bf16 first.
 struct DwPlan {
-  bool large;  // 256 x 256 tiles, else 128 x 128
-  int tiles, splits, per_split;
+  int bm, bn, tiles, splits, per_split;
+  bool restore;
 };
 
+// Restoring X reads and writes it once more (3 bytes a value, and a launch); it saves
+// every one of the n_out / bm tiles in its column the conversion, about 6e-10 us a
+// product.  Measured, restored and converted: 16384 x 7680 x 1920 (tokens x outputs x
+// inputs) 429 and 540 us, 2048 x 4096 x 1024 33 and 35; 2048 x 1024 x 1024 25 and 22,
+// 333 x 1920 x 640 11 and 9.
+static bool dw_restore(double tokens, double n_out, double n_in) {
+  return 6e-10 * tokens * n_out * n_in > 2.5 + 6.7e-7 * tokens * n_in;
+}
+
+// Tile and splits by estimated time: whole rounds of workgroups over the chip, each as
+// long as its stages (and about four more for its start and end); splits add their
+// sums' way through memory and a launch.  us a stage, measured: 256 x 256 1.6, 256 x 192
+// 1.16 (one workgroup a CU); 128 x 128 0.65 alone on its CU, 0.92 for two; converting adds a
+// seventh.  What it decides, with the other choice's time: 8192 x 6400 x 1600 256 x 192
+// 161 us, 256 x 256 170, 128 x 128 201; 16384 x 7680 x 1920 256 x 256 429, 128 x 128 499;
+// 4096 x 2048 x 2048 128 x 128 in two splits 53, in one 58.
 static DwPlan dw_plan(int tokens, int n_out, int n_in) {
-  auto tiles = [&](int t) { return (long long)((n_out + t - 1) / t) * ((n_in + t - 1) / t); };
-  DwPlan p;
-  p.large = tiles(256) >= 160;
-  p.tiles = (int)tiles(p.large ? 256 : 128);
+  struct Tile {
+    int bm, bn, resident;
+    double alone, full;
+  };
+  static const Tile tiles[] = {{128, 128, 2, 0.65, 0.92}, {256, 256, 1, 1.6, 1.6}, {256, 192, 1, 1.16, 1.16}};
+  DwPlan best{};
+  best.restore = dw_restore(tokens, n_out, n_in);
   const int stages = (tokens + kBK - 1) / kBK;
-  int splits = 1;
-  if (!p.large) splits = (int)std::min<long long>(std::max<long long>(512 / p.tiles, 1), (stages + 7) / 8);
-  const int per = (stages + splits - 1) / splits;
+  double least = 0.0;
+  for (const Tile& t : tiles) {
+    if (t.bm != 128 && !best.restore) continue;  // converting, only 128 x 128 is ever the fastest
+    const long long n = (long long)((n_out + t.bm - 1) / t.bm) * ((n_in + t.bn - 1) / t.bn);
+    for (int want = 1; want == 1 || (want <= 512 && want <= stages / 2 && want * n <= 1024);
+         want = want < 4 ? want + 1 : want * 4 / 3) {
+      const int per = (stages + want - 1) / want, splits = (stages + per - 1) / per;
+      const long long wg = n * splits, slots = 256LL * t.resident;
+      const double us = (double)((wg + slots - 1) / slots) * (per + 4) * (wg <= 256 ? t.alone : t.full) *
+                            (best.restore ? 1.0 : 8.0 / 7.0) +
+                        (splits > 1 ? 5.0 + splits * (double)n_out * n_in * 8.0 / 7e6 : 0.0);
+      if (best.bm == 0 || us < least) {
+        least = us;
+        best.bm = t.bm;
+        best.bn = t.bn;
+        best.tiles = (int)n;
+        best.splits = splits;
+        best.per_split = per * kBK;
+      }
+    }
+  }
+  return best;
+}
+
+// fp32: 64 x 64 tiles, and splits of at least eight stages where the tiles alone would leave
+// CUs without work (32768 x 512 x 512: 1.1 ms in one split).
+static DwPlan dw_plan_f32(int tokens, int n_out, int n_in) {
+  DwPlan p{};
+  p.bm = p.bn = kDwTileF32;
+  p.tiles = (int)((n_out + kDwTileF32 - 1LL) / kDwTileF32 * ((n_in + kDwTileF32 - 1LL) / kDwTileF32));
+  const int stages = (tokens + kStageF32 - 1) / kStageF32;
+  const int want = std::max(1, std::min(1024 / p.tiles, stages / 8));
+  const int per = (stages + want - 1) / want;
   p.splits = (stages + per - 1) / per;
-  p.per_split = per * kBK;
+  p.per_split = per * kStageF32;
   return p;
 }
 
-size_t act8_gemm_dw_scratch_bytes(int dtype, int tokens, int n_out, int n_in) {
-  if (dtype != DT_BF16) return 0;
-  const DwPlan p = dw_plan(tokens, n_out, n_in);
-  return p.splits > 1 ? (size_t)p.splits * n_out * n_in * sizeof(float) : 0;
+static DwPlan dw_plan_of(int dtype, int tokens, int n_out, int n_in) {
+  return dtype == DT_BF16 ? dw_plan(tokens, n_out, n_in) : dw_plan_f32(tokens, n_out, n_in);
 }
 
-template <int BM, int BN, int WM, int WN>
+// Scratch: X's values (if they are restored), the splits' sums (if there are several).
+static size_t dw_values_bytes(const DwPlan& p, int tokens, int n_in) {
+  return p.restore ? ((size_t)tokens * n_in * 2 + 255) / 256 * 256 : 0;
+}
+
+size_t act8_gemm_dw_scratch_bytes(int dtype, int tokens, int n_out, int n_in) {
+  const DwPlan p = dw_plan_of(dtype, tokens, n_out, n_in);
+  return dw_values_bytes(p, tokens, n_in) + (p.splits > 1 ? (size_t)p.splits * n_out * n_in * sizeof(float) : 0);
+}
+
+template <int BM, int BN, int WM, int WN, bool CODES>
 static hipError_t run_dw(const DwArgs& a, int splits, hipStream_t s) {
   constexpr size_t lds = 2 * (BM + BN) * 128;
   static_assert(lds <= 160 * 1024, "LDS budget");
-  auto kern = act8_dw_kernel<BM, BN, WM, WN>;
+  auto kern = act8_dw_kernel<BM, BN, WM, WN, CODES>;
   static std::atomic<uint64_t> lds_set{0};
   const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(kern), lds, lds_set);
   if (e != hipSuccess) return e;
@@ -531,25 +653,36 @@ static hipError_t run_dw(const DwArgs& a, int splits, hipStream_t s) {
   return hipGetLastError();
 }
 
+static hipError_t run_dw_plan(const DwPlan& p, const DwArgs& a, hipStream_t s) {
+  if (!p.restore) return run_dw<128, 128, 2, 2, true>(a, p.splits, s);
+  if (p.bm == 128) return run_dw<128, 128, 2, 2, false>(a, p.splits, s);
+  if (p.bn == 192) return run_dw<256, 192, 4, 2, false>(a, p.splits, s);
+  return run_dw<256, 256, 2, 4, false>(a, p.splits, s);
+}
+
 hipError_t launch_act8_gemm_dw(int dtype, int tokens, int n_out, int n_in, const void* dy, const uint8_t* q,
                                const uint8_t* scales, float* dw, int accumulate, void* scratch, hipStream_t s) {
-  if (dtype == DT_BF16) {
-    const DwPlan p = dw_plan(tokens, n_out, n_in);
-    const bool split = p.splits > 1;
-    const DwArgs a{tokens, n_out, n_in, p.per_split, p.tiles, split ? 0 : accumulate, (const bf16_t*)dy, q, scales,
-                   split ? (float*)scratch : dw};
-    hipError_t e = p.large ? run_dw<256, 256, 2, 4>(a, p.splits, s) : run_dw<128, 128, 2, 2>(a, p.splits, s);
-    if (e != hipSuccess || !split) return e;
-    const long long chunks = (long long)n_out * n_in / 4;
-    hipLaunchKernelGGL(act8_dw_join_kernel, dim3((unsigned)((chunks + 255) / 256)), dim3(256), 0, s, chunks, p.splits,
-                       (const float*)scratch, dw, accumulate);
-    return hipGetLastError();
+  const DwPlan p = dw_plan_of(dtype, tokens, n_out, n_in);
+  const bool split = p.splits > 1;
+  bf16_t* values = (bf16_t*)scratch;
+  float* sums = (float*)((char*)scratch + dw_values_bytes(p, tokens, n_in));
+  if (p.restore) {
+    const hipError_t e = launch_act8_restore(dtype, tokens, n_in, q, scales, values, s);
+    if (e != hipSuccess) return e;
   }
-  const long long wg = ((n_out + 63LL) / 64) * ((n_in + 63LL) / 64);
-  if (wg > 0x7fffffffLL) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(act8_dw_f32_kernel, dim3((unsigned)wg), dim3(256), 0, s, tokens, n_out, n_in, (const float*)dy, q,
-                     scales, dw, accumulate);
-  return hipGetLastError();
+  const DwArgs a{tokens, n_out, n_in, p.per_split, p.tiles, split ? 0 : accumulate, (const bf16_t*)dy, q, scales,
+                 values, split ? sums : dw};
+  hipError_t e;
+  if (dtype == DT_BF16) {
+    e = run_dw_plan(p, a, s);
+  } else {
+    const long long wg = (long long)p.tiles * p.splits;
+    if (wg > 0x7fffffffLL) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(act8_dw_f32_kernel, dim3((unsigned)wg), dim3(256), 0, s, a, (const float*)dy);
+    e = hipGetLastError();
+  }
+  if (e != hipSuccess || !split) return e;
+  return launch_dw_join((long long)n_out * n_in, p.splits, sums, dw, accumulate, s);
 }
 
 }  // namespace merak
