@@ -489,9 +489,9 @@ int merak_embedding_fwd(int dtype, int id_type, int tokens, int hidden, int tabl
 /* Its gradient: dtable[v, :] (= or +=) scale * sum over the tokens t with ids[t] -
  * first_id = v of dy[t, :], fp32, in one fixed order (tokens sorted by row).
  * accumulate = 0 writes every row, zeros where no token names it; accumulate = 1
- * leaves those rows untouched.  Ids outside the table add nothing.  scratch:
- * merak_embedding_scratch_bytes(tokens, hidden) bytes (may be NULL when that is
- * 0). */
+ * leaves those rows untouched.  Ids outside the table add nothing.  At most 2^22
+ * tokens.  scratch: merak_embedding_scratch_bytes(tokens, hidden) bytes (may be
+ * NULL when that is 0). */
 size_t merak_embedding_scratch_bytes(int tokens, int hidden);
 int merak_embedding_bwd(int dtype, int id_type, int tokens, int hidden, int table_rows, int64_t first_id,
                         float scale, const void* ids, const void* dy, float* dtable, int accumulate,

@@ -88,6 +88,12 @@ __device__ __forceinline__ void store8(float* p, const float v[8]) {
   reinterpret_cast<f32x4_t*>(p)[1] = f32x4_t{v[4], v[5], v[6], v[7]};
 }
 
+// 16 bytes, past the caches if `past` (uniform).
+__device__ __forceinline__ void store16(void* p, u32x4_t v, bool past) {
+  if (past) __builtin_nontemporal_store(v, reinterpret_cast<u32x4_t*>(p));
+  else *reinterpret_cast<u32x4_t*>(p) = v;
+}
+
 // Wave64 reductions (butterfly over all 64 lanes; every lane gets the result).
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll

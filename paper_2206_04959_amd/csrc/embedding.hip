@@ -36,7 +36,7 @@ constexpr int kFwdUnroll = 4;
 
 template <typename T, typename I>
 __global__ void __launch_bounds__(256) embedding_fwd_kernel(int tokens, int hidden, int rows, long long first,
-                                                            float scale, const I* __restrict__ ids,
+                                                            float scale, bool past, const I* __restrict__ ids,
                                                             const T* __restrict__ table, T* __restrict__ y) {
   constexpr int EPC = 16 / sizeof(T);  // elements per chunk
   const unsigned cpr = hidden / EPC;
@@ -61,17 +61,17 @@ __global__ void __launch_bounds__(256) embedding_fwd_kernel(int tokens, int hidd
 #pragma unroll
   for (int u = 0; u < kFwdUnroll; ++u) {
     if (!live[u]) continue;
+    u32x4_t o;
     if constexpr (sizeof(T) == 2) {
       float f[8];
       unpack8(v[u], f);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] *= scale;
-      store8(y + at[u], f);
+      for (int e = 0; e < 4; ++e) o[e] = pack_bf16x2(f[2 * e] * scale, f[2 * e + 1] * scale);
     } else {
-      const f32x4_t f = __builtin_bit_cast(f32x4_t, v[u]);
-      const float o[4] = {f[0] * scale, f[1] * scale, f[2] * scale, f[3] * scale};
-      store4(y + at[u], o);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = __float_as_uint(__uint_as_float(v[u][e]) * scale);
     }
+    store16(y + at[u], o, past);
   }
 }
 
@@ -254,8 +254,8 @@ __device__ __forceinline__ void write_row(float* out, const float acc[8], float 
   store8(out, v);
 }
 
-__device__ __forceinline__ void clear_row(float* row, int hidden, int lane) {
-  for (int c = lane * 4; c < hidden; c += 256) *reinterpret_cast<f32x4_t*>(row + c) = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+__device__ __forceinline__ void clear_row(float* row, int hidden, int lane, bool past) {
+  for (int c = lane * 4; c < hidden; c += 256) store16(row + c, u32x4_t{0u, 0u, 0u, 0u}, past);
 }
 
 struct EmbeddingSum {
@@ -267,6 +267,7 @@ struct EmbeddingSum {
   int* split;       // split[0]: how many runs are split, then the chunks in which they begin
   float* out;       // [rows][hidden]
   int sum_blocks;   // workgroups that sum; the rest clear rows
+  bool past;        // clear them past the caches
 };
 
 // Tokens of the run across the border at sorted position p > 0, counted to both sides of
@@ -307,7 +308,7 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(EmbeddingSum a, cons
     if ((lane & 15) == 0) used[threadIdx.x >> 4] = p < a.tokens && a.key[p] == r;
     __syncthreads();
     for (int i = w; i < kFillRows && r0 + i < a.rows; i += 4)
-      if (!used[i]) clear_row(a.out + (size_t)(r0 + i) * a.hidden, a.hidden, lane);
+      if (!used[i]) clear_row(a.out + (size_t)(r0 + i) * a.hidden, a.hidden, lane, a.past);
     return;
   }
   const int slabs = (a.hidden + kSlab - 1) / kSlab;
@@ -447,7 +448,7 @@ __global__ void __launch_bounds__(256) embedding_direct_kernel(EmbeddingSum a, l
       bool used = false;
 #pragma unroll
       for (int g = 0; g < KG; ++g) used |= key[g] == r0 + i;
-      if (__ballot(used) == 0ull) clear_row(a.out + (size_t)(r0 + i) * a.hidden, a.hidden, lane);
+      if (__ballot(used) == 0ull) clear_row(a.out + (size_t)(r0 + i) * a.hidden, a.hidden, lane, a.past);
     }
     return;
   }
@@ -514,7 +515,8 @@ static hipError_t fwd_t(int tokens, int hidden, int rows, long long first, float
   const long long wg = (chunks + 256 * kFwdUnroll - 1) / (256 * kFwdUnroll);
   if (wg > 0x7fffffffLL) return hipErrorInvalidValue;
   hipLaunchKernelGGL((embedding_fwd_kernel<T, I>), dim3((unsigned)wg), dim3(256), 0, s, tokens, hidden, rows, first,
-                     scale, (const I*)ids, (const T*)table, (T*)y);
+                     scale, (size_t)tokens * hidden * sizeof(T) >= kStreamBytes, (const I*)ids, (const T*)table,
+                     (T*)y);
   return hipGetLastError();
 }
 
@@ -597,6 +599,7 @@ hipError_t launch_embedding_bwd(int dtype, int id_type, int tokens, int hidden, 
   a.accumulate = accumulate;
   a.scale = scale;
   a.out = dtable;
+  a.past = (size_t)rows * hidden * sizeof(float) >= kStreamBytes;
   char* sc = (char*)scratch;
   if (dtype == DT_BF16)
     return id_type == ID_I32 ? bwd_t<bf16_t, int>(a, first, ids, dy, sc, s)

@@ -35,6 +35,7 @@ int check_apart(std::initializer_list<Span> written, std::initializer_list<Span>
 
 size_t elem(int dtype) { return dtype == MERAK_BF16 ? 2 : 4; }
 
+constexpr int kMaxSorted = 1 << 22;  // tokens of one embedding gradient: sorting compares every pair of 2048-token blocks
 constexpr int kMaxRows = 1 << 30;  // tokens and table rows: the kernels count them in 32 bits
 
 size_t id_bytes(int id_type) { return id_type == MERAK_I32 ? 4 : 8; }
@@ -103,9 +104,10 @@ size_t merak_embedding_scratch_bytes(int tokens, int hidden) {
 int merak_embedding_bwd(int dtype, int id_type, int tokens, int hidden, int table_rows, int64_t first_id, float scale,
                         const void* ids, const void* dy, float* dtable, int accumulate, void* scratch, void* stream) {
   TRY(check_embedding(dtype, id_type, tokens, hidden, table_rows, first_id, scale));
+  if (tokens > kMaxSorted) return MERAK_ERR_SHAPE;
   TRY(check_flag(accumulate));
   TRY(check_ptr(ids)); TRY(check_ptr(dy)); TRY(check_ptr(dtable));
-  const size_t sb = embedding_scratch_bytes(tokens, hidden);
+  const size_t sb = merak_embedding_scratch_bytes(tokens, hidden);
   if (sb > 0) TRY(check_ptr(scratch));
   TRY(check_apart({{dtable, (size_t)table_rows * hidden * 4}, {scratch, sb}},
                   {{ids, tokens * id_bytes(id_type)}, {dy, (size_t)tokens * hidden * elem(dtype)}}));

@@ -72,6 +72,7 @@ NAN, INF = float("nan"), float("inf")
     (_embed_fwd, dict(table=None), INVALID), (_embed_fwd, dict(y=P[2] + 2), ALIGN),
     (_embed_fwd, dict(y=P[1]), INVALID), (_embed_fwd, dict(y=P[1] + 100 * 128 - 16), INVALID),
     (_embed_bwd, dict(accumulate=2), INVALID), (_embed_bwd, dict(scratch=None), INVALID),
+    (_embed_bwd, dict(tokens=2 ** 22 + 1), SHAPE),
     (_embed_bwd, dict(scratch=P[3] + 8), ALIGN), (_embed_bwd, dict(dtable=P[1]), INVALID),
     (_embed_bwd, dict(scratch=P[2] + 16), INVALID),
     *[(f, c, s) for f in (_qk_fwd, _qk_bwd) for c, s in (
