@@ -8,6 +8,7 @@ If the library is missing the calls raise: there is no fallback path.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Dict, List, Optional, Sequence
 
@@ -482,6 +483,7 @@ def embedding_fwd(ids, table, y, scale=1.0, first_id=0, stream=None) -> None:
                                         table.data_ptr(), y.data_ptr()), stream, "ids table y", ids, table, y)
 
 
+@functools.lru_cache(maxsize=256)
 def embedding_scratch_bytes(tokens: int, hidden: int) -> int:
     return int(lib().merak_embedding_scratch_bytes(tokens, hidden))
 
@@ -559,6 +561,7 @@ def qk_norm_rope_fwd(qkv, q_gamma, k_gamma, table, out, q_heads, kv_heads, posit
           "qkv q_gamma k_gamma table positions out", qkv, q_gamma, k_gamma, table, positions, out)
 
 
+@functools.lru_cache(maxsize=256)
 def qk_norm_rope_scratch_elems(tokens: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
     return int(lib().merak_qk_norm_rope_scratch_elems(tokens, q_heads, kv_heads, head_dim))
 
@@ -634,6 +637,7 @@ def act8_gelu_bwd(dg, q, scales, du, g=None, stream=None) -> None:
                                         _ptr(g)), stream, "dg q scales du g", dg, q, scales, du, g)
 
 
+@functools.lru_cache(maxsize=256)
 def act8_gemm_dw_scratch_bytes(dtype, tokens: int, n_out: int, n_in: int) -> int:
     """dtype: the torch type of dy."""
     import torch

@@ -96,22 +96,22 @@ __global__ void __launch_bounds__(256) act8_save_kernel(long long chunks, const 
   if ((i & 3) == 0) scales[i >> 2] = (uint8_t)b;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256) act8_restore_kernel(long long chunks, bool past, const uint8_t* __restrict__ q,
+template <typename T, bool PAST>
+__global__ void __launch_bounds__(256) act8_restore_kernel(long long chunks, const uint8_t* __restrict__ q,
                                                            const uint8_t* __restrict__ scales, T* __restrict__ x) {
   const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
   if (i >= chunks) return;
   const u32x2_t c = *reinterpret_cast<const u32x2_t*>(q + i * 8);
   const float s = scale_of(scales[i >> 2]);
   if constexpr (sizeof(T) == 2) {
-    store16(x + i * 8, decode8_bf16(c[0], c[1], s), past);
+    store16<PAST>(x + i * 8, decode8_bf16(c[0], c[1], s));
   } else {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       float v[4];
       decode4(c[h], s, v);
-      store16(x + i * 8 + 4 * h, u32x4_t{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]),
-                                         __float_as_uint(v[3])}, past);
+      store16<PAST>(x + i * 8 + 4 * h, u32x4_t{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]),
+                                               __float_as_uint(v[3])});
     }
   }
 }
@@ -539,9 +539,11 @@ hipError_t launch_act8_restore(int dtype, int rows, int cols, const uint8_t* q, 
   if (!chunk_grid(rows, cols, &n, &grid)) return hipErrorInvalidValue;
   const bool past = (size_t)rows * cols * (dtype == DT_BF16 ? 2 : 4) >= kStreamBytes;
   if (dtype == DT_BF16)
-    hipLaunchKernelGGL(act8_restore_kernel<bf16_t>, grid, dim3(256), 0, s, n, past, q, scales, (bf16_t*)x);
+    hipLaunchKernelGGL((past ? act8_restore_kernel<bf16_t, true> : act8_restore_kernel<bf16_t, false>), grid, dim3(256), 0,
+                       s, n, q, scales, (bf16_t*)x);
   else
-    hipLaunchKernelGGL(act8_restore_kernel<float>, grid, dim3(256), 0, s, n, past, q, scales, (float*)x);
+    hipLaunchKernelGGL((past ? act8_restore_kernel<float, true> : act8_restore_kernel<float, false>), grid, dim3(256), 0, s,
+                       n, q, scales, (float*)x);
   return hipGetLastError();
 }
 

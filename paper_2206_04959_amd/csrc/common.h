@@ -88,9 +88,11 @@ __device__ __forceinline__ void store8(float* p, const float v[8]) {
   reinterpret_cast<f32x4_t*>(p)[1] = f32x4_t{v[4], v[5], v[6], v[7]};
 }
 
-// 16 bytes, past the caches if `past` (uniform).
-__device__ __forceinline__ void store16(void* p, u32x4_t v, bool past) {
-  if (past) __builtin_nontemporal_store(v, reinterpret_cast<u32x4_t*>(p));
+// 16 bytes, past the caches if PAST.  (A template argument: with a run-time flag the compiler
+// makes one ordinary store of the two.)
+template <bool PAST>
+__device__ __forceinline__ void store16(void* p, u32x4_t v) {
+  if constexpr (PAST) __builtin_nontemporal_store(v, reinterpret_cast<u32x4_t*>(p));
   else *reinterpret_cast<u32x4_t*>(p) = v;
 }
 

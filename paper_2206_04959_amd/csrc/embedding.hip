@@ -34,9 +34,9 @@ __device__ __forceinline__ int table_row(I id, long long first, int rows) {
 // ---------------------------------------------------------------------------
 constexpr int kFwdUnroll = 4;
 
-template <typename T, typename I>
+template <typename T, typename I, bool PAST>
 __global__ void __launch_bounds__(256) embedding_fwd_kernel(int tokens, int hidden, int rows, long long first,
-                                                            float scale, bool past, const I* __restrict__ ids,
+                                                            float scale, const I* __restrict__ ids,
                                                             const T* __restrict__ table, T* __restrict__ y) {
   constexpr int EPC = 16 / sizeof(T);  // elements per chunk
   const unsigned cpr = hidden / EPC;
@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(256) embedding_fwd_kernel(int tokens, int hidd
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[e] = __float_as_uint(__uint_as_float(v[u][e]) * scale);
     }
-    store16(y + at[u], o, past);
+    store16<PAST>(y + at[u], o);
   }
 }
 
@@ -254,8 +254,9 @@ __device__ __forceinline__ void write_row(float* out, const float acc[8], float 
   store8(out, v);
 }
 
-__device__ __forceinline__ void clear_row(float* row, int hidden, int lane, bool past) {
-  for (int c = lane * 4; c < hidden; c += 256) store16(row + c, u32x4_t{0u, 0u, 0u, 0u}, past);
+template <bool PAST>
+__device__ __forceinline__ void clear_row(float* row, int hidden, int lane) {
+  for (int c = lane * 4; c < hidden; c += 256) store16<PAST>(row + c, u32x4_t{0u, 0u, 0u, 0u});
 }
 
 struct EmbeddingSum {
@@ -267,7 +268,6 @@ struct EmbeddingSum {
   int* split;       // split[0]: how many runs are split, then the chunks in which they begin
   float* out;       // [rows][hidden]
   int sum_blocks;   // workgroups that sum; the rest clear rows
-  bool past;        // clear them past the caches
 };
 
 // Tokens of the run across the border at sorted position p > 0, counted to both sides of
@@ -296,7 +296,7 @@ __device__ __forceinline__ Across run_across(const EmbeddingSum& a, int p, int k
 // begins in the chunk, else into part[c][0]; the chunk in which it begins is noted, and
 // embedding_join_kernel adds the parts.
 // The workgroups after those clear the rows that no token names.
-template <typename T>
+template <typename T, bool PAST>
 __global__ void __launch_bounds__(256) embedding_sum_kernel(EmbeddingSum a, const T* __restrict__ dy) {
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if ((int)blockIdx.x >= a.sum_blocks) {
@@ -308,7 +308,7 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(EmbeddingSum a, cons
     if ((lane & 15) == 0) used[threadIdx.x >> 4] = p < a.tokens && a.key[p] == r;
     __syncthreads();
     for (int i = w; i < kFillRows && r0 + i < a.rows; i += 4)
-      if (!used[i]) clear_row(a.out + (size_t)(r0 + i) * a.hidden, a.hidden, lane, a.past);
+      if (!used[i]) clear_row<PAST>(a.out + (size_t)(r0 + i) * a.hidden, a.hidden, lane);
     return;
   }
   const int slabs = (a.hidden + kSlab - 1) / kSlab;
@@ -431,7 +431,7 @@ __global__ void __launch_bounds__(64 * kJoinWaves) embedding_join_kernel(Embeddi
 
 // Up to kDirect tokens: every wave holds all rows in its lanes, four a lane.  A wave per
 // token and 512 columns; the first token of a row adds the row's tokens in order.
-template <typename T, typename I>
+template <typename T, typename I, bool PAST>
 __global__ void __launch_bounds__(256) embedding_direct_kernel(EmbeddingSum a, long long first,
                                                                const I* __restrict__ ids, const T* __restrict__ dy) {
   constexpr int KG = kDirect / 64;
@@ -448,7 +448,7 @@ __global__ void __launch_bounds__(256) embedding_direct_kernel(EmbeddingSum a, l
       bool used = false;
 #pragma unroll
       for (int g = 0; g < KG; ++g) used |= key[g] == r0 + i;
-      if (__ballot(used) == 0ull) clear_row(a.out + (size_t)(r0 + i) * a.hidden, a.hidden, lane, a.past);
+      if (__ballot(used) == 0ull) clear_row<PAST>(a.out + (size_t)(r0 + i) * a.hidden, a.hidden, lane);
     }
     return;
   }
@@ -514,9 +514,9 @@ static hipError_t fwd_t(int tokens, int hidden, int rows, long long first, float
   const long long chunks = (long long)tokens * (hidden / (16 / (int)sizeof(T)));
   const long long wg = (chunks + 256 * kFwdUnroll - 1) / (256 * kFwdUnroll);
   if (wg > 0x7fffffffLL) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((embedding_fwd_kernel<T, I>), dim3((unsigned)wg), dim3(256), 0, s, tokens, hidden, rows, first,
-                     scale, (size_t)tokens * hidden * sizeof(T) >= kStreamBytes, (const I*)ids, (const T*)table,
-                     (T*)y);
+  const bool past = (size_t)tokens * hidden * sizeof(T) >= kStreamBytes;
+  hipLaunchKernelGGL((past ? embedding_fwd_kernel<T, I, true> : embedding_fwd_kernel<T, I, false>), dim3((unsigned)wg),
+                     dim3(256), 0, s, tokens, hidden, rows, first, scale, (const I*)ids, (const T*)table, (T*)y);
   return hipGetLastError();
 }
 
@@ -545,10 +545,11 @@ template <typename T, typename I>
 static hipError_t bwd_t(EmbeddingSum a, long long first, const void* ids, const void* dy, char* scratch,
                         hipStream_t s) {
   const long long slabs = (a.hidden + kSlab - 1) / kSlab;
+  const bool past = (size_t)a.rows * a.hidden * sizeof(float) >= kStreamBytes;
   const long long fill = a.accumulate ? 0 : ((long long)a.rows + kFillRows - 1) / kFillRows;
   if (a.tokens <= kDirect) {
     a.sum_blocks = (int)((a.tokens * slabs + 3) / 4);
-    hipLaunchKernelGGL((embedding_direct_kernel<T, I>), dim3((unsigned)(a.sum_blocks + fill)), dim3(256), 0, s, a,
+    hipLaunchKernelGGL((past ? embedding_direct_kernel<T, I, true> : embedding_direct_kernel<T, I, false>), dim3((unsigned)(a.sum_blocks + fill)), dim3(256), 0, s, a,
                        first, (const I*)ids, (const T*)dy);
     return hipGetLastError();
   }
@@ -581,7 +582,7 @@ static hipError_t bwd_t(EmbeddingSum a, long long first, const void* ids, const 
   a.part = (float*)(scratch + 4 * ob + order_bytes(1 + kMaxChunks));
   const long long units = (((long long)a.tokens + a.chunk - 1) / a.chunk) * slabs;
   a.sum_blocks = (int)((units + 3) / 4);
-  hipLaunchKernelGGL(embedding_sum_kernel<T>, dim3((unsigned)(a.sum_blocks + fill)), dim3(256), 0, s, a,
+  hipLaunchKernelGGL((past ? embedding_sum_kernel<T, true> : embedding_sum_kernel<T, false>), dim3((unsigned)(a.sum_blocks + fill)), dim3(256), 0, s, a,
                      (const T*)dy);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
@@ -599,7 +600,6 @@ hipError_t launch_embedding_bwd(int dtype, int id_type, int tokens, int hidden, 
   a.accumulate = accumulate;
   a.scale = scale;
   a.out = dtable;
-  a.past = (size_t)rows * hidden * sizeof(float) >= kStreamBytes;
   char* sc = (char*)scratch;
   if (dtype == DT_BF16)
     return id_type == ID_I32 ? bwd_t<bf16_t, int>(a, first, ids, dy, sc, s)
