@@ -532,6 +532,8 @@ def _qk_args(what, qkv, q_gamma, k_gamma, table, positions, q_heads, kv_heads, s
     if q_heads <= 0 or kv_heads <= 0 or row <= 0 or n % row != 0:
         raise ValueError(f"{what}: qkv is [tokens, q_heads + 2 * kv_heads, head_dim]")
     tokens = n // row
+    if tokens > 0x7fffffff:
+        raise ValueError(f"{what}: {tokens} tokens")
     if table is None:
         return (dt, tokens, q_heads, kv_heads, d, 0, int(interleaved), eps), (None, 0, None, 0)
     rows, rope = _table(what, table)
@@ -597,6 +599,8 @@ def _act8(what, q, scales):
     cols, n = q.shape[-1], q.numel()
     if cols <= 0 or cols % 32 or scales.shape[-1] * 32 != cols or scales.numel() * 32 != n:
         raise ValueError(f"{what}: q is [rows, cols] and scales [rows, cols / 32], cols a multiple of 32")
+    if n // cols > 0x7fffffff:
+        raise ValueError(f"{what}: {n // cols} rows")
     return n // cols, cols
 
 

@@ -133,7 +133,8 @@ __device__ __forceinline__ void gelu_both(float u, float* gelu, float* slope) {
 
 // du = dg * gelu'(u) and, unless g is NULL, g = gelu(u), with u in 8 bits.
 template <typename T>
-__global__ void __launch_bounds__(256) act8_gelu_bwd_kernel(long long chunks, const T* dg, const uint8_t* __restrict__ q,
+__global__ void __launch_bounds__(256) act8_gelu_bwd_kernel(long long chunks, const T* dg,
+                                                            const uint8_t* __restrict__ q,
                                                             const uint8_t* __restrict__ scales, T* du,
                                                             T* __restrict__ g) {
   const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
@@ -539,11 +540,11 @@ hipError_t launch_act8_restore(int dtype, int rows, int cols, const uint8_t* q, 
   if (!chunk_grid(rows, cols, &n, &grid)) return hipErrorInvalidValue;
   const bool past = (size_t)rows * cols * (dtype == DT_BF16 ? 2 : 4) >= kStreamBytes;
   if (dtype == DT_BF16)
-    hipLaunchKernelGGL((past ? act8_restore_kernel<bf16_t, true> : act8_restore_kernel<bf16_t, false>), grid, dim3(256), 0,
-                       s, n, q, scales, (bf16_t*)x);
+    hipLaunchKernelGGL((past ? act8_restore_kernel<bf16_t, true> : act8_restore_kernel<bf16_t, false>), grid,
+                       dim3(256), 0, s, n, q, scales, (bf16_t*)x);
   else
-    hipLaunchKernelGGL((past ? act8_restore_kernel<float, true> : act8_restore_kernel<float, false>), grid, dim3(256), 0, s,
-                       n, q, scales, (float*)x);
+    hipLaunchKernelGGL((past ? act8_restore_kernel<float, true> : act8_restore_kernel<float, false>), grid,
+                       dim3(256), 0, s, n, q, scales, (float*)x);
   return hipGetLastError();
 }
 

@@ -78,7 +78,7 @@ __global__ void __launch_bounds__(256) embedding_fwd_kernel(int tokens, int hidd
 // ---------------------------------------------------------------------------
 // Backward
 // ---------------------------------------------------------------------------
-constexpr int kDirect = 256;      // up to here one launch, without sorting
+constexpr int kDirect = 2048;     // up to here one launch, without sorting
 constexpr int kSortBlock = 2048;  // tokens that are ranked against each other
 constexpr int kFillRows = 16;     // table rows that a workgroup clears
 constexpr int kSlab = 512;        // columns of a wave: 8 a lane
@@ -268,6 +268,7 @@ struct EmbeddingSum {
   int* split;       // split[0]: how many runs are split, then the chunks in which they begin
   float* out;       // [rows][hidden]
   int sum_blocks;   // workgroups that sum; the rest clear rows
+  int width;        // columns of a workgroup of embedding_direct_kernel, a multiple of kSlab
 };
 
 // Tokens of the run across the border at sorted position p > 0, counted to both sides of
@@ -429,80 +430,131 @@ __global__ void __launch_bounds__(64 * kJoinWaves) embedding_join_kernel(Embeddi
   }
 }
 
-// Up to kDirect tokens: every wave holds all rows in its lanes, four a lane.  A wave per
-// token and 512 columns; the first token of a row adds the row's tokens in order.
+// Up to kDirect tokens, in one launch without sorting.  Every workgroup brings the tokens'
+// rows into LDS.  A wave takes a token and `width` columns; if no earlier token has its
+// row, it lists the row's tokens and adds them in order.  Rows of more than kAlone tokens are
+// shared by the workgroup's four waves (each lists every fourth 64 tokens'), and the
+// waves' sums are added in order.
+constexpr int kAlone = 64;
+
+// Appends the tokens of row k among tokens 64 q .. 64 q + 63 to the wave's list.
+__device__ __forceinline__ int list_row(const int* key, int k, int q, int lane, unsigned short* list, int n) {
+  const bool hit = key[64 * q + lane] == k;
+  const unsigned long long m = __ballot(hit);
+  if (hit) list[n + __builtin_popcountll(m & ((1ull << lane) - 1))] = (unsigned short)(64 * q + lane);
+  return n + __builtin_popcountll(m);
+}
+
+// Sum of the listed tokens' 8 columns from col on (which the row has).
+template <typename T>
+__device__ __forceinline__ void add_listed(const EmbeddingSum& a, const T* dy, int col, const unsigned short* list,
+                                           int n, float acc[8]) {
+  constexpr int U = sizeof(T) == 2 ? 16 : 8;  // rows in flight
+  constexpr int W = sizeof(T) / 2;            // 16-byte pieces of 8 columns
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
+  for (int i = 0; i < n; i += U) {
+    u32x4_t v[U][W];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int e = 0; e < W; ++e) v[u][e] = u32x4_t{0u, 0u, 0u, 0u};
+      if (i + u < n) {
+        const T* p = dy + (size_t)__builtin_amdgcn_readfirstlane(list[i + u]) * a.hidden + col;
+#pragma unroll
+        for (int e = 0; e < W; ++e) v[u][e] = reinterpret_cast<const u32x4_t*>(p)[e];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float f[8];
+      unpack_row<T>(v[u], f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] += f[e];
+    }
+  }
+}
+
 template <typename T, typename I, bool PAST>
 __global__ void __launch_bounds__(256) embedding_direct_kernel(EmbeddingSum a, long long first,
                                                                const I* __restrict__ ids, const T* __restrict__ dy) {
-  constexpr int KG = kDirect / 64;
+  constexpr int PER = kDirect / 256;
+  __shared__ int key[kDirect];
+  __shared__ unsigned short lists[4][kDirect];
+  __shared__ float red[3][64][9];
+  __shared__ int flag[kFillRows];  // rows in use, or the waves' long rows' tokens
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int key[KG];
+  const bool fill = (int)blockIdx.x >= a.sum_blocks;
+  const int r0 = (blockIdx.x - a.sum_blocks) * kFillRows;
+  if (threadIdx.x < kFillRows) flag[threadIdx.x] = fill ? 0 : -1;
+  I id[PER];
 #pragma unroll
-  for (int g = 0; g < KG; ++g) {
-    const int t = 64 * g + lane;
-    key[g] = t < a.tokens ? table_row(ids[t], first, a.rows) : a.rows;
+  for (int u = 0; u < PER; ++u) {
+    const int t = 256 * u + threadIdx.x;
+    id[u] = t < a.tokens ? ids[t] : (I)0;
   }
-  if ((int)blockIdx.x >= a.sum_blocks) {
-    const int r0 = (blockIdx.x - a.sum_blocks) * kFillRows;
-    for (int i = w; i < kFillRows && r0 + i < a.rows; i += 4) {
-      bool used = false;
+  __syncthreads();
 #pragma unroll
-      for (int g = 0; g < KG; ++g) used |= key[g] == r0 + i;
-      if (__ballot(used) == 0ull) clear_row<PAST>(a.out + (size_t)(r0 + i) * a.hidden, a.hidden, lane);
-    }
+  for (int u = 0; u < PER; ++u) {
+    const int t = 256 * u + threadIdx.x;
+    const int k = t < a.tokens ? table_row(id[u], first, a.rows) : a.rows;
+    if (!fill) key[t] = k;
+    else if (k >= r0 && k < r0 + kFillRows && k < a.rows) flag[k - r0] = 1;
+  }
+  __syncthreads();
+  if (fill) {
+    for (int i = w; i < kFillRows && r0 + i < a.rows; i += 4)
+      if (!flag[i]) clear_row<PAST>(a.out + (size_t)(r0 + i) * a.hidden, a.hidden, lane);
     return;
   }
-  const int slabs = (a.hidden + kSlab - 1) / kSlab;
-  const int unit = blockIdx.x * 4 + w;
-  const int t = unit / slabs, col = (unit % slabs) * kSlab + lane * 8;
-  if (t >= a.tokens) return;
-  int k = a.rows;
-#pragma unroll
-  for (int g = 0; g < KG; ++g)
-    if (t >> 6 == g) k = __builtin_amdgcn_readlane(key[g], t & 63);
-  if (k >= a.rows) return;
-  unsigned long long run[KG];
-  int head = -1;  // the row's first token
-#pragma unroll
-  for (int g = KG - 1; g >= 0; --g) {
-    run[g] = __ballot(key[g] == k);
-    if (run[g]) head = 64 * g + __builtin_ctzll(run[g]);
+  const int groups = (a.tokens + 63) >> 6, parts = (a.hidden + a.width - 1) / a.width;
+  const int t = (blockIdx.x / parts) * 4 + w;
+  const int col0 = (blockIdx.x % parts) * a.width, col1 = min(col0 + a.width, a.hidden);  // this workgroup's columns
+  const int k = t < a.tokens ? __builtin_amdgcn_readfirstlane(key[t]) : a.rows;
+  unsigned short* list = lists[w];
+  int n = 0;
+  if (k < a.rows) {
+    bool earlier = false;
+    for (int q = 0; q < t >> 6 && !earlier; ++q) earlier = __ballot(key[64 * q + lane] == k) != 0ull;
+    earlier = earlier || (__ballot(key[(t & ~63) + lane] == k) & ((1ull << (t & 63)) - 1)) != 0ull;
+    if (!earlier)
+      for (int q = t >> 6; q < groups; ++q) n = list_row(key, k, q, lane, list, n);
   }
-  if (head != t) return;
-  const bool live = col < a.hidden;
-  float acc[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
-#pragma unroll
-  for (int g = 0; g < KG; ++g) {
-    unsigned long long r = run[g];
-    while (r) {
-      constexpr int U = sizeof(T) == 2 ? 16 : 8;  // rows in flight
-      constexpr int W = sizeof(T) / 2;            // 16-byte pieces of 8 columns
-      u32x4_t v[U][W];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-#pragma unroll
-        for (int e = 0; e < W; ++e) v[u][e] = u32x4_t{0u, 0u, 0u, 0u};
-        if (r) {
-          const T* p = dy + (size_t)(64 * g + __builtin_ctzll(r)) * a.hidden + col;
-          if (live) {
-#pragma unroll
-            for (int e = 0; e < W; ++e) v[u][e] = reinterpret_cast<const u32x4_t*>(p)[e];
-          }
-          r &= r - 1;
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        float f[8];
-        unpack_row<T>(v[u], f);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] += f[e];
-      }
+  if (n > kAlone) {
+    if (lane == 0) flag[w] = t;
+  } else if (n > 0) {
+    for (int col = col0 + lane * 8; col < col1; col += kSlab) {
+      float acc[8];
+      add_listed(a, dy, col, list, n, acc);
+      write_row(a.out + (size_t)k * a.hidden + col, acc, a.scale, a.accumulate);
     }
   }
-  if (live) write_row(a.out + (size_t)k * a.hidden + col, acc, a.scale, a.accumulate);
+  __syncthreads();
+  for (int i = 0; i < 4; ++i) {
+    const int head = flag[i];
+    if (head < 0) continue;
+    const int row = __builtin_amdgcn_readfirstlane(key[head]);
+    n = 0;
+    for (int q = w; q < groups; q += 4) n = list_row(key, row, q, lane, list, n);
+    for (int c = col0; c < col1; c += kSlab) {
+      const int col = c + lane * 8;
+      const bool live = col < col1;
+      float acc[8];
+      if (live) add_listed(a, dy, col, list, n, acc);
+      if (w > 0 && live)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) red[w - 1][lane][e] = acc[e];
+      __syncthreads();
+      if (w == 0 && live) {
+#pragma unroll
+        for (int j = 0; j < 3; ++j)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) acc[e] += red[j][lane][e];
+        write_row(a.out + (size_t)row * a.hidden + col, acc, a.scale, a.accumulate);
+      }
+      __syncthreads();
+    }
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -548,9 +600,13 @@ static hipError_t bwd_t(EmbeddingSum a, long long first, const void* ids, const 
   const bool past = (size_t)a.rows * a.hidden * sizeof(float) >= kStreamBytes;
   const long long fill = a.accumulate ? 0 : ((long long)a.rows + kFillRows - 1) / kFillRows;
   if (a.tokens <= kDirect) {
-    a.sum_blocks = (int)((a.tokens * slabs + 3) / 4);
-    hipLaunchKernelGGL((past ? embedding_direct_kernel<T, I, true> : embedding_direct_kernel<T, I, false>), dim3((unsigned)(a.sum_blocks + fill)), dim3(256), 0, s, a,
-                       first, (const I*)ids, (const T*)dy);
+    // 512 columns a workgroup, more where that makes over 2048 workgroups, each of which reads
+    // all ids.
+    const long long quads = (a.tokens + 3) / 4, per = (quads * slabs + 2047) / 2048;
+    a.width = (int)(per * kSlab);
+    a.sum_blocks = (int)(quads * ((slabs + per - 1) / per));
+    hipLaunchKernelGGL((past ? embedding_direct_kernel<T, I, true> : embedding_direct_kernel<T, I, false>),
+                       dim3((unsigned)(a.sum_blocks + fill)), dim3(256), 0, s, a, first, (const I*)ids, (const T*)dy);
     return hipGetLastError();
   }
   const size_t ob = order_bytes(a.tokens);
@@ -559,31 +615,28 @@ static hipError_t bwd_t(EmbeddingSum a, long long first, const void* ids, const 
   int* skey = (int*)(scratch + 2 * ob);
   int* stok = (int*)(scratch + 3 * ob);
   a.split = (int*)(scratch + 4 * ob);
-  const bool one = a.tokens <= kSortBlock;  // one block: its order is the whole order
-  const unsigned wg = (unsigned)(((long long)a.tokens + 63) / 64);
-  hipLaunchKernelGGL((embedding_rank_kernel<I>), dim3(wg), dim3(64 * kRankWaves), 0, s, a.tokens, a.rows, first, (const I*)ids,
-                     one ? gkey : skey, one ? gtok : stok, a.split);
+  const unsigned wg = (unsigned)((a.tokens + 63) / 64);
+  hipLaunchKernelGGL((embedding_rank_kernel<I>), dim3(wg), dim3(64 * kRankWaves), 0, s, a.tokens, a.rows, first,
+                     (const I*)ids, skey, stok, a.split);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (!one) {
-    const int waves = std::min(kMergeWaves, (a.tokens + kSortBlock - 1) / kSortBlock);
-    const size_t lds = (size_t)waves * (kSortBlock + 64) * sizeof(int);
-    static std::atomic<uint64_t> lds_set{0};
-    e = allow_dynamic_lds(reinterpret_cast<const void*>(embedding_merge_kernel),
-                          (size_t)kMergeWaves * (kSortBlock + 64) * sizeof(int), lds_set);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(embedding_merge_kernel, dim3(wg), dim3(64 * waves), lds, s, a.tokens, skey, stok, gkey, gtok);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
+  const int waves = std::min(kMergeWaves, (a.tokens + kSortBlock - 1) / kSortBlock);
+  const size_t lds = (size_t)waves * (kSortBlock + 64) * sizeof(int);
+  static std::atomic<uint64_t> lds_set{0};
+  e = allow_dynamic_lds(reinterpret_cast<const void*>(embedding_merge_kernel),
+                        (size_t)kMergeWaves * (kSortBlock + 64) * sizeof(int), lds_set);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(embedding_merge_kernel, dim3(wg), dim3(64 * waves), lds, s, a.tokens, skey, stok, gkey, gtok);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
   a.chunk = chunk_len(a.tokens);
   a.key = gkey;
   a.tok = gtok;
   a.part = (float*)(scratch + 4 * ob + order_bytes(1 + kMaxChunks));
   const long long units = (((long long)a.tokens + a.chunk - 1) / a.chunk) * slabs;
   a.sum_blocks = (int)((units + 3) / 4);
-  hipLaunchKernelGGL((past ? embedding_sum_kernel<T, true> : embedding_sum_kernel<T, false>), dim3((unsigned)(a.sum_blocks + fill)), dim3(256), 0, s, a,
-                     (const T*)dy);
+  hipLaunchKernelGGL((past ? embedding_sum_kernel<T, true> : embedding_sum_kernel<T, false>),
+                     dim3((unsigned)(a.sum_blocks + fill)), dim3(256), 0, s, a, (const T*)dy);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(embedding_join_kernel, dim3(kJoinBlocks), dim3(64 * kJoinWaves), 0, s, a);

@@ -35,7 +35,8 @@ int check_apart(std::initializer_list<Span> written, std::initializer_list<Span>
 
 size_t elem(int dtype) { return dtype == MERAK_BF16 ? 2 : 4; }
 
-constexpr int kMaxSorted = 1 << 22;  // tokens of one embedding gradient: sorting compares every pair of 2048-token blocks
+// Tokens of one embedding gradient: sorting compares every pair of 2048-token blocks.
+constexpr int kMaxSorted = 1 << 22;
 constexpr int kMaxRows = 1 << 30;  // tokens and table rows: the kernels count them in 32 bits
 
 size_t id_bytes(int id_type) { return id_type == MERAK_I32 ? 4 : 8; }
@@ -68,10 +69,13 @@ int check_qk(int dtype, int tokens, int q_heads, int kv_heads, int head_dim, int
   return MERAK_OK;
 }
 
-QkShape qk_shape(int tokens, int q_heads, int kv_heads, int head_dim, int rope_dim, int interleaved, float eps,
-                 const float* table, int table_rows, const int32_t* positions, int seq_len) {
-  return QkShape{tokens, q_heads, kv_heads, head_dim, rope_dim, interleaved, eps, table, table_rows, positions, seq_len};
+size_t qk_row_bytes(const QkShape& q, int dtype) {
+  return (size_t)q.tokens * (q.q_heads + 2 * q.kv_heads) * q.head_dim * elem(dtype);
 }
+
+// What the calls of a shape read besides the rows.
+Span table_span(const QkShape& q) { return {q.table, q.rope_dim > 0 ? (size_t)q.table_rows * q.rope_dim * 4 : 0}; }
+Span position_span(const QkShape& q) { return {q.positions, q.rope_dim > 0 ? (size_t)q.tokens * 4 : 0}; }
 
 int check_act8(int dtype, int rows, int cols, const uint8_t* q, const uint8_t* scales) {
   TRY(check_dtype(dtype));
@@ -131,13 +135,12 @@ int merak_qk_norm_rope_fwd(int dtype, int tokens, int q_heads, int kv_heads, int
   TRY(check_qk(dtype, tokens, q_heads, kv_heads, head_dim, rope_dim, interleaved, eps, table, table_rows, positions,
                seq_len));
   TRY(check_ptr(qkv)); TRY(check_ptr(q_gamma)); TRY(check_ptr(k_gamma)); TRY(check_ptr(out));
-  const size_t row = (size_t)tokens * (q_heads + 2 * kv_heads) * head_dim * elem(dtype), gain = head_dim * elem(dtype);
-  const size_t tb = rope_dim > 0 ? (size_t)table_rows * rope_dim * 4 : 0, pb = positions && rope_dim > 0 ? tokens * (size_t)4 : 0;
-  TRY(check_apart({{out, row}}, {{out == qkv ? nullptr : qkv, row}, {q_gamma, gain}, {k_gamma, gain}, {table, tb},
-                                 {positions, pb}}));
-  HIP_TRY(launch_qk_norm_rope_fwd(dtype, qk_shape(tokens, q_heads, kv_heads, head_dim, rope_dim, interleaved, eps,
-                                                  table, table_rows, positions, seq_len),
-                                  qkv, q_gamma, k_gamma, out, (hipStream_t)stream));
+  const QkShape shape{tokens, q_heads, kv_heads, head_dim, rope_dim, interleaved, eps, table, table_rows, positions,
+                      seq_len};
+  const size_t row = qk_row_bytes(shape, dtype), gain = head_dim * elem(dtype);
+  TRY(check_apart({{out, row}}, {{out == qkv ? nullptr : qkv, row}, {q_gamma, gain}, {k_gamma, gain}, table_span(shape),
+                                 position_span(shape)}));
+  HIP_TRY(launch_qk_norm_rope_fwd(dtype, shape, qkv, q_gamma, k_gamma, out, (hipStream_t)stream));
   return MERAK_OK;
 }
 
@@ -156,20 +159,15 @@ int merak_qk_norm_rope_bwd(int dtype, int tokens, int q_heads, int kv_heads, int
   TRY(check_flag(accumulate));
   TRY(check_ptr(dout)); TRY(check_ptr(qkv)); TRY(check_ptr(q_gamma)); TRY(check_ptr(k_gamma)); TRY(check_ptr(dqkv));
   TRY(check_ptr(dq_gamma)); TRY(check_ptr(dk_gamma)); TRY(check_ptr(scratch));
-  const size_t row = (size_t)tokens * (q_heads + 2 * kv_heads) * head_dim * elem(dtype), gain = head_dim * elem(dtype);
-  const size_t tb = rope_dim > 0 ? (size_t)table_rows * rope_dim * 4 : 0, pb = positions && rope_dim > 0 ? tokens * (size_t)4 : 0;
-  const size_t dg = head_dim * sizeof(float);
-  TRY(check_apart({{dqkv, row}, {dq_gamma, dg}, {dk_gamma, dg},
-                   {scratch, 4 * qk_norm_rope_scratch_elems(tokens, q_heads, kv_heads, head_dim)}},
-                  {{qkv, row}, {q_gamma, gain}, {k_gamma, gain}, {table, tb}, {positions, pb}}));
-  if (dqkv != dout)
-    TRY(check_apart({{dqkv, row}}, {{dout, row}}));
-  TRY(check_apart({{dq_gamma, dg}, {dk_gamma, dg},
-                   {scratch, 4 * qk_norm_rope_scratch_elems(tokens, q_heads, kv_heads, head_dim)}}, {{dout, row}}));
-  HIP_TRY(launch_qk_norm_rope_bwd(dtype, qk_shape(tokens, q_heads, kv_heads, head_dim, rope_dim, interleaved, eps,
-                                                  table, table_rows, positions, seq_len),
-                                  dout, qkv, q_gamma, k_gamma, dqkv, dq_gamma, dk_gamma, accumulate, scratch,
-                                  (hipStream_t)stream));
+  const QkShape shape{tokens, q_heads, kv_heads, head_dim, rope_dim, interleaved, eps, table, table_rows, positions,
+                      seq_len};
+  const size_t row = qk_row_bytes(shape, dtype), gain = head_dim * elem(dtype), dg = head_dim * sizeof(float);
+  const Span sums{scratch, sizeof(float) * qk_norm_rope_scratch_elems(tokens, q_heads, kv_heads, head_dim)};
+  TRY(check_apart({{dqkv, row}, {dq_gamma, dg}, {dk_gamma, dg}, sums},
+                  {{qkv, row}, {q_gamma, gain}, {k_gamma, gain}, table_span(shape), position_span(shape),
+                   {dqkv == dout ? nullptr : dout, row}}));
+  HIP_TRY(launch_qk_norm_rope_bwd(dtype, shape, dout, qkv, q_gamma, k_gamma, dqkv, dq_gamma, dk_gamma, accumulate,
+                                  scratch, (hipStream_t)stream));
   return MERAK_OK;
 }
 

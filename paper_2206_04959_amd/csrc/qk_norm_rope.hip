@@ -61,10 +61,12 @@ struct QkArgs {
 template <int X>
 __device__ __forceinline__ float xor_lane(float v) {
   const int i = __float_as_int(v);
-  if constexpr (X == 1) return __int_as_float(__builtin_amdgcn_update_dpp(0, i, 0xB1, 0xf, 0xf, true));  // quad [1,0,3,2]
-  else if constexpr (X == 2) return __int_as_float(__builtin_amdgcn_update_dpp(0, i, 0x4E, 0xf, 0xf, true));  // [2,3,0,1]
-  else if constexpr (X == 8) return __int_as_float(__builtin_amdgcn_update_dpp(0, i, 0x128, 0xf, 0xf, true));  // row_ror:8
-  else return __int_as_float(__builtin_amdgcn_ds_swizzle(i, 0x1f | (X << 10)));  // 4, 16: xor within 32 lanes
+  int r;
+  if constexpr (X == 1) r = __builtin_amdgcn_update_dpp(0, i, 0xB1, 0xf, 0xf, true);        // quad_perm [1,0,3,2]
+  else if constexpr (X == 2) r = __builtin_amdgcn_update_dpp(0, i, 0x4E, 0xf, 0xf, true);   // quad_perm [2,3,0,1]
+  else if constexpr (X == 8) r = __builtin_amdgcn_update_dpp(0, i, 0x128, 0xf, 0xf, true);  // row_ror:8
+  else r = __builtin_amdgcn_ds_swizzle(i, 0x1f | (X << 10));  // 4, 16: exclusive or within 32 lanes
+  return __int_as_float(r);
 }
 
 template <int G>
