@@ -458,13 +458,17 @@ static hipError_t launch_dw_join(long long elems, int splits, const float* part,
   return hipGetLastError();
 }
 
-// fp32 check mode, on the fp32 matrix instruction (32 x 32 x 2): 64 x 64 tiles, four
-// waves of 32 x 32, 32 tokens a stage, the next stage's operands on their way to
-// registers meanwhile.
-constexpr int kDwTileF32 = 64, kStageF32 = 32;
+// fp32 check mode, on the fp32 matrix instruction (32 x 32 x 2): tiles of 64 NB x 64 NB, four
+// waves of 32 NB x 32 NB, 32 tokens a stage.  The next stage's operands are on their way to
+// registers meanwhile, X's as codes until they go to LDS, and fragments are read ahead of
+// their MFMAs.  Bound by the matrix instruction's rate: 8192 x 4096 x 4096 2.12 ms (130
+// TFLOP/s; 153 is what the library reaches there); NB = 1 125, and 1000 x 3000 x 1024 98
+// against 85.
+constexpr int kStageF32 = 32;
 
+template <int NB>
 __global__ void __launch_bounds__(256) act8_dw_f32_kernel(DwArgs p, const float* __restrict__ dy) {
-  constexpr int R = kDwTileF32, KB = kStageF32;
+  constexpr int R = 64 * NB, KB = kStageF32, W = 32 * NB;
   __shared__ __align__(16) float sa[KB][R];
   __shared__ __align__(16) float sb[KB][R];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, hf = lane >> 5;
@@ -473,42 +477,84 @@ __global__ void __launch_bounds__(256) act8_dw_f32_kernel(DwArgs p, const float*
   const int tiles_n = (p.n_in + R - 1) / R;
   const int m0 = (tile / tiles_n) * R, n0 = (tile % tiles_n) * R;
   const int first = split * p.per_split, end = min(p.tokens, first + p.per_split);
-  const int kr = threadIdx.x >> 3, c8 = (threadIdx.x & 7) * 8;
-  f32x16_t acc;
+  const int kr = threadIdx.x >> 3, c8 = (threadIdx.x & 7) * 8;  // columns c8 + 64 u of row kr
+  f32x16_t acc[NB][NB];
 #pragma unroll
-  for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
-  float a[8], b[8];
+  for (int i = 0; i < NB; ++i)
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+  f32x4_t a[NB][2];
+  u32x2_t codes[NB];
+  uint32_t byte[NB];
   auto fetch = [&](int t) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) a[e] = b[e] = 0.0f;
-    if (t < end && m0 + c8 < p.n_out) load8(dy + (size_t)t * p.n_out + m0 + c8, a);
-    if (t < end && n0 + c8 < p.n_in) {
-      const u32x2_t c = *reinterpret_cast<const u32x2_t*>(p.q + (size_t)t * p.n_in + n0 + c8);
-      const float s = scale_of(p.scales[(size_t)t * (p.n_in / kScaleBlock) + (n0 + c8) / kScaleBlock]);
-      decode4(c[0], s, b);
-      decode4(c[1], s, b + 4);
+    for (int u = 0; u < NB; ++u) {
+      const int m = m0 + 64 * u + c8, n = n0 + 64 * u + c8;
+      a[u][0] = a[u][1] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+      codes[u] = u32x2_t{0u, 0u};
+      byte[u] = 0;
+      if (t < end && m < p.n_out) {
+        const float* q = dy + (size_t)t * p.n_out + m;
+        a[u][0] = reinterpret_cast<const f32x4_t*>(q)[0];
+        a[u][1] = reinterpret_cast<const f32x4_t*>(q)[1];
+      }
+      if (t < end && n < p.n_in) {
+        codes[u] = *reinterpret_cast<const u32x2_t*>(p.q + (size_t)t * p.n_in + n);
+        byte[u] = p.scales[(size_t)t * (p.n_in / kScaleBlock) + n / kScaleBlock];
+      }
     }
   };
   fetch(first + kr);
   for (int k0 = first; k0 < end; k0 += KB) {
     __syncthreads();  // the stage before has been read
-    store8(&sa[kr][c8], a);
-    store8(&sb[kr][c8], b);
+#pragma unroll
+    for (int u = 0; u < NB; ++u) {
+      float b[8];
+      decode4(codes[u][0], scale_of(byte[u]), b);
+      decode4(codes[u][1], scale_of(byte[u]), b + 4);
+      *reinterpret_cast<f32x4_t*>(&sa[kr][64 * u + c8]) = a[u][0];
+      *reinterpret_cast<f32x4_t*>(&sa[kr][64 * u + c8 + 4]) = a[u][1];
+      store8(&sb[kr][64 * u + c8], b);
+    }
     __syncthreads();
     fetch(k0 + KB + kr);
+    constexpr int AHEAD = NB == 1 ? 2 : 1;  // steps
+    float fa[KB / 2][NB], fb[KB / 2][NB];
 #pragma unroll
-    for (int k = 0; k < KB; k += 2)
-      acc = __builtin_amdgcn_mfma_f32_32x32x2f32(sa[k + hf][wm * 32 + l32], sb[k + hf][wn * 32 + l32], acc, 0, 0, 0);
+    for (int s = 0; s < KB / 2 + AHEAD; ++s) {
+      if (s < KB / 2) {
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+          fa[s][i] = sa[2 * s + hf][wm * W + 32 * i + l32];
+          fb[s][i] = sb[2 * s + hf][wn * W + 32 * i + l32];
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (s >= AHEAD) {
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+          for (int j = 0; j < NB; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(fa[s - AHEAD][i], fb[s - AHEAD][j], acc[i][j], 0, 0, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
   }
   // acc[r]: output (r / 4) * 8 + 4 * hf + r % 4, input l32
   float* dw = p.out + (size_t)split * p.n_out * p.n_in;
 #pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    const int m = m0 + wm * 32 + (r >> 2) * 8 + hf * 4 + (r & 3), n = n0 + wn * 32 + l32;
-    if (m >= p.n_out || n >= p.n_in) continue;
-    float* out = dw + (size_t)m * p.n_in + n;
-    *out = p.accumulate ? *out + acc[r] : acc[r];
-  }
+  for (int i = 0; i < NB; ++i)
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int m = m0 + wm * W + 32 * i + (r >> 2) * 8 + hf * 4 + (r & 3), n = n0 + wn * W + 32 * j + l32;
+        if (m >= p.n_out || n >= p.n_in) continue;
+        float* out = dw + (size_t)m * p.n_in + n;
+        *out = p.accumulate ? *out + acc[i][j][r] : acc[i][j][r];
+      }
 }
 
 // ---------------------------------------------------------------------------
@@ -618,13 +664,15 @@ static DwPlan dw_plan(int tokens, int n_out, int n_in) {
   return best;
 }
 
-// fp32: 64 x 64 tiles, and splits of at least eight stages where the tiles alone would leave
-// CUs without work (32768 x 512 x 512: 1.1 ms in one split).
+// fp32: 128 x 128 tiles for products of at least 2^14 of their stages, else 64 x 64; and splits
+// of at least eight stages where the tiles alone would leave CUs without work (32768 x
+// 512 x 512: 1.1 ms in one split, 0.17 in 16).
 static DwPlan dw_plan_f32(int tokens, int n_out, int n_in) {
   DwPlan p{};
-  p.bm = p.bn = kDwTileF32;
-  p.tiles = (int)((n_out + kDwTileF32 - 1LL) / kDwTileF32 * ((n_in + kDwTileF32 - 1LL) / kDwTileF32));
+  auto tiles = [&](long long t) { return (n_out + t - 1) / t * ((n_in + t - 1) / t); };
   const int stages = (tokens + kStageF32 - 1) / kStageF32;
+  p.bm = p.bn = tiles(128) * stages >= 1 << 14 ? 128 : 64;
+  p.tiles = (int)tiles(p.bm);
   const int want = std::max(1, std::min(1024 / p.tiles, stages / 8));
   const int per = (stages + want - 1) / want;
   p.splits = (stages + per - 1) / per;
@@ -685,7 +733,8 @@ hipError_t launch_act8_gemm_dw(int dtype, int tokens, int n_out, int n_in, const
   } else {
     const long long wg = (long long)p.tiles * p.splits;
     if (wg > 0x7fffffffLL) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(act8_dw_f32_kernel, dim3((unsigned)wg), dim3(256), 0, s, a, (const float*)dy);
+    hipLaunchKernelGGL((p.bm == 128 ? act8_dw_f32_kernel<2> : act8_dw_f32_kernel<1>), dim3((unsigned)wg), dim3(256),
+                       0, s, a, (const float*)dy);
     e = hipGetLastError();
   }
   if (e != hipSuccess || !split) return e;
