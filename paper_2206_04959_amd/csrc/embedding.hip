@@ -80,7 +80,8 @@ __global__ void __launch_bounds__(256) embedding_fwd_kernel(int tokens, int hidd
 // ---------------------------------------------------------------------------
 constexpr int kDirect = 2048;     // up to here one launch, without sorting
 constexpr int kSortBlock = 2048;  // tokens that are ranked against each other
-constexpr int kFillRows = 16;     // table rows that a workgroup clears
+constexpr int kFillRows = 16;     // most table rows that a workgroup clears
+constexpr size_t kFillBytes = 65536;  // that a workgroup clears, about
 constexpr int kSlab = 512;        // columns of a wave: 8 a lane
 constexpr int kMinChunk = 16, kMaxChunks = 1024;
 constexpr int kWhole = 32;        // a run of up to this many tokens is never split
@@ -267,7 +268,8 @@ struct EmbeddingSum {
   float* part;      // [chunks][2][hidden]
   int* split;       // split[0]: how many runs are split, then the chunks in which they begin
   float* out;       // [rows][hidden]
-  int sum_blocks;   // workgroups that sum; the rest clear rows
+  int sum_blocks;   // workgroups that sum; the rest clear fill_rows rows each
+  int fill_rows;
   int width;        // columns of a workgroup of embedding_direct_kernel, a multiple of kSlab
 };
 
@@ -302,13 +304,13 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(EmbeddingSum a, cons
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if ((int)blockIdx.x >= a.sum_blocks) {
     __shared__ int used[kFillRows];
-    const int r0 = (blockIdx.x - a.sum_blocks) * kFillRows;
+    const int r0 = (blockIdx.x - a.sum_blocks) * a.fill_rows;
     static_assert(kFillRows * 16 == 256, "16 lanes look for a row");
     const int r = r0 + (threadIdx.x >> 4);
-    const int p = lower_bound16(a.key, a.tokens, r, lane);
+    const int p = (int)threadIdx.x >> 4 < a.fill_rows ? lower_bound16(a.key, a.tokens, r, lane) : 0;
     if ((lane & 15) == 0) used[threadIdx.x >> 4] = p < a.tokens && a.key[p] == r;
     __syncthreads();
-    for (int i = w; i < kFillRows && r0 + i < a.rows; i += 4)
+    for (int i = w; i < a.fill_rows && r0 + i < a.rows; i += 4)
       if (!used[i]) clear_row<PAST>(a.out + (size_t)(r0 + i) * a.hidden, a.hidden, lane);
     return;
   }
@@ -485,7 +487,7 @@ __global__ void __launch_bounds__(256) embedding_direct_kernel(EmbeddingSum a, l
   __shared__ int flag[kFillRows];  // rows in use, or the waves' long rows' tokens
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool fill = (int)blockIdx.x >= a.sum_blocks;
-  const int r0 = (blockIdx.x - a.sum_blocks) * kFillRows;
+  const int r0 = (blockIdx.x - a.sum_blocks) * a.fill_rows;
   if (threadIdx.x < kFillRows) flag[threadIdx.x] = fill ? 0 : -1;
   I id[PER];
 #pragma unroll
@@ -499,11 +501,11 @@ __global__ void __launch_bounds__(256) embedding_direct_kernel(EmbeddingSum a, l
     const int t = 256 * u + threadIdx.x;
     const int k = t < a.tokens ? table_row(id[u], first, a.rows) : a.rows;
     if (!fill) key[t] = k;
-    else if (k >= r0 && k < r0 + kFillRows && k < a.rows) flag[k - r0] = 1;
+    else if (k >= r0 && k < r0 + a.fill_rows && k < a.rows) flag[k - r0] = 1;
   }
   __syncthreads();
   if (fill) {
-    for (int i = w; i < kFillRows && r0 + i < a.rows; i += 4)
+    for (int i = w; i < a.fill_rows && r0 + i < a.rows; i += 4)
       if (!flag[i]) clear_row<PAST>(a.out + (size_t)(r0 + i) * a.hidden, a.hidden, lane);
     return;
   }
@@ -598,7 +600,9 @@ static hipError_t bwd_t(EmbeddingSum a, long long first, const void* ids, const 
                         hipStream_t s) {
   const long long slabs = (a.hidden + kSlab - 1) / kSlab;
   const bool past = (size_t)a.rows * a.hidden * sizeof(float) >= kStreamBytes;
-  const long long fill = a.accumulate ? 0 : ((long long)a.rows + kFillRows - 1) / kFillRows;
+  // four rows or more, at most 16, of about kFillBytes together
+  a.fill_rows = std::min(kFillRows, std::max(4, (int)(kFillBytes / (a.hidden * sizeof(float)))));
+  const long long fill = a.accumulate ? 0 : ((long long)a.rows + a.fill_rows - 1) / a.fill_rows;
   if (a.tokens <= kDirect) {
     // 512 columns a workgroup, more where that makes over 2048 workgroups, each of which reads
     // all ids.
