@@ -517,7 +517,8 @@ int merak_rope_table(int positions, int rope_dim, double theta, float* table, vo
  *   table      [table_rows, rope_dim / 2, 2] as above; ignored if rope_dim = 0
  *   positions  [tokens], or NULL: token t is at t % seq_len (seq_len at most
  *              table_rows; ignored otherwise).  A position outside the table
- *              makes the token's rotated features NaN.
+ *              makes the token's rotated features NaN (and, in the gradient, its
+ *              heads and the gains' sums).
  * head_dim a multiple of 8, at most 256 (else MERAK_ERR_UNSUPPORTED); rope_dim a
  * multiple of 16, at most head_dim; at most 4096 heads of a kind; eps > 0. */
 int merak_qk_norm_rope_fwd(int dtype, int tokens, int q_heads, int kv_heads, int head_dim, int rope_dim,

@@ -22,7 +22,7 @@ struct Span {
 
 int check_apart(std::initializer_list<Span> written, std::initializer_list<Span> read) {
   auto meet = [](const Span& a, const Span& b) {
-    return a.p && b.p && (uintptr_t)a.p < (uintptr_t)b.p + b.bytes && (uintptr_t)b.p < (uintptr_t)a.p + a.bytes;
+    return a.p && b.p && a.bytes && b.bytes && (uintptr_t)a.p < (uintptr_t)b.p + b.bytes && (uintptr_t)b.p < (uintptr_t)a.p + a.bytes;
   };
   for (const Span* a = written.begin(); a != written.end(); ++a) {
     for (const Span* b = written.begin(); b != a; ++b)
