@@ -304,30 +304,29 @@ __global__ void __launch_bounds__(WM * WN * 64) act8_dw_kernel(DwArgs p) {
   };
   auto nothing = [](int) {};
 
+  // Both buffers' loads go out before the first wait.
+  la.issue(dy_rsrc(0), smem, wave);
+  la.issue(dy_rsrc(1), smem + STAGE, wave);
   if constexpr (CODES) {
 #pragma unroll
     for (int u = 0; u < LB; ++u) load_codes(now, 0, u);
-    la.issue(dy_rsrc(0), smem, wave);
+#pragma unroll
+    for (int u = 0; u < LB; ++u) load_codes(next, 1, u);
 #pragma unroll
     for (int u = 0; u < LB; ++u) {
       write_codes(smem, u, 0);
       write_codes(smem, u, 1);
     }
-#pragma unroll
-    for (int u = 0; u < LB; ++u) load_codes(next, 1, u);
   } else {
-    la.issue(dy_rsrc(0), smem, wave);
     lb.issue(x_rsrc(0), smem + A_BYTES, wave);
+    lb.issue(x_rsrc(1), smem + STAGE + A_BYTES, wave);
   }
   wait_vm_barrier<0>();
   if constexpr (CODES) {
     now = next;
 #pragma unroll
     for (int u = 0; u < LB; ++u) load_codes(next, 2, u);
-  } else {
-    lb.issue(x_rsrc(1), smem + STAGE + A_BYTES, wave);
   }
-  la.issue(dy_rsrc(1), smem + STAGE, wave);
 #pragma unroll
   for (int j = 0; j < TN; ++j) b0[j] = fb.read(smem + A_BYTES, wn * WTN + j * 32, 0);
 #pragma unroll

@@ -22,7 +22,8 @@ struct Span {
 
 int check_apart(std::initializer_list<Span> written, std::initializer_list<Span> read) {
   auto meet = [](const Span& a, const Span& b) {
-    return a.p && b.p && a.bytes && b.bytes && (uintptr_t)a.p < (uintptr_t)b.p + b.bytes && (uintptr_t)b.p < (uintptr_t)a.p + a.bytes;
+    const uintptr_t p = (uintptr_t)a.p, q = (uintptr_t)b.p;
+    return p && q && a.bytes && b.bytes && p < q + b.bytes && q < p + a.bytes;
   };
   for (const Span* a = written.begin(); a != written.end(); ++a) {
     for (const Span* b = written.begin(); b != a; ++b)
