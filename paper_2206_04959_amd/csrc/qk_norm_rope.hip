@@ -25,6 +25,10 @@
 //     one bit;
 //   any other head, or any other number of rotated features: one chunk a lane, pairs
 //     anywhere in the group.
+// In bf16, values copied: 32768 tokens of 20 + 20 heads of 96 163 us (4.6 TB/s; a large copy
+// has 4.8), 16384 tokens of 12 + 12 of 128 61 (4.9), of 80 50 (3.8: 6 of 16 lanes idle);
+// gradients of 16384 tokens: 25 + 25 heads of 64 86 us (4.9), 12 + 12 of 128 82 (4.9), of
+// 96 72 (4.2: three waves a SIMD).
 #include <algorithm>
 #include <cmath>
 
