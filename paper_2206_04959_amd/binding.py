@@ -395,6 +395,16 @@ def attention_bwd(qkv, o, lse, dout, dqkv, delta, batch, seq, heads, head_dim, s
 # ---------------------------------------------------------------------------
 
 I32, I64 = 0, 1
+_torch = None
+
+
+def _load_torch():
+    """torch, imported by the first call that needs it (an import statement in every function
+    costs a short call a tenth of its time)."""
+    global _torch
+    import torch
+    _torch = torch
+    return torch
 
 
 def _call(what: str, fn: str, args, stream, names: str, *tensors) -> None:
@@ -402,7 +412,7 @@ def _call(what: str, fn: str, args, stream, names: str, *tensors) -> None:
     are dense and on one GPU.  The call goes to that GPU: its current stream unless `stream`
     names another one of its streams.  (A short call's time is mostly the host's, so the checks
     are kept to a tenth of a microsecond or two each.)"""
-    import torch
+    torch = _torch or _load_torch()
     index = tensors[0].get_device()
     for t in tensors:
         if t is not None and (t.get_device() != index or not t.is_contiguous()):
@@ -420,7 +430,7 @@ def _call(what: str, fn: str, args, stream, names: str, *tensors) -> None:
     else:
         handle = stream.cuda_stream
     entry = getattr(_lib or lib(), fn)
-    if torch.cuda.current_device() == index:
+    if torch._C._cuda_getDevice() == index:
         status = entry(*args, handle)
     else:
         with torch.cuda.device(index):
@@ -431,7 +441,7 @@ def _call(what: str, fn: str, args, stream, names: str, *tensors) -> None:
 
 def _element(what: str, *tensors) -> int:
     """BF16 or FP32 of tensors that share that type."""
-    import torch
+    torch = _torch or _load_torch()
     dt = tensors[0].dtype
     for t in tensors:
         if t.dtype is not dt:
@@ -460,7 +470,7 @@ def _scratch(what: str, scratch, nbytes: int):
 
 
 def _id_type(what: str, ids) -> int:
-    import torch
+    torch = _torch or _load_torch()
     if ids.dtype is torch.int64:
         return I64
     if ids.dtype is torch.int32:
@@ -491,7 +501,7 @@ def embedding_scratch_bytes(tokens: int, hidden: int) -> int:
 def embedding_bwd(ids, dy, dtable, scratch=None, scale=1.0, first_id=0, accumulate=False, stream=None) -> None:
     """dtable[v] (= or +=) scale * sum of dy[t] over the tokens t with ids[t] - first_id = v;
     dtable fp32 [rows, hidden], scratch of embedding_scratch_bytes(tokens, hidden) bytes."""
-    import torch
+    torch = _torch or _load_torch()
     what = "embedding_bwd"
     dt, it = _element(what, dy), _id_type(what, ids)
     if dtable.dim() != 2 or dtable.dtype is not torch.float32:
@@ -515,7 +525,7 @@ def rope_table(table, theta=10000.0, stream=None) -> None:
 
 def _table(what: str, table):
     """(positions, rotated features) of a rotation table."""
-    import torch
+    torch = _torch or _load_torch()
     if table.dim() != 3 or table.shape[2] != 2 or table.dtype is not torch.float32:
         raise ValueError(f"{what}: table is fp32 [positions, rope_dim / 2, 2]")
     return table.shape[0], 2 * table.shape[1]
@@ -523,7 +533,7 @@ def _table(what: str, table):
 
 def _qk_args(what, qkv, q_gamma, k_gamma, table, positions, q_heads, kv_heads, seq_len, interleaved, eps):
     """(leading arguments, table and position arguments) of the query/key norm calls."""
-    import torch
+    torch = _torch or _load_torch()
     dt = _element(what, qkv, q_gamma, k_gamma)
     d = q_gamma.numel()
     if k_gamma.numel() != d:
@@ -573,7 +583,7 @@ def qk_norm_rope_bwd(dout, qkv, q_gamma, k_gamma, table, dqkv, dq_gamma, dk_gamm
                      stream=None) -> None:
     """Gradient of qk_norm_rope_fwd from the raw qkv: dqkv (dout itself or another tensor) and
     the gains' fp32 gradients, written or added."""
-    import torch
+    torch = _torch or _load_torch()
     what = "qk_norm_rope_bwd"
     head, tail = _qk_args(what, qkv, q_gamma, k_gamma, table, positions, q_heads, kv_heads, seq_len, interleaved, eps)
     n = qkv.numel()
@@ -593,7 +603,7 @@ def qk_norm_rope_bwd(dout, qkv, q_gamma, k_gamma, table, dqkv, dq_gamma, dk_gamm
 
 def _act8(what, q, scales):
     """(rows, cols) of a checkpoint."""
-    import torch
+    torch = _torch or _load_torch()
     if q.dtype is not torch.uint8 or scales.dtype is not torch.uint8:
         raise ValueError(f"{what}: q and scales are uint8")
     cols, n = q.shape[-1], q.numel()
@@ -644,7 +654,7 @@ def act8_gelu_bwd(dg, q, scales, du, g=None, stream=None) -> None:
 @functools.lru_cache(maxsize=256)
 def act8_gemm_dw_scratch_bytes(dtype, tokens: int, n_out: int, n_in: int) -> int:
     """dtype: the torch type of dy."""
-    import torch
+    torch = _torch or _load_torch()
     dt = BF16 if dtype == torch.bfloat16 else FP32
     return int(lib().merak_act8_gemm_dw_scratch_bytes(dt, tokens, n_out, n_in))
 
@@ -652,7 +662,7 @@ def act8_gemm_dw_scratch_bytes(dtype, tokens: int, n_out: int, n_in: int) -> int
 def act8_gemm_dw(dy, q, scales, dw, scratch=None, accumulate=False, stream=None) -> None:
     """dw [n_out, n_in] fp32 (= or +=) dy^T X, with dy [.., n_out] and X [.., n_in] from its
     checkpoint; scratch of act8_gemm_dw_scratch_bytes(dy.dtype, tokens, n_out, n_in) bytes."""
-    import torch
+    torch = _torch or _load_torch()
     what = "act8_gemm_dw"
     dt = _element(what, dy)
     tokens, n_in = _act8(what, q, scales)
