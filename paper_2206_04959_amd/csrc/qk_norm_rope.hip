@@ -339,7 +339,7 @@ __global__ void __launch_bounds__(256) qk_bwd_kernel(QkArgs a, QkGrid grid, cons
 }
 
 // Gain gradients from the workgroups' sums, 16 columns of one gain a workgroup: 64
-// threads a column take every 64th sum (8 in flight), and are added in order.  (One
+// threads a column take every 64th sum (16 in flight), and are added in order.  (One
 // column a lane with 16 waves, the way the other column sums end, took 17 us for
 // 1024 sums.)
 __global__ void __launch_bounds__(1024) qk_gain_kernel(int d, QkGrid grid, const float* __restrict__ part,
@@ -353,8 +353,14 @@ __global__ void __launch_bounds__(1024) qk_gain_kernel(int d, QkGrid grid, const
   const float* p = part + (size_t)(keys ? grid.q : 0) * d;
   float s = 0.0f;
   if (col < d) {
-#pragma unroll 8
-    for (int i = slice; i < n; i += 64) s += p[(size_t)i * d + col];
+    constexpr int U = 16;
+    for (int i = slice; i < n; i += 64 * U) {
+      float v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = i + 64 * u < n ? p[(size_t)(i + 64 * u) * d + col] : 0.0f;
+#pragma unroll
+      for (int u = 0; u < U; ++u) s += v[u];
+    }
   }
   red[slice][threadIdx.x & 15] = s;
   __syncthreads();
@@ -452,7 +458,11 @@ struct Bwd {
     // Up to four steps of one workgroup a kind take less than the launch that would add the
     // sums of several: 8 tokens of 6 + 6 heads of 128 14.1 us a call with it, 11.7 without.
     const bool one = heads_blocks(q.tokens, std::max(q.q_heads, q.kv_heads), G) <= 4;
-    if (!one) bwd_blocks(q.tokens, q.q_heads, q.kv_heads, q.head_dim, &bq, &bk);
+    if (!one) {
+      bwd_blocks(q.tokens, q.q_heads, q.kv_heads, q.head_dim, &bq, &bk);
+      bq = (int)std::min<long long>(bq, heads_blocks(q.tokens, q.q_heads, G));  // with 64 heads a workgroup
+      bk = (int)std::min<long long>(bk, heads_blocks(q.tokens, q.kv_heads, G));
+    }
     const long long bv = c.dout != c.out ? copy_blocks(q, sizeof(T)) : 0;
     if (bq + bk + bv > 0x7fffffffLL) return hipErrorInvalidValue;
     hipLaunchKernelGGL((qk_bwd_kernel<T, G, CH, MODE>), dim3((unsigned)(bq + bk + bv)), dim3(256), 0, c.s, qk_args(q),
