@@ -176,7 +176,10 @@ __global__ void __launch_bounds__(256) act8_gelu_bwd_kernel(long long chunks, co
 // Behind the barrier at the end of stage kt's reads its buffer is refilled with
 // stage kt + 2, piece by piece between the MFMAs too: dY's loads and the loads of the
 // codes of stage kt + 3 in the last sub-step, the conversions in the next two.  Every
-// wait is for the loads of a whole stage ago.
+// wait is for the loads of a whole stage ago.  A workgroup alone on its CU has nothing
+// else to run meanwhile and waits for memory once a stage; it has eight waves and, from
+// eight times kBK tokens on, stages of twice the length (H = 2): 4096 x 2048 x 2048 56.5 us
+// with four waves and one kBK a stage, 48.8 so; 64 x 1024 x 1024 5.3, and 6.3 with H = 2.
 // Buffers are addressed from each stage's first token, so operands may be of any
 // size; tokens past the end read as zeros.
 // ---------------------------------------------------------------------------
@@ -201,13 +204,14 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t stage_buffer(const void* p, in
   return operand_rsrc(p, rows > 0 ? (uint32_t)(min(rows, kBK) * ld) : 0u);
 }
 
-template <int BM, int BN, int WM, int WN, bool CODES>
+template <int BM, int BN, int WM, int WN, bool CODES, int H>
 __global__ void __launch_bounds__(WM * WN * 64) act8_dw_kernel(DwArgs p) {
   constexpr int NW = WM * WN, NT = NW * 64;
   constexpr int WTM = BM / WM, WTN = BN / WN, TM = WTM / 32, TN = WTN / 32;
-  constexpr int A_BYTES = BM * 128, STAGE = (BM + BN) * 128;
-  constexpr int LA = BM / 8 / NW;         // dY loads of a wave and stage
-  // X: runs of 16 codes of a thread and stage, or loads of a wave
+  // A stage is H times kBK tokens, each kBK with its own part of the LDS buffer.
+  constexpr int A_BYTES = BM * 128, PART = (BM + BN) * 128, STAGE = H * PART;
+  constexpr int LA = BM / 8 / NW;         // dY loads of a wave and part
+  // X: runs of 16 codes of a thread and part, or loads of a wave
   constexpr int LB = CODES ? BN * kBK / 16 / NT : BN / 8 / NW;
   constexpr int RPR = BN / 16, CPR = BN / 8;
   static_assert(!CODES || (LB * NT * 16 == BN * kBK && CPR % 16 == 0), "whole runs, slots in pairs");
@@ -227,7 +231,7 @@ __global__ void __launch_bounds__(WM * WN * 64) act8_dw_kernel(DwArgs p) {
 
   const int k0 = split * p.per_split;
   const int rows = min(p.per_split, p.tokens - k0);
-  const int KT = (rows + kBK - 1) / kBK;
+  const int KT = (rows + H * kBK - 1) / (H * kBK);
   const size_t lda = (size_t)p.n_out * 2, ldx = (size_t)p.n_in * 2, ldq = p.n_in, lds = p.n_in / kScaleBlock;
   const char* pa = reinterpret_cast<const char*>(p.dy) + (size_t)k0 * lda;
   const char* px = reinterpret_cast<const char*>(p.x) + (size_t)k0 * ldx;
@@ -267,23 +271,27 @@ __global__ void __launch_bounds__(WM * WN * 64) act8_dw_kernel(DwArgs p) {
 
   // The codes of the next stage to convert, and of the one after it (on their way).
   struct Codes {
-    u32x4_t q[LB];
-    uint32_t s[LB];
+    u32x4_t q[H][LB];
+    uint32_t s[H][LB];
   } now, next;
   bf16x8_t a0[TM], a1[TM], b0[TN], b1[TN];  // two fragment sets
-  auto load_codes = [&](Codes& c, int kt, int u) {  // run u of stage kt
-    const int left = rows - kt * kBK;
-    const __amdgpu_buffer_rsrc_t rq = stage_buffer(pq + (size_t)kt * kBK * ldq, left, ldq);
-    const __amdgpu_buffer_rsrc_t rc = stage_buffer(ps + (size_t)kt * kBK * lds, left, lds);
-    c.q[u] = __builtin_amdgcn_raw_buffer_load_b128(rq, qoff[u], 0, 0);
-    c.s[u] = __builtin_amdgcn_raw_buffer_load_b8(rc, soff[u], 0, 0);
+  auto load_codes = [&](Codes& c, int kt, int h, int u) {  // run u of part h of stage kt
+    const int k = kt * H + h, left = rows - k * kBK;
+    const __amdgpu_buffer_rsrc_t rq = stage_buffer(pq + (size_t)k * kBK * ldq, left, ldq);
+    const __amdgpu_buffer_rsrc_t rc = stage_buffer(ps + (size_t)k * kBK * lds, left, lds);
+    c.q[h][u] = __builtin_amdgcn_raw_buffer_load_b128(rq, qoff[u], 0, 0);
+    c.s[h][u] = __builtin_amdgcn_raw_buffer_load_b8(rc, soff[u], 0, 0);
   };
-  auto write_codes = [&](char* st, int u, int half) {  // half a run; its two chunks are neighbours in LDS
-    *reinterpret_cast<u32x4_t*>(st + w0[u] + 16 * half) =
-        decode8_bf16(now.q[u][2 * half], now.q[u][2 * half + 1], scale_of(now.s[u]));
+  // Half run i of the stage in `now`, counted through its parts; a run's halves are neighbours
+  // in LDS.
+  auto write_codes = [&](char* st, int i) {
+    const int h = i / (2 * LB), u = i % (2 * LB) / 2, half = i % 2;
+    *reinterpret_cast<u32x4_t*>(st + h * PART + w0[u] + 16 * half) =
+        decode8_bf16(now.q[h][u][2 * half], now.q[h][u][2 * half + 1], scale_of(now.s[h][u]));
   };
-  auto x_rsrc = [&](int kt) { return stage_rsrc(px + (size_t)kt * kBK * ldx, rows - kt * kBK, ldx); };
-  auto dy_rsrc = [&](int kt) { return stage_rsrc(pa + (size_t)kt * kBK * lda, rows - kt * kBK, lda); };
+  // Tokens kBK k on of the split.
+  auto x_rsrc = [&](int k) { return stage_rsrc(px + (size_t)k * kBK * ldx, rows - k * kBK, ldx); };
+  auto dy_rsrc = [&](int k) { return stage_rsrc(pa + (size_t)k * kBK * lda, rows - k * kBK, lda); };
   // A sub-step: the MFMAs of set c, each followed by the read of one fragment of (st, ks)
   // into set n and by piece(u), in that order.
   constexpr int NMF = TM * TN;
@@ -305,30 +313,27 @@ __global__ void __launch_bounds__(WM * WN * 64) act8_dw_kernel(DwArgs p) {
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  auto nothing = [](int) {};
 
   // Both buffers' loads go out before the first wait.
-  la.issue(dy_rsrc(0), smem, wave);
-  la.issue(dy_rsrc(1), smem + STAGE, wave);
+#pragma unroll
+  for (int k = 0; k < 2 * H; ++k) {
+    la.issue(dy_rsrc(k), smem + k * PART, wave);
+    if constexpr (!CODES) lb.issue(x_rsrc(k), smem + k * PART + A_BYTES, wave);
+  }
+  auto load_stage = [&](Codes& c, int kt) {
+#pragma unroll
+    for (int i = 0; i < H * LB; ++i) load_codes(c, kt, i / LB, i % LB);
+  };
   if constexpr (CODES) {
+    load_stage(now, 0);
+    load_stage(next, 1);
 #pragma unroll
-    for (int u = 0; u < LB; ++u) load_codes(now, 0, u);
-#pragma unroll
-    for (int u = 0; u < LB; ++u) load_codes(next, 1, u);
-#pragma unroll
-    for (int u = 0; u < LB; ++u) {
-      write_codes(smem, u, 0);
-      write_codes(smem, u, 1);
-    }
-  } else {
-    lb.issue(x_rsrc(0), smem + A_BYTES, wave);
-    lb.issue(x_rsrc(1), smem + STAGE + A_BYTES, wave);
+    for (int i = 0; i < 2 * LB * H; ++i) write_codes(smem, i);
   }
   wait_vm_barrier<0>();
   if constexpr (CODES) {
     now = next;
-#pragma unroll
-    for (int u = 0; u < LB; ++u) load_codes(next, 2, u);
+    load_stage(next, 2);
   }
 #pragma unroll
   for (int j = 0; j < TN; ++j) b0[j] = fb.read(smem + A_BYTES, wn * WTN + j * 32, 0);
@@ -337,34 +342,39 @@ __global__ void __launch_bounds__(WM * WN * 64) act8_dw_kernel(DwArgs p) {
   __builtin_amdgcn_sched_barrier(0);
 
   // Past the last stage the loads find empty buffers: they fetch nothing and write zeros.
-  constexpr int CONV = 2 * LB;  // half runs to convert, half of them in each of two sub-steps
   for (int kt = 0; kt < KT; ++kt) {
     char* st = smem + (kt & 1) * STAGE;
     char* other = smem + ((kt + 1) & 1) * STAGE;
-    auto convert = [&](int first, int u) {
+    // LB half runs of the next stage are converted in each of the first 2 H sub-steps.
+    auto convert = [&](int i, int u) {
       if constexpr (CODES) {
-        constexpr int EVERY = NMF / (CONV / 2);
-        static_assert(NMF % (CONV / 2) == 0, "conversions spread evenly over the MFMAs");
-        if (u % EVERY == 0) write_codes(other, (first + u / EVERY) / 2, (first + u / EVERY) % 2);
+        constexpr int EVERY = NMF / LB;
+        static_assert(NMF % LB == 0, "conversions spread evenly over the MFMAs");
+        if (i <= 2 * H && u % EVERY == 0) write_codes(other, (i - 1) * LB + u / EVERY);
       }
     };
-    step(st, 1, a1, b1, a0, b0, [&](int u) { convert(0, u); });
-    step(st, 2, a0, b0, a1, b1, [&](int u) { convert(CONV / 2, u); });
-    step(st, 3, a1, b1, a0, b0, nothing);
+#pragma unroll
+    for (int i = 1; i < 4 * H; ++i) {
+      if (i & 1) step(st + i / 4 * PART, i % 4, a1, b1, a0, b0, [&](int u) { convert(i, u); });
+      else step(st + i / 4 * PART, i % 4, a0, b0, a1, b1, [&](int u) { convert(i, u); });
+    }
     wait_vm_barrier<0>();  // stage kt + 1 is in LDS, `next` is there, and all have read stage kt
     if constexpr (CODES) now = next;
-    const i32x4_t ra = dy_rsrc(kt + 2), rx = x_rsrc(CODES ? 0 : kt + 2);
-    constexpr int NP = LA + LB, PER = (NP + NMF - 1) / NMF;
+    i32x4_t ra[H], rx[H];
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      ra[h] = dy_rsrc((kt + 2) * H + h);
+      rx[h] = x_rsrc(CODES ? 0 : (kt + 2) * H + h);
+    }
+    constexpr int NP = H * (LA + LB), PER = (NP + NMF - 1) / NMF;
     step(other, 0, a0, b0, a1, b1, [&](int u) {
 #pragma unroll
       for (int e = 0; e < PER; ++e) {
-        const int c = u * PER + e;
-        if (c < LA) {
-          la.issue_one(ra, st, wave, c);
-        } else if (c < NP) {
-          if constexpr (CODES) load_codes(next, kt + 3, c - LA);
-          else lb.issue_one(rx, st + A_BYTES, wave, c - LA);
-        }
+        const int c = u * PER + e, h = c / (LA + LB), r = c % (LA + LB);
+        if (c >= NP) continue;
+        if (r < LA) la.issue_one(ra[h], st + h * PART, wave, r);
+        else if constexpr (CODES) load_codes(next, kt + 3, h, r - LA);
+        else lb.issue_one(rx[h], st + h * PART + A_BYTES, wave, r - LA);
       }
     });
   }
@@ -619,7 +629,7 @@ struct DwPlan {
 
 // Restoring X reads and writes it once more (3 bytes a value, and a launch); it saves
 // every one of the n_out / bm tiles in its column the conversion, about 6e-10 us a
-// product.  Measured, restored and converted: 16384 x 7680 x 1920 (tokens x outputs x
+// product.  Measured (four waves a workgroup), restored and converted: 16384 x 7680 x 1920 (tokens x outputs x
 // inputs) 429 and 540 us, 2048 x 4096 x 1024 33 and 35; 2048 x 1024 x 1024 25 and 22,
 // 333 x 1920 x 640 11 and 9.
 static bool dw_restore(double tokens, double n_out, double n_in) {
@@ -629,16 +639,16 @@ static bool dw_restore(double tokens, double n_out, double n_in) {
 // Tile and splits by estimated time: whole rounds of workgroups over the chip, each as
 // long as its stages (and about four more for its start and end); splits add their
 // sums' way through memory and a launch.  us a stage, measured: 256 x 256 1.6, 256 x 192
-// 1.16 (one workgroup a CU); 128 x 128 0.65 alone on its CU, 0.92 for two; converting adds a
+// 1.16 (one workgroup a CU); 128 x 128 0.6 alone on its CU, 0.92 for two; converting adds a
 // seventh.  What it decides, with the other choice's time: 8192 x 6400 x 1600 256 x 192
 // 161 us, 256 x 256 170, 128 x 128 201; 16384 x 7680 x 1920 256 x 256 429, 128 x 128 499;
-// 4096 x 2048 x 2048 128 x 128 in two splits 53, in one 58.
+// 4096 x 2048 x 2048 128 x 128 in one split 49, in two 53.
 static DwPlan dw_plan(int tokens, int n_out, int n_in) {
   struct Tile {
     int bm, bn, resident;
     double alone, full;
   };
-  static const Tile tiles[] = {{128, 128, 2, 0.65, 0.92}, {256, 256, 1, 1.6, 1.6}, {256, 192, 1, 1.16, 1.16}};
+  static const Tile tiles[] = {{128, 128, 2, 0.6, 0.92}, {256, 256, 1, 1.6, 1.6}, {256, 192, 1, 1.16, 1.16}};
   DwPlan best{};
   best.restore = dw_restore(tokens, n_out, n_in);
   const int stages = (tokens + kBK - 1) / kBK;
@@ -696,11 +706,11 @@ size_t act8_gemm_dw_scratch_bytes(int dtype, int tokens, int n_out, int n_in) {
   return dw_values_bytes(p, tokens, n_in) + (p.splits > 1 ? (size_t)p.splits * n_out * n_in * sizeof(float) : 0);
 }
 
-template <int BM, int BN, int WM, int WN, bool CODES>
+template <int BM, int BN, int WM, int WN, bool CODES, int H>
 static hipError_t run_dw(const DwArgs& a, int splits, hipStream_t s) {
-  constexpr size_t lds = 2 * (BM + BN) * 128;
+  constexpr size_t lds = 2 * H * (BM + BN) * 128;
   static_assert(lds <= 160 * 1024, "LDS budget");
-  auto kern = act8_dw_kernel<BM, BN, WM, WN, CODES>;
+  auto kern = act8_dw_kernel<BM, BN, WM, WN, CODES, H>;
   static std::atomic<uint64_t> lds_set{0};
   const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(kern), lds, lds_set);
   if (e != hipSuccess) return e;
@@ -711,10 +721,16 @@ static hipError_t run_dw(const DwArgs& a, int splits, hipStream_t s) {
 }
 
 static hipError_t run_dw_plan(const DwPlan& p, const DwArgs& a, hipStream_t s) {
-  if (!p.restore) return run_dw<128, 128, 2, 2, true>(a, p.splits, s);
-  if (p.bm == 128) return run_dw<128, 128, 2, 2, false>(a, p.splits, s);
-  if (p.bn == 192) return run_dw<256, 192, 4, 2, false>(a, p.splits, s);
-  return run_dw<256, 256, 2, 4, false>(a, p.splits, s);
+  if (p.bm == 128) {
+    const bool alone = (long long)p.tiles * p.splits <= 256, longer = p.per_split >= 8 * kBK;
+    if (p.restore)  // (alone, it has more than eight kBK: dw_restore)
+      return alone ? run_dw<128, 128, 2, 4, false, 2>(a, p.splits, s)
+                   : run_dw<128, 128, 2, 2, false, 1>(a, p.splits, s);
+    if (!alone) return run_dw<128, 128, 2, 2, true, 1>(a, p.splits, s);
+    return longer ? run_dw<128, 128, 2, 4, true, 2>(a, p.splits, s) : run_dw<128, 128, 2, 4, true, 1>(a, p.splits, s);
+  }
+  if (p.bn == 192) return run_dw<256, 192, 4, 2, false, 1>(a, p.splits, s);
+  return run_dw<256, 256, 2, 4, false, 1>(a, p.splits, s);
 }
 
 hipError_t launch_act8_gemm_dw(int dtype, int tokens, int n_out, int n_in, const void* dy, const uint8_t* q,
