@@ -395,6 +395,7 @@ def attention_bwd(qkv, o, lse, dout, dqkv, delta, batch, seq, heads, head_dim, s
 # ---------------------------------------------------------------------------
 
 I32, I64 = 0, 1
+_INT = 0x7fffffff  # the largest size that fits the entry points' integers: ctypes cuts others to 32 bits
 _torch = None
 
 
@@ -453,10 +454,15 @@ def _element(what: str, *tensors) -> int:
     raise ValueError(f"{what}: element type {dt}: bf16 or fp32")
 
 
-def _count(what: str, ids) -> int:
+def _too_large(what: str, **sizes) -> None:
+    raise ValueError(f"{what}: too large: " + ", ".join(f"{name} {value}" for name, value in sizes.items()))
+
+
+def _count(what: str, ids, rows: int, hidden: int, first_id: int) -> int:
+    """How many ids there are; all sizes fit the entry point's integers."""
     n = ids.numel()
-    if n > 1 << 30:  # (as an argument of the entry point a larger one would wrap)
-        raise ValueError(f"{what}: {n} ids")
+    if (n | rows | hidden) > _INT or not -1 << 63 <= first_id < 1 << 63:
+        _too_large(what, ids=n, rows=rows, hidden=hidden, first_id=first_id)
     return n
 
 
@@ -486,7 +492,7 @@ def embedding_fwd(ids, table, y, scale=1.0, first_id=0, stream=None) -> None:
     if table.dim() != 2:
         raise ValueError(f"{what}: table is [rows, hidden]")
     rows, hidden = table.shape
-    tokens = _count(what, ids)
+    tokens = _count(what, ids, rows, hidden, first_id)
     if y.numel() != tokens * hidden or y.shape[-1] != hidden:
         raise ValueError(f"{what}: y is one row for each id")
     _call(what, "merak_embedding_fwd", (dt, it, tokens, hidden, rows, first_id, scale, ids.data_ptr(),
@@ -495,6 +501,8 @@ def embedding_fwd(ids, table, y, scale=1.0, first_id=0, stream=None) -> None:
 
 @functools.lru_cache(maxsize=256)
 def embedding_scratch_bytes(tokens: int, hidden: int) -> int:
+    if max(abs(tokens), abs(hidden)) > _INT:
+        _too_large("embedding_scratch_bytes", tokens=tokens, hidden=hidden)
     return int(lib().merak_embedding_scratch_bytes(tokens, hidden))
 
 
@@ -507,7 +515,7 @@ def embedding_bwd(ids, dy, dtable, scratch=None, scale=1.0, first_id=0, accumula
     if dtable.dim() != 2 or dtable.dtype is not torch.float32:
         raise ValueError(f"{what}: dtable is fp32 [rows, hidden]")
     rows, hidden = dtable.shape
-    tokens = _count(what, ids)
+    tokens = _count(what, ids, rows, hidden, first_id)
     if dy.numel() != tokens * hidden or dy.shape[-1] != hidden:
         raise ValueError(f"{what}: dy is one row for each id")
     sp = _scratch(what, scratch, embedding_scratch_bytes(tokens, hidden))
@@ -528,7 +536,10 @@ def _table(what: str, table):
     torch = _torch or _load_torch()
     if table.dim() != 3 or table.shape[2] != 2 or table.dtype is not torch.float32:
         raise ValueError(f"{what}: table is fp32 [positions, rope_dim / 2, 2]")
-    return table.shape[0], 2 * table.shape[1]
+    positions, rope = table.shape[0], 2 * table.shape[1]
+    if (positions | rope) > _INT:
+        _too_large(what, positions=positions, rope_dim=rope)
+    return positions, rope
 
 
 def _qk_args(what, qkv, q_gamma, k_gamma, table, positions, q_heads, kv_heads, seq_len, interleaved, eps):
@@ -542,8 +553,8 @@ def _qk_args(what, qkv, q_gamma, k_gamma, table, positions, q_heads, kv_heads, s
     if q_heads <= 0 or kv_heads <= 0 or row <= 0 or n % row != 0:
         raise ValueError(f"{what}: qkv is [tokens, q_heads + 2 * kv_heads, head_dim]")
     tokens = n // row
-    if tokens > 0x7fffffff:
-        raise ValueError(f"{what}: {tokens} tokens")
+    if (tokens | q_heads | kv_heads | d) > _INT:
+        _too_large(what, tokens=tokens, q_heads=q_heads, kv_heads=kv_heads, head_dim=d)
     if table is None:
         return (dt, tokens, q_heads, kv_heads, d, 0, int(interleaved), eps), (None, 0, None, 0)
     rows, rope = _table(what, table)
@@ -554,6 +565,8 @@ def _qk_args(what, qkv, q_gamma, k_gamma, table, positions, q_heads, kv_heads, s
     else:
         if seq_len is None:
             raise ValueError(f"{what}: positions or seq_len needed")
+        if not -_INT <= seq_len <= _INT:
+            _too_large(what, seq_len=seq_len)
         place = None
     return ((dt, tokens, q_heads, kv_heads, d, rope, int(interleaved), eps),
             (table.data_ptr(), rows, place, seq_len or 0))
@@ -575,6 +588,8 @@ def qk_norm_rope_fwd(qkv, q_gamma, k_gamma, table, out, q_heads, kv_heads, posit
 
 @functools.lru_cache(maxsize=256)
 def qk_norm_rope_scratch_elems(tokens: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
+    if max(map(abs, (tokens, q_heads, kv_heads, head_dim))) > _INT:
+        _too_large("qk_norm_rope_scratch_elems", tokens=tokens, q_heads=q_heads, kv_heads=kv_heads, head_dim=head_dim)
     return int(lib().merak_qk_norm_rope_scratch_elems(tokens, q_heads, kv_heads, head_dim))
 
 
@@ -609,9 +624,10 @@ def _act8(what, q, scales):
     cols, n = q.shape[-1], q.numel()
     if cols <= 0 or cols % 32 or scales.shape[-1] * 32 != cols or scales.numel() * 32 != n:
         raise ValueError(f"{what}: q is [rows, cols] and scales [rows, cols / 32], cols a multiple of 32")
-    if n // cols > 0x7fffffff:
-        raise ValueError(f"{what}: {n // cols} rows")
-    return n // cols, cols
+    rows = n // cols
+    if (rows | cols) > _INT:
+        _too_large(what, rows=rows, cols=cols)
+    return rows, cols
 
 
 def _like(what, q, names, *tensors) -> None:
@@ -655,6 +671,8 @@ def act8_gelu_bwd(dg, q, scales, du, g=None, stream=None) -> None:
 def act8_gemm_dw_scratch_bytes(dtype, tokens: int, n_out: int, n_in: int) -> int:
     """dtype: the torch type of dy."""
     torch = _torch or _load_torch()
+    if max(abs(tokens), abs(n_out), abs(n_in)) > _INT:
+        _too_large("act8_gemm_dw_scratch_bytes", tokens=tokens, n_out=n_out, n_in=n_in)
     dt = BF16 if dtype == torch.bfloat16 else FP32
     return int(lib().merak_act8_gemm_dw_scratch_bytes(dt, tokens, n_out, n_in))
 

@@ -1,0 +1,64 @@
+"""Sizes at and beyond what the operators around the blocks take (no GPU): such a call is
+refused before anything is enqueued, by the status or the error that names the size."""
+import pytest
+
+from paper_2206_04959_amd import binding as B
+
+torch = pytest.importorskip("torch")
+
+BF, U8, F32, I32 = torch.bfloat16, torch.uint8, torch.float32, torch.int32
+WRAP = 2 ** 32 + 64  # 64 in 32 bits
+
+
+def _v(*shape, dtype=BF):
+    """A tensor of any shape without memory behind it."""
+    return torch.empty(shape, dtype=dtype, device="meta")
+
+
+def _qk(**change):
+    a = dict(qkv=_v(4, 6, 64), gq=_v(64), gk=_v(64), table=_v(9, 32, 2, dtype=F32), out=_v(4, 6, 64), q_heads=2,
+             kv_heads=2, seq_len=4, positions=None, **{})
+    a.update(change)
+    return lambda: B.qk_norm_rope_fwd(a["qkv"], a["gq"], a["gk"], a["table"], a["out"], a["q_heads"], a["kv_heads"],
+                                      positions=a["positions"], seq_len=a["seq_len"])
+
+
+# The entry points' integers have 32 bits (first_id: 64), and ctypes cuts larger ones: a table of
+# 2^32 + 64 rows went on as one of 64.
+@pytest.mark.parametrize("call", [
+    lambda: B.embedding_fwd(_v(4, dtype=I32), _v(WRAP, 64), _v(4, 64)),
+    lambda: B.embedding_fwd(_v(1, dtype=I32), _v(9, WRAP), _v(1, WRAP)),
+    lambda: B.embedding_fwd(_v(4, dtype=I32), _v(9, 64), _v(4, 64), first_id=2 ** 64 + 3),
+    lambda: B.embedding_fwd(_v(4, dtype=I32), _v(9, 64), _v(4, 64), first_id=3 - 2 ** 64),
+    lambda: B.embedding_bwd(_v(4, dtype=I32), _v(4, 64), _v(WRAP, 64, dtype=F32)),
+    lambda: B.embedding_bwd(_v(1, dtype=I32), _v(1, WRAP), _v(9, WRAP, dtype=F32)),
+    lambda: B.embedding_bwd(_v(4, dtype=I32), _v(4, 64), _v(9, 64, dtype=F32), first_id=2 ** 64),
+    lambda: B.embedding_scratch_bytes(WRAP, 64),
+    lambda: B.embedding_scratch_bytes(4, WRAP),
+    lambda: B.embedding_scratch_bytes(4 - 2 ** 32, 64),
+    lambda: B.rope_table(_v(WRAP, 32, 2, dtype=F32)),
+    lambda: B.rope_table(_v(9, WRAP // 2, 2, dtype=F32)),
+    _qk(seq_len=2 ** 32 + 4),
+    _qk(seq_len=4 - 2 ** 32),
+    _qk(table=_v(WRAP, 32, 2, dtype=F32)),
+    _qk(table=_v(9, WRAP // 2, 2, dtype=F32)),
+    _qk(qkv=_v(1, WRAP + 4, 64), out=_v(1, WRAP + 4, 64), q_heads=WRAP),
+    _qk(qkv=_v(1, 2 * WRAP + 2, 64), out=_v(1, 2 * WRAP + 2, 64), kv_heads=WRAP),
+    _qk(qkv=_v(1, 6, WRAP), out=_v(1, 6, WRAP), gq=_v(WRAP), gk=_v(WRAP)),
+    lambda: B.qk_norm_rope_scratch_elems(WRAP, 2, 2, 64),
+    lambda: B.qk_norm_rope_scratch_elems(4, WRAP, 2, 64),
+    lambda: B.act8_save(_v(1, WRAP), _v(1, WRAP, dtype=U8), _v(1, WRAP // 32, dtype=U8)),
+    lambda: B.act8_save(_v(WRAP, 64), _v(WRAP, 64, dtype=U8), _v(WRAP, 2, dtype=U8)),
+    lambda: B.act8_gemm_dw(_v(4, WRAP), _v(4, 64, dtype=U8), _v(4, 2, dtype=U8), _v(WRAP, 64, dtype=F32)),
+    lambda: B.act8_gemm_dw_scratch_bytes(BF, WRAP, 64, 64),
+    lambda: B.act8_gemm_dw_scratch_bytes(BF, 4, 64, WRAP),
+])
+def test_binding_refuses_sizes_that_ctypes_would_cut(call):
+    with pytest.raises(ValueError, match="too large"):
+        call()
+
+
+def test_positions_make_seq_len_irrelevant():
+    """A sequence length that positions replace is not looked at (the call ends at the device)."""
+    with pytest.raises(ValueError, match="one GPU"):
+        _qk(positions=_v(4, dtype=I32), seq_len=2 ** 32 + 4)()
