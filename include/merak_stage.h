@@ -482,7 +482,8 @@ typedef enum { MERAK_I32 = 0, MERAK_I64 = 1 } merak_id_type;
  * [tokens, hidden] of dtype.  An id outside first_id .. first_id + table_rows - 1
  * (another rank's, or padding such as -1) gives a row of zeros, so the ranks' y
  * add up to the whole lookup.  hidden % 8 == 0 and at most 2^20; tokens and
- * table_rows at most 2^30; first_id >= 0; scale finite. */
+ * table_rows at most 2^30; first_id >= 0, first_id + table_rows at most 2^63; scale
+ * finite. */
 int merak_embedding_fwd(int dtype, int id_type, int tokens, int hidden, int table_rows, int64_t first_id,
                         float scale, const void* ids, const void* table, void* y, void* stream);
 

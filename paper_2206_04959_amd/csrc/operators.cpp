@@ -47,7 +47,8 @@ int check_embedding(int dtype, int id_type, int tokens, int hidden, int rows, in
   if (id_type != MERAK_I32 && id_type != MERAK_I64) return MERAK_ERR_INVALID_ARG;
   if (tokens <= 0 || hidden <= 0 || rows <= 0 || hidden % 8) return MERAK_ERR_SHAPE;
   if (tokens > kMaxRows || rows > kMaxRows || hidden > (1 << 20)) return MERAK_ERR_SHAPE;
-  if (first < 0 || !std::isfinite(scale)) return MERAK_ERR_INVALID_ARG;
+  // the last row's id is an int64 too: the kernels form id - first in 64 bits
+  if (first < 0 || first > INT64_MAX - (rows - 1) || !std::isfinite(scale)) return MERAK_ERR_INVALID_ARG;
   return MERAK_OK;
 }
 

@@ -62,3 +62,26 @@ def test_positions_make_seq_len_irrelevant():
     """A sequence length that positions replace is not looked at (the call ends at the device)."""
     with pytest.raises(ValueError, match="one GPU"):
         _qk(positions=_v(4, dtype=I32), seq_len=2 ** 32 + 4)()
+
+
+P = [0x1000000 * (i + 1) for i in range(12)]  # addresses far apart; nothing reads them
+INVALID, SHAPE, ALIGN = -1, -2, -4
+LAST = 2 ** 63 - 1  # the largest id
+
+
+def _embedding(first, rows, y=P[2]):
+    L = B.lib()
+    return (L.merak_embedding_fwd(0, 1, 10, 64, rows, first, 1.0, P[0], P[1], y, None),
+            L.merak_embedding_bwd(0, 1, 10, 64, rows, first, 1.0, P[0], P[1], y, 0, None, None))
+
+
+def test_the_tables_last_row_has_an_id():
+    """Rows whose ids would be beyond 2^63 - 1: id - first_id is formed in 64 bits, so the id
+    -2^63 was taken for row 1 of a table that begins at 2^63 - 1."""
+    assert (-2 ** 63 - LAST) % 2 ** 64 == 1
+    for rows in (2, 100, 2 ** 30):
+        assert _embedding(LAST - rows + 2, rows) == (INVALID, INVALID)
+        assert _embedding(LAST, rows) == (INVALID, INVALID)
+        # the next check is reached by tables that end at the last id
+        assert _embedding(LAST - rows + 1, rows, y=P[2] + 4) == (ALIGN, ALIGN)
+    assert _embedding(LAST, 1, y=P[2] + 4) == (ALIGN, ALIGN)
