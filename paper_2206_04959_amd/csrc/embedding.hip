@@ -274,8 +274,8 @@ struct EmbeddingSum {
   float* part;      // [chunks][2][hidden]
   int* split;       // split[0]: how many runs are split, then the chunks in which they begin
   float* out;       // [rows][hidden]
-  int sum_blocks;   // workgroups that sum; the rest clear fill_rows rows each
-  int fill_rows;
+  int sum_blocks;   // workgroups that sum; the rest clear fill_rows rows each, from row0 on
+  int fill_rows, row0;
   int width;        // columns of a workgroup of embedding_direct_kernel, a multiple of kSlab
 };
 
@@ -311,7 +311,7 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(EmbeddingSum a, cons
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if ((int)blockIdx.x >= a.sum_blocks) {
     __shared__ int used[kFillRows];
-    const int r0 = (blockIdx.x - a.sum_blocks) * a.fill_rows;
+    const int r0 = a.row0 + (blockIdx.x - a.sum_blocks) * a.fill_rows;
     static_assert(kFillRows * 16 == 256, "16 lanes look for a row");
     const int r = r0 + (threadIdx.x >> 4);
     const int p = (int)threadIdx.x >> 4 < a.fill_rows ? lower_bound16(a.key, a.tokens, r, lane) : 0;
@@ -495,7 +495,7 @@ __global__ void __launch_bounds__(256) embedding_direct_kernel(EmbeddingSum a, l
   __shared__ int flag[kFillRows];  // rows in use, or the waves' long rows' tokens
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool fill = (int)blockIdx.x >= a.sum_blocks;
-  const int r0 = (blockIdx.x - a.sum_blocks) * a.fill_rows;
+  const int r0 = a.row0 + (blockIdx.x - a.sum_blocks) * a.fill_rows;
   if (threadIdx.x < kFillRows) flag[threadIdx.x] = fill ? 0 : -1;
   I id[PER];
 #pragma unroll
@@ -603,6 +603,23 @@ size_t embedding_scratch_bytes(int tokens, int hidden) {
   return 4 * order_bytes(tokens) + order_bytes(1 + kMaxChunks) + chunks * 2 * hidden * sizeof(float);
 }
 
+// Launch of a kernel whose workgroups sum and clear.  What one launch cannot clear (from 2^28
+// rows of few columns on) further ones do, which sum nothing.
+template <typename... P, typename... A>
+static hipError_t launch_sum_and_clear(void (*kernel)(EmbeddingSum, P...), EmbeddingSum a, hipStream_t s, A... args) {
+  long long left = a.accumulate ? 0 : ((long long)a.rows + a.fill_rows - 1) / a.fill_rows;
+  do {
+    const long long fill = std::min(left, max_groups(256) - a.sum_blocks);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(a.sum_blocks + fill)), dim3(256), 0, s, a, args...);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    a.row0 += (int)fill * a.fill_rows;
+    a.sum_blocks = 0;
+    left -= fill;
+  } while (left > 0);
+  return hipSuccess;
+}
+
 template <typename T, typename I>
 static hipError_t bwd_t(EmbeddingSum a, long long first, const void* ids, const void* dy, char* scratch,
                         hipStream_t s) {
@@ -610,16 +627,14 @@ static hipError_t bwd_t(EmbeddingSum a, long long first, const void* ids, const 
   const bool past = (size_t)a.rows * a.hidden * sizeof(float) >= kStreamBytes;
   // four rows or more, at most 16, of about kFillBytes together
   a.fill_rows = std::min(kFillRows, std::max(4, (int)(kFillBytes / (a.hidden * sizeof(float)))));
-  const long long fill = a.accumulate ? 0 : ((long long)a.rows + a.fill_rows - 1) / a.fill_rows;
   if (a.tokens <= kDirect) {
     // 512 columns a workgroup, more where that makes over 2048 workgroups, each of which reads
     // all ids.
     const long long quads = (a.tokens + 3) / 4, per = (quads * slabs + 2047) / 2048;
     a.width = (int)(per * kSlab);
     a.sum_blocks = (int)(quads * ((slabs + per - 1) / per));
-    hipLaunchKernelGGL((past ? embedding_direct_kernel<T, I, true> : embedding_direct_kernel<T, I, false>),
-                       dim3((unsigned)(a.sum_blocks + fill)), dim3(256), 0, s, a, first, (const I*)ids, (const T*)dy);
-    return hipGetLastError();
+    return launch_sum_and_clear((past ? embedding_direct_kernel<T, I, true> : embedding_direct_kernel<T, I, false>), a,
+                                s, first, (const I*)ids, (const T*)dy);
   }
   const size_t ob = order_bytes(a.tokens);
   int* gkey = (int*)scratch;
@@ -647,9 +662,8 @@ static hipError_t bwd_t(EmbeddingSum a, long long first, const void* ids, const 
   a.part = (float*)(scratch + 4 * ob + order_bytes(1 + kMaxChunks));
   const long long units = (((long long)a.tokens + a.chunk - 1) / a.chunk) * slabs;
   a.sum_blocks = (int)((units + 3) / 4);
-  hipLaunchKernelGGL((past ? embedding_sum_kernel<T, true> : embedding_sum_kernel<T, false>),
-                     dim3((unsigned)(a.sum_blocks + fill)), dim3(256), 0, s, a, (const T*)dy);
-  e = hipGetLastError();
+  e = launch_sum_and_clear((past ? embedding_sum_kernel<T, true> : embedding_sum_kernel<T, false>), a, s,
+                           (const T*)dy);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(embedding_join_kernel, dim3(kJoinBlocks), dim3(64 * kJoinWaves), 0, s, a);
   return hipGetLastError();

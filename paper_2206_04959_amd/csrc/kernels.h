@@ -136,6 +136,10 @@ hipError_t launch_attention_bwd_d128(int B, int S, int H, int G, int mstride, co
 // 43.9 us and 156.8 to 153.5; but 101 MB 23.3 to 22.9 and 63.1 to 69.1.
 constexpr size_t kStreamBytes = (size_t)128 << 20;
 
+// Workgroups of `threads` threads that a launch can have: its threads are counted in 32 bits.
+// (A launch of more reports no error and runs the rest of the count.)
+constexpr long long max_groups(int threads) { return 0xffffffffLL / threads; }
+
 // Element type of token ids.
 enum IdType { ID_I32 = 0, ID_I64 = 1 };
 
