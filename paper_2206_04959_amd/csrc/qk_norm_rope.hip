@@ -55,9 +55,10 @@ struct QkArgs {
   int tokens, q_heads, kv_heads, d;
   int rope;         // rotated features of a head
   int table_rows;
-  int seq_len;      // without positions: token t is at t % seq_len
+  int seq_len;      // without positions: token t of the call is at t % seq_len
+  int first;        // the call's tokens before this launch's
   float eps;
-  const int* positions;
+  const int* positions;  // this launch's
   const float* table;
 };
 
@@ -155,7 +156,7 @@ __device__ __forceinline__ void rotate(const QkArgs& a, int pos, int j, int base
 }
 
 __device__ __forceinline__ int position_of(const QkArgs& a, unsigned t) {
-  return a.positions ? a.positions[t] : (int)(t % (unsigned)a.seq_len);
+  return a.positions ? a.positions[t] : (int)((a.first + t) % (unsigned)a.seq_len);
 }
 
 // Workgroups of a launch: for queries, for keys, for copying values.
@@ -394,8 +395,8 @@ static QkLanes lanes_of(const QkShape& q) {
 
 static long long heads_blocks(long long tokens, int heads, int G) { return (tokens * heads + 256 / G - 1) / (256 / G); }
 
-static long long copy_blocks(const QkShape& q, size_t esz) {
-  const long long chunks = (long long)q.tokens * q.kv_heads * q.head_dim * (long long)esz / 16;
+static long long copy_blocks(long long tokens, const QkShape& q, size_t esz) {
+  const long long chunks = tokens * q.kv_heads * q.head_dim * (long long)esz / 16;
   return (chunks + 256 * kCopyUnroll - 1) / (256 * kCopyUnroll);
 }
 
@@ -425,7 +426,7 @@ hipError_t launch_rope_table(int positions, int rope_dim, double theta, float* t
 
 static QkArgs qk_args(const QkShape& q) {
   return QkArgs{q.tokens, q.q_heads, q.kv_heads, q.head_dim, q.rope_dim, q.table_rows, q.seq_len > 0 ? q.seq_len : 1,
-                q.eps, q.positions, q.table};
+                0, q.eps, q.positions, q.table};
 }
 
 struct QkCall {
@@ -441,12 +442,26 @@ struct Fwd {
   template <typename T, int G, int CH, int MODE>
   static hipError_t run(const QkCall& c) {
     const QkShape& q = c.q;
-    const long long bq = heads_blocks(q.tokens, q.q_heads, G), bk = heads_blocks(q.tokens, q.kv_heads, G);
-    const long long bv = c.in != c.out ? copy_blocks(q, sizeof(T)) : 0;
-    if (bq + bk + bv > 0x7fffffffLL) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((qk_fwd_kernel<T, G, CH, MODE>), dim3((unsigned)(bq + bk + bv)), dim3(256), 0, c.s, qk_args(q),
-                       QkGrid{(int)bq, (int)bk, (int)bv}, (const T*)c.in, (const T*)c.gq, (const T*)c.gk, (T*)c.out);
-    return hipGetLastError();
+    QkArgs a = qk_args(q);
+    // Tokens that one launch can hold; a call of more goes in several.
+    constexpr long long heads = 256 / G, chunks = 256 * kCopyUnroll;  // of a workgroup
+    const long long per = (long long)(q.q_heads + q.kv_heads) * chunks +
+                          (c.in != c.out ? (long long)q.kv_heads * q.head_dim * sizeof(T) / 16 * heads : 0);
+    const long long most = (max_groups(256) - 3) * (heads * chunks) / per;
+    const size_t row = (size_t)(q.q_heads + 2 * q.kv_heads) * q.head_dim;
+    for (long long t = 0; t < q.tokens; t += a.tokens) {
+      a.first = (int)t;
+      a.tokens = (int)std::min(most, q.tokens - t);
+      a.positions = q.positions ? q.positions + t : nullptr;
+      const long long bq = heads_blocks(a.tokens, q.q_heads, G), bk = heads_blocks(a.tokens, q.kv_heads, G);
+      const long long bv = c.in != c.out ? copy_blocks(a.tokens, q, sizeof(T)) : 0;
+      hipLaunchKernelGGL((qk_fwd_kernel<T, G, CH, MODE>), dim3((unsigned)(bq + bk + bv)), dim3(256), 0, c.s, a,
+                         QkGrid{(int)bq, (int)bk, (int)bv}, (const T*)c.in + t * row, (const T*)c.gq, (const T*)c.gk,
+                         (T*)c.out + t * row);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
   }
 };
 
@@ -463,7 +478,7 @@ struct Bwd {
       bq = (int)std::min<long long>(bq, heads_blocks(q.tokens, q.q_heads, G));  // with 64 heads a workgroup
       bk = (int)std::min<long long>(bk, heads_blocks(q.tokens, q.kv_heads, G));
     }
-    const long long bv = c.dout != c.out ? copy_blocks(q, sizeof(T)) : 0;
+    const long long bv = c.dout != c.out ? copy_blocks(q.tokens, q, sizeof(T)) : 0;
     if (bq + bk + bv > 0x7fffffffLL) return hipErrorInvalidValue;
     hipLaunchKernelGGL((qk_bwd_kernel<T, G, CH, MODE>), dim3((unsigned)(bq + bk + bv)), dim3(256), 0, c.s, qk_args(q),
                        QkGrid{bq, bk, (int)bv}, (const T*)c.dout, (const T*)c.in, (const T*)c.gq, (const T*)c.gk,
