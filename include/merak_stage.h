@@ -482,8 +482,8 @@ typedef enum { MERAK_I32 = 0, MERAK_I64 = 1 } merak_id_type;
  * [tokens, hidden] of dtype.  An id outside first_id .. first_id + table_rows - 1
  * (another rank's, or padding such as -1) gives a row of zeros, so the ranks' y
  * add up to the whole lookup.  hidden % 8 == 0 and at most 2^20; tokens and
- * table_rows at most 2^30; first_id >= 0, first_id + table_rows at most 2^63; scale
- * finite. */
+ * table_rows at most 2^30; y at most 2^38 - 2^14 bytes; first_id >= 0, first_id +
+ * table_rows at most 2^63; scale finite. */
 int merak_embedding_fwd(int dtype, int id_type, int tokens, int hidden, int table_rows, int64_t first_id,
                         float scale, const void* ids, const void* table, void* y, void* stream);
 
@@ -500,8 +500,9 @@ int merak_embedding_bwd(int dtype, int id_type, int tokens, int hidden, int tabl
 
 /* Rotation table: table[p][i] = (cos a, sin a), a = p * theta^(-2 i / rope_dim),
  * for p < positions and i < rope_dim / 2, evaluated in fp64 and rounded to fp32.
- * rope_dim a multiple of 16, at most 256.  A caller with other angles (stretched
- * positions, other frequencies) may fill a table itself. */
+ * rope_dim a multiple of 16, at most 256; positions * rope_dim / 2 at most 2^32 - 2^8.
+ * A caller with other angles (stretched positions, other frequencies) may fill a table
+ * itself. */
 int merak_rope_table(int positions, int rope_dim, double theta, float* table, void* stream);
 
 /* RMS norm of every query and key head, then rotation by the token's position, in
@@ -548,7 +549,8 @@ int merak_qk_norm_rope_bwd(int dtype, int tokens, int q_heads, int kv_heads, int
  * values are rounded to nearest, ties to even.  A restored value is off by at most
  * 2^-4 of itself, or by 2^-10 of the scale below 2^-6 of it.  Magnitudes
  * above 240 * 2^120 (3.19e38) come back as that; NaN and infinities come back as NaN
- * and do not touch their neighbours.  cols % 32 == 0. */
+ * and do not touch their neighbours.  cols % 32 == 0; rows * cols at most 2^35 - 2^11
+ * (else MERAK_ERR_SHAPE), here and in the calls that read a checkpoint. */
 int merak_act8_save(int dtype, int rows, int cols, const void* x, uint8_t* q, uint8_t* scales, void* stream);
 
 /* x from its checkpoint (exact in either dtype: 4 significant bits). */

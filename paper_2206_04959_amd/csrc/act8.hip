@@ -575,7 +575,7 @@ __global__ void __launch_bounds__(256) act8_dw_f32_kernel(DwArgs p, const float*
 static bool chunk_grid(int rows, int cols, long long* chunks, dim3* grid) {
   *chunks = (long long)rows * (cols / 8);
   const long long wg = (*chunks + 255) / 256;
-  if (wg > 0x7fffffffLL) return false;
+  if (wg > max_groups(256)) return false;
   *grid = dim3((unsigned)wg);
   return true;
 }
@@ -583,7 +583,7 @@ static bool chunk_grid(int rows, int cols, long long* chunks, dim3* grid) {
 hipError_t launch_act8_save(int dtype, int rows, int cols, const void* x, uint8_t* q, uint8_t* scales, hipStream_t s) {
   long long n;
   dim3 grid;
-  if (!chunk_grid(rows, cols, &n, &grid)) return hipErrorInvalidValue;
+  if (!chunk_grid(rows, cols, &n, &grid)) return hipErrorInvalidConfiguration;
   if (dtype == DT_BF16)
     hipLaunchKernelGGL(act8_save_kernel<bf16_t>, grid, dim3(256), 0, s, n, (const bf16_t*)x, q, scales);
   else
@@ -595,7 +595,7 @@ hipError_t launch_act8_restore(int dtype, int rows, int cols, const uint8_t* q, 
                                hipStream_t s) {
   long long n;
   dim3 grid;
-  if (!chunk_grid(rows, cols, &n, &grid)) return hipErrorInvalidValue;
+  if (!chunk_grid(rows, cols, &n, &grid)) return hipErrorInvalidConfiguration;
   const bool past = (size_t)rows * cols * (dtype == DT_BF16 ? 2 : 4) >= kStreamBytes;
   if (dtype == DT_BF16)
     hipLaunchKernelGGL((past ? act8_restore_kernel<bf16_t, true> : act8_restore_kernel<bf16_t, false>), grid,
@@ -610,7 +610,7 @@ hipError_t launch_act8_gelu_bwd(int dtype, int rows, int cols, const void* dg, c
                                 void* du, void* g, hipStream_t s) {
   long long n;
   dim3 grid;
-  if (!chunk_grid(rows, cols, &n, &grid)) return hipErrorInvalidValue;
+  if (!chunk_grid(rows, cols, &n, &grid)) return hipErrorInvalidConfiguration;
   if (dtype == DT_BF16)
     hipLaunchKernelGGL(act8_gelu_bwd_kernel<bf16_t>, grid, dim3(256), 0, s, n, (const bf16_t*)dg, q, scales,
                        (bf16_t*)du, (bf16_t*)g);
@@ -714,9 +714,7 @@ static hipError_t run_dw(const DwArgs& a, int splits, hipStream_t s) {
   static std::atomic<uint64_t> lds_set{0};
   const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(kern), lds, lds_set);
   if (e != hipSuccess) return e;
-  const long long wg = (long long)a.tiles * splits;
-  if (wg > 0x7fffffffLL) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(kern, dim3((unsigned)wg), dim3(WM * WN * 64), lds, s, a);
+  hipLaunchKernelGGL(kern, dim3((unsigned)(a.tiles * splits)), dim3(WM * WN * 64), lds, s, a);
   return hipGetLastError();
 }
 
@@ -736,6 +734,7 @@ static hipError_t run_dw_plan(const DwPlan& p, const DwArgs& a, hipStream_t s) {
 hipError_t launch_act8_gemm_dw(int dtype, int tokens, int n_out, int n_in, const void* dy, const uint8_t* q,
                                const uint8_t* scales, float* dw, int accumulate, void* scratch, hipStream_t s) {
   const DwPlan p = dw_plan_of(dtype, tokens, n_out, n_in);
+  if ((long long)p.tiles * p.splits > max_groups(512)) return hipErrorInvalidConfiguration;
   const bool split = p.splits > 1;
   bf16_t* values = (bf16_t*)scratch;
   float* sums = (float*)((char*)scratch + dw_values_bytes(p, tokens, n_in));
@@ -749,10 +748,8 @@ hipError_t launch_act8_gemm_dw(int dtype, int tokens, int n_out, int n_in, const
   if (dtype == DT_BF16) {
     e = run_dw_plan(p, a, s);
   } else {
-    const long long wg = (long long)p.tiles * p.splits;
-    if (wg > 0x7fffffffLL) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((p.bm == 128 ? act8_dw_f32_kernel<2> : act8_dw_f32_kernel<1>), dim3((unsigned)wg), dim3(256),
-                       0, s, a, (const float*)dy);
+    hipLaunchKernelGGL((p.bm == 128 ? act8_dw_f32_kernel<2> : act8_dw_f32_kernel<1>),
+                       dim3((unsigned)(p.tiles * p.splits)), dim3(256), 0, s, a, (const float*)dy);
     e = hipGetLastError();
   }
   if (e != hipSuccess || !split) return e;

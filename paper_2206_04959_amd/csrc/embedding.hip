@@ -575,7 +575,7 @@ static hipError_t fwd_t(int tokens, int hidden, int rows, long long first, float
                         const void* table, void* y, hipStream_t s) {
   const long long chunks = (long long)tokens * (hidden / (16 / (int)sizeof(T)));
   const long long wg = (chunks + 256 * kFwdUnroll - 1) / (256 * kFwdUnroll);
-  if (wg > 0x7fffffffLL) return hipErrorInvalidValue;
+  if (wg > max_groups(256)) return hipErrorInvalidConfiguration;
   const bool past = (size_t)tokens * hidden * sizeof(T) >= kStreamBytes;
   hipLaunchKernelGGL((past ? embedding_fwd_kernel<T, I, true> : embedding_fwd_kernel<T, I, false>), dim3((unsigned)wg),
                      dim3(256), 0, s, tokens, hidden, rows, first, scale, (const I*)ids, (const T*)table, (T*)y);

@@ -14,6 +14,15 @@ namespace {
 int check_dtype(int dtype) { return dtype == MERAK_BF16 || dtype == MERAK_FP32 ? MERAK_OK : MERAK_ERR_INVALID_ARG; }
 int check_flag(int f) { return f == 0 || f == 1 ? MERAK_OK : MERAK_ERR_INVALID_ARG; }
 
+// A call that needs more workgroups than a launch can have is refused by its launcher, before
+// anything is enqueued.
+#define LAUNCH_TRY(expr)                                                  \
+  do {                                                                    \
+    const hipError_t e_ = (expr);                                         \
+    if (e_ == hipErrorInvalidConfiguration) return MERAK_ERR_SHAPE;       \
+    if (e_ != hipSuccess) return MERAK_ERR_HIP;                           \
+  } while (0)
+
 // A call's arrays: what it writes must not overlap anything else it uses.
 struct Span {
   const void* p;
@@ -97,8 +106,8 @@ int merak_embedding_fwd(int dtype, int id_type, int tokens, int hidden, int tabl
   TRY(check_ptr(ids)); TRY(check_ptr(table)); TRY(check_ptr(y));
   const size_t row = hidden * elem(dtype);
   TRY(check_apart({{y, tokens * row}}, {{ids, tokens * id_bytes(id_type)}, {table, table_rows * row}}));
-  HIP_TRY(launch_embedding_fwd(dtype, id_type, tokens, hidden, table_rows, first_id, scale, ids, table, y,
-                               (hipStream_t)stream));
+  LAUNCH_TRY(launch_embedding_fwd(dtype, id_type, tokens, hidden, table_rows, first_id, scale, ids, table, y,
+                                  (hipStream_t)stream));
   return MERAK_OK;
 }
 
@@ -117,8 +126,8 @@ int merak_embedding_bwd(int dtype, int id_type, int tokens, int hidden, int tabl
   if (sb > 0) TRY(check_ptr(scratch));
   TRY(check_apart({{dtable, (size_t)table_rows * hidden * 4}, {scratch, sb}},
                   {{ids, tokens * id_bytes(id_type)}, {dy, (size_t)tokens * hidden * elem(dtype)}}));
-  HIP_TRY(launch_embedding_bwd(dtype, id_type, tokens, hidden, table_rows, first_id, scale, ids, dy, dtable,
-                               accumulate, scratch, (hipStream_t)stream));
+  LAUNCH_TRY(launch_embedding_bwd(dtype, id_type, tokens, hidden, table_rows, first_id, scale, ids, dy, dtable,
+                                  accumulate, scratch, (hipStream_t)stream));
   return MERAK_OK;
 }
 
@@ -126,7 +135,7 @@ int merak_rope_table(int positions, int rope_dim, double theta, float* table, vo
   if (positions <= 0 || rope_dim <= 0 || rope_dim % 16 || rope_dim > 256) return MERAK_ERR_SHAPE;
   if (!(theta > 0.0) || !std::isfinite(theta)) return MERAK_ERR_INVALID_ARG;
   TRY(check_ptr(table));
-  HIP_TRY(launch_rope_table(positions, rope_dim, theta, table, (hipStream_t)stream));
+  LAUNCH_TRY(launch_rope_table(positions, rope_dim, theta, table, (hipStream_t)stream));
   return MERAK_OK;
 }
 
@@ -142,7 +151,7 @@ int merak_qk_norm_rope_fwd(int dtype, int tokens, int q_heads, int kv_heads, int
   const size_t row = qk_row_bytes(shape, dtype), gain = head_dim * elem(dtype);
   TRY(check_apart({{out, row}}, {{out == qkv ? nullptr : qkv, row}, {q_gamma, gain}, {k_gamma, gain}, table_span(shape),
                                  position_span(shape)}));
-  HIP_TRY(launch_qk_norm_rope_fwd(dtype, shape, qkv, q_gamma, k_gamma, out, (hipStream_t)stream));
+  LAUNCH_TRY(launch_qk_norm_rope_fwd(dtype, shape, qkv, q_gamma, k_gamma, out, (hipStream_t)stream));
   return MERAK_OK;
 }
 
@@ -168,8 +177,8 @@ int merak_qk_norm_rope_bwd(int dtype, int tokens, int q_heads, int kv_heads, int
   TRY(check_apart({{dqkv, row}, {dq_gamma, dg}, {dk_gamma, dg}, sums},
                   {{qkv, row}, {q_gamma, gain}, {k_gamma, gain}, table_span(shape), position_span(shape),
                    {dqkv == dout ? nullptr : dout, row}}));
-  HIP_TRY(launch_qk_norm_rope_bwd(dtype, shape, dout, qkv, q_gamma, k_gamma, dqkv, dq_gamma, dk_gamma, accumulate,
-                                  scratch, (hipStream_t)stream));
+  LAUNCH_TRY(launch_qk_norm_rope_bwd(dtype, shape, dout, qkv, q_gamma, k_gamma, dqkv, dq_gamma, dk_gamma, accumulate,
+                                     scratch, (hipStream_t)stream));
   return MERAK_OK;
 }
 
@@ -178,7 +187,7 @@ int merak_act8_save(int dtype, int rows, int cols, const void* x, uint8_t* q, ui
   TRY(check_ptr(x));
   const size_t n = (size_t)rows * cols;
   TRY(check_apart({{q, n}, {scales, n / 32}}, {{x, n * elem(dtype)}}));
-  HIP_TRY(launch_act8_save(dtype, rows, cols, x, q, scales, (hipStream_t)stream));
+  LAUNCH_TRY(launch_act8_save(dtype, rows, cols, x, q, scales, (hipStream_t)stream));
   return MERAK_OK;
 }
 
@@ -187,7 +196,7 @@ int merak_act8_restore(int dtype, int rows, int cols, const uint8_t* q, const ui
   TRY(check_ptr(x));
   const size_t n = (size_t)rows * cols;
   TRY(check_apart({{x, n * elem(dtype)}}, {{q, n}, {scales, n / 32}}));
-  HIP_TRY(launch_act8_restore(dtype, rows, cols, q, scales, x, (hipStream_t)stream));
+  LAUNCH_TRY(launch_act8_restore(dtype, rows, cols, q, scales, x, (hipStream_t)stream));
   return MERAK_OK;
 }
 
@@ -198,7 +207,7 @@ int merak_act8_gelu_bwd(int dtype, int rows, int cols, const void* dg, const uin
   if (g) TRY(check_ptr(g));
   const size_t n = (size_t)rows * cols, nb = n * elem(dtype);
   TRY(check_apart({{du, nb}, {g, nb}}, {{q, n}, {scales, n / 32}, {du == dg ? nullptr : dg, nb}}));
-  HIP_TRY(launch_act8_gelu_bwd(dtype, rows, cols, dg, q, scales, du, g, (hipStream_t)stream));
+  LAUNCH_TRY(launch_act8_gelu_bwd(dtype, rows, cols, dg, q, scales, du, g, (hipStream_t)stream));
   return MERAK_OK;
 }
 
@@ -217,8 +226,8 @@ int merak_act8_gemm_dw(int dtype, int tokens, int n_out, int n_in, const void* d
   if (sb > 0) TRY(check_ptr(scratch));
   TRY(check_apart({{dw, (size_t)n_out * n_in * 4}, {scratch, sb}},
                   {{dy, (size_t)tokens * n_out * elem(dtype)}, {q, n}, {scales, n / 32}}));
-  HIP_TRY(launch_act8_gemm_dw(dtype, tokens, n_out, n_in, dy, q, scales, dw, accumulate, scratch,
-                              (hipStream_t)stream));
+  LAUNCH_TRY(launch_act8_gemm_dw(dtype, tokens, n_out, n_in, dy, q, scales, dw, accumulate, scratch,
+                                 (hipStream_t)stream));
   return MERAK_OK;
 }
 

@@ -418,7 +418,7 @@ size_t qk_norm_rope_scratch_elems(int tokens, int q_heads, int kv_heads, int d) 
 
 hipError_t launch_rope_table(int positions, int rope_dim, double theta, float* table, hipStream_t s) {
   const long long wg = ((long long)positions * (rope_dim / 2) + 255) / 256;
-  if (wg > 0x7fffffffLL) return hipErrorInvalidValue;
+  if (wg > max_groups(256)) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL(rope_table_kernel, dim3((unsigned)wg), dim3(256), 0, s, positions, rope_dim / 2, std::log(theta),
                      table);
   return hipGetLastError();
@@ -479,7 +479,7 @@ struct Bwd {
       bk = (int)std::min<long long>(bk, heads_blocks(q.tokens, q.kv_heads, G));
     }
     const long long bv = c.dout != c.out ? copy_blocks(q.tokens, q, sizeof(T)) : 0;
-    if (bq + bk + bv > 0x7fffffffLL) return hipErrorInvalidValue;
+    if (bq + bk + bv > max_groups(256)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL((qk_bwd_kernel<T, G, CH, MODE>), dim3((unsigned)(bq + bk + bv)), dim3(256), 0, c.s, qk_args(q),
                        QkGrid{bq, bk, (int)bv}, (const T*)c.dout, (const T*)c.in, (const T*)c.gq, (const T*)c.gk,
                        (T*)c.out, one ? nullptr : c.part, c.dgq, c.dgk, c.accumulate);

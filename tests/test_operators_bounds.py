@@ -85,3 +85,50 @@ def test_the_tables_last_row_has_an_id():
         # the next check is reached by tables that end at the last id
         assert _embedding(LAST - rows + 1, rows, y=P[2] + 4) == (ALIGN, ALIGN)
     assert _embedding(LAST, 1, y=P[2] + 4) == (ALIGN, ALIGN)
+
+
+# A launch counts its threads in 32 bits, and one of more does only a part of its work, without an
+# error.  The least sizes that are too large, each with the largest that is not (whose call ends
+# at an unaligned pointer or, here without a GPU, at the launch).
+HIP = -6
+FAR = [(i + 1) << 44 for i in range(5)]  # addresses that no array of these sizes connects
+
+
+def _act8(rows, cols):
+    L = B.lib()
+    return {L.merak_act8_save(0, rows, cols, FAR[0], FAR[1], FAR[2], None),
+            L.merak_act8_restore(1, rows, cols, FAR[1], FAR[2], FAR[0], None),
+            L.merak_act8_gelu_bwd(0, rows, cols, FAR[0], FAR[1], FAR[2], FAR[3], None, None)}
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the allowed sizes would be launched")
+@pytest.mark.parametrize("rows,cols,status", [
+    (2 ** 30, 32, SHAPE), (2 ** 24, 2 ** 11, SHAPE), (2 ** 30 - 63, 32, SHAPE), (2 ** 30 - 64, 32, HIP),
+    (2 ** 24 - 1, 2 ** 11, HIP)])
+def test_act8_largest_arrays(rows, cols, status):
+    assert _act8(rows, cols) == {status}
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the allowed sizes would be launched")
+@pytest.mark.parametrize("dtype,tokens,hidden,status", [
+    (0, 2 ** 24, 2 ** 13, SHAPE), (0, 2 ** 24 - 1, 2 ** 13, HIP), (1, 2 ** 24, 2 ** 12, SHAPE),
+    (1, 2 ** 24 - 1, 2 ** 12, HIP), (0, 2 ** 30, 8, HIP)])
+def test_embedding_largest_output(dtype, tokens, hidden, status):
+    assert B.lib().merak_embedding_fwd(dtype, 0, tokens, hidden, 10, 0, 1.0, FAR[0], FAR[1], FAR[2], None) == status
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the allowed sizes would be launched")
+@pytest.mark.parametrize("positions,rope,status", [
+    (2 ** 25 - 1, 256, SHAPE), (2 ** 25 - 2, 256, HIP), (2 ** 29, 16, SHAPE), (2 ** 29 - 32, 16, HIP)])
+def test_rope_table_largest(positions, rope, status):
+    assert B.lib().merak_rope_table(positions, rope, 1e4, FAR[0], None) == status
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the allowed sizes would be launched")
+@pytest.mark.parametrize("dtype,tokens,n_out,n_in,status", [
+    (0, 64, 2 ** 20, 2 ** 20, SHAPE), (1, 64, 2 ** 20, 2 ** 20, SHAPE),  # more output tiles than a launch holds
+    (0, 2 ** 25, 2048, 1024, SHAPE),                                     # X is restored first, and too large for it
+    (0, 2 ** 25, 512, 1024, HIP), (1, 2 ** 25, 2048, 1024, HIP), (0, 2 ** 24, 2048, 1024, HIP)])
+def test_weight_gradient_largest(dtype, tokens, n_out, n_in, status):
+    L = B.lib()
+    assert L.merak_act8_gemm_dw(dtype, tokens, n_out, n_in, FAR[0], FAR[1], FAR[2], FAR[3], 0, FAR[4], None) == status
