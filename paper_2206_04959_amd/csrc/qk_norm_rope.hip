@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(256) qk_bwd_kernel(QkArgs a, QkGrid grid, cons
       for (int e = 0; e < 8; ++e) dz[i][e] = rstd * (dz[i][e] - x[i][e] * m);
     store_chunks<G, CH>(dx + at, j, a.d, dz);
   }
-  // the wave's groups, then the four waves in order
+  // the wave's groups, then the four waves, as trees
 #pragma unroll
   for (int i = 0; i < CH; ++i)
 #pragma unroll
@@ -329,7 +329,7 @@ __global__ void __launch_bounds__(256) qk_bwd_kernel(QkArgs a, QkGrid grid, cons
     }
   __syncthreads();
   for (int i = threadIdx.x; i < a.d; i += 256) {
-    const float v = red[0][i] + red[1][i] + red[2][i] + red[3][i];
+    const float v = (red[0][i] + red[1][i]) + (red[2][i] + red[3][i]);
     if (part) {
       part[(size_t)blockIdx.x * a.d + i] = v;
     } else {
@@ -340,9 +340,10 @@ __global__ void __launch_bounds__(256) qk_bwd_kernel(QkArgs a, QkGrid grid, cons
 }
 
 // Gain gradients from the workgroups' sums, 16 columns of one gain a workgroup: 64
-// threads a column take every 64th sum (16 in flight), and are added in order.  (One
-// column a lane with 16 waves, the way the other column sums end, took 17 us for
-// 1024 sums.)
+// threads a column take every 64th sum (16 in flight), and are added as a tree: in a chain
+// the last additions' roundings were most of the result's (1023 tokens of 24 heads of 128 in
+// fp32: off by 2.0e-7 of the largest, 1.2e-7 so).  (One column a lane with 16 waves, the
+// way the other column sums end, took 17 us for 1024 sums.)
 __global__ void __launch_bounds__(1024) qk_gain_kernel(int d, QkGrid grid, const float* __restrict__ part,
                                                        float* __restrict__ dgq, float* __restrict__ dgk,
                                                        int accumulate) {
@@ -366,11 +367,15 @@ __global__ void __launch_bounds__(1024) qk_gain_kernel(int d, QkGrid grid, const
   red[slice][threadIdx.x & 15] = s;
   __syncthreads();
   if (threadIdx.x < 16 && col < d) {
-    float v = 0.0f;
+    float v[64];
 #pragma unroll
-    for (int i = 0; i < 64; ++i) v += red[i][threadIdx.x];
+    for (int i = 0; i < 64; ++i) v[i] = red[i][threadIdx.x];
+#pragma unroll
+    for (int n = 32; n > 0; n >>= 1)
+#pragma unroll
+      for (int i = 0; i < n; ++i) v[i] += v[i + n];
     float* o = (keys ? dgk : dgq) + col;
-    *o = accumulate ? *o + v : v;
+    *o = accumulate ? *o + v[0] : v[0];
   }
 }
 
