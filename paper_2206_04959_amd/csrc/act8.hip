@@ -77,7 +77,8 @@ __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_floa
 
 // ---------------------------------------------------------------------------
 // Save and restore: four lanes to a block, 8 features a lane.  Bound by memory: 16384 x
-// 6144 in bf16 (305 MB each) 52 and 43 us.
+// 6144 in bf16 (305 MB each) 54 and 49 us, one behind the other 98 (the codes are then
+// still in the last-level cache); in fp32 (506 MB) 87 and 132.
 // ---------------------------------------------------------------------------
 template <typename T>
 __global__ void __launch_bounds__(256) act8_save_kernel(long long chunks, const T* __restrict__ x,
@@ -132,8 +133,8 @@ __device__ __forceinline__ void gelu_both(float u, float* gelu, float* slope) {
   *slope = s + u * (big * small) * (2.0f * kGeluC * (1.0f + 3.0f * kGeluA * u2));
 }
 
-// Bound by memory (8191 x 6400 in bf16, 369 MB: 61 us): one exponential and one reciprocal a
-// value fit beside it.
+// Bound by memory (8191 x 6400 in bf16, 369 MB: 64 us; without g 47; in fp32 125): one
+// exponential and one reciprocal a value fit beside it.
 // du = dg * gelu'(u) and, unless g is NULL, g = gelu(u), with u in 8 bits.
 template <typename T>
 __global__ void __launch_bounds__(256) act8_gelu_bwd_kernel(long long chunks, const T* dg,
@@ -178,8 +179,9 @@ __global__ void __launch_bounds__(256) act8_gelu_bwd_kernel(long long chunks, co
 // codes of stage kt + 3 in the last sub-step, the conversions in the next two.  Every
 // wait is for the loads of a whole stage ago.  A workgroup alone on its CU has nothing
 // else to run meanwhile and waits for memory once a stage; it has eight waves and, from
-// eight times kBK tokens on, stages of twice the length (H = 2): 4096 x 2048 x 2048 56.5 us
-// with four waves and one kBK a stage, 48.8 so; 64 x 1024 x 1024 5.3, and 6.3 with H = 2.
+// eight times kBK tokens on, stages of twice the length (H = 2): 4096 x 2048 x 2048 52.8 us
+// with four waves and one kBK a stage, 44.6 so; 64 x 1024 x 1024 5.2, and 6.1 with H = 2;
+// 512 x 1024 x 1024 9.3 either way.
 // Buffers are addressed from each stage's first token, so operands may be of any
 // size; tokens past the end read as zeros.
 // ---------------------------------------------------------------------------
@@ -456,8 +458,9 @@ __global__ void __launch_bounds__(256) act8_dw_join_kernel(long long chunks, int
   *o = s;
 }
 
-// Many splits (16 and more, of small outputs) share a chunk among eight threads: 128 splits
-// of 64 x 64, added by one thread each, took 40 us.
+// Many splits (16 and more, of small outputs) share a chunk among eight threads: a call of
+// 171 splits of 64 x 64 takes 10.9 us, 18.4 with one thread a chunk; 128 of 128 x 128 12.3
+// and 17.0.
 static hipError_t launch_dw_join(long long elems, int splits, const float* part, float* dw, int accumulate,
                                  hipStream_t s) {
   const long long chunks = elems / 4;
@@ -473,9 +476,9 @@ static hipError_t launch_dw_join(long long elems, int splits, const float* part,
 // fp32 check mode, on the fp32 matrix instruction (32 x 32 x 2): tiles of 64 NB x 64 NB, four
 // waves of 32 NB x 32 NB, 32 tokens a stage.  The next stage's operands are on their way to
 // registers meanwhile, X's as codes until they go to LDS, and fragments are read ahead of
-// their MFMAs.  Bound by the matrix instruction's rate: 8192 x 4096 x 4096 2.12 ms (130
-// TFLOP/s; 153 is what the library reaches there); NB = 1 125, and 1000 x 3000 x 1024 98
-// against 85.
+// their MFMAs.  Bound by the matrix instruction's rate: 8192 x 4096 x 4096 2.13 ms (129
+// TFLOP/s; 151 is what the library reaches there), and 2.19 with NB = 1; 1000 x 3000 x 1024
+// 62 us with NB = 1 and 70 with NB = 2.
 constexpr int kStageF32 = 32;
 
 template <int NB>
@@ -629,9 +632,12 @@ struct DwPlan {
 
 // Restoring X reads and writes it once more (3 bytes a value, and a launch); it saves
 // every one of the n_out / bm tiles in its column the conversion, about 6e-10 us a
-// product.  Measured (four waves a workgroup), restored and converted: 16384 x 7680 x 1920 (tokens x outputs x
-// inputs) 429 and 540 us, 2048 x 4096 x 1024 33 and 35; 2048 x 1024 x 1024 25 and 22,
-// 333 x 1920 x 640 11 and 9.
+// product.  Measured, restored and converted: 16384 x 7680 x 1920 (tokens x outputs x
+// inputs) 427 and 611 us, 4096 x 2048 x 2048 44.8 and 50.5, 2048 x 4096 x 1024 26.7 and 28.8,
+// 512 x 7680 x 1920 29.1 and 30.9; 2048 x 1024 x 1024 19.6 and 17.9, 4096 x 1024 x 1024 24.1
+// and 22.7, 333 x 1920 x 640 10.0 and 8.2.  Near the border the rule does not know how the
+// product will be cut up, and takes the slower side of 16384 x 1304 x 2080 (restored, 153 and
+// 137), 32768 x 2048 x 512 (restored, 105 and 96) and 16384 x 1024 x 8192 (converted, 292 and 314).
 static bool dw_restore(double tokens, double n_out, double n_in) {
   return 6e-10 * tokens * n_out * n_in > 2.5 + 6.7e-7 * tokens * n_in;
 }
@@ -639,10 +645,10 @@ static bool dw_restore(double tokens, double n_out, double n_in) {
 // Tile and splits by estimated time: whole rounds of workgroups over the chip, each as
 // long as its stages (and about four more for its start and end); splits add their
 // sums' way through memory and a launch.  us a stage, measured: 256 x 256 1.6, 256 x 192
-// 1.16 (one workgroup a CU); 128 x 128 0.6 alone on its CU, 0.92 for two; converting adds a
-// seventh.  What it decides, with the other choice's time: 8192 x 6400 x 1600 256 x 192
-// 161 us, 256 x 256 170, 128 x 128 201; 16384 x 7680 x 1920 256 x 256 429, 128 x 128 499;
-// 4096 x 2048 x 2048 128 x 128 in one split 49, in two 53.
+// 1.0 to 1.3 (one workgroup a CU); 128 x 128 0.6 alone on its CU, 0.95 for two; converting adds
+// a seventh.  What it decides, with the other choice's time: 8192 x 6400 x 1600 256 x 192
+// 184 us, 256 x 256 188, 128 x 128 212; 16384 x 7680 x 1920 256 x 256 428, 128 x 128 514,
+// 256 x 192 541; 4096 x 2048 x 2048 128 x 128 in one split 48, in two 52.
 static DwPlan dw_plan(int tokens, int n_out, int n_in) {
   struct Tile {
     int bm, bn, resident;
@@ -678,7 +684,7 @@ static DwPlan dw_plan(int tokens, int n_out, int n_in) {
 
 // fp32: 128 x 128 tiles for products of at least 2^14 of their stages, else 64 x 64; and splits
 // of at least eight stages where the tiles alone would leave CUs without work (32768 x
-// 512 x 512: 1.1 ms in one split, 0.17 in 16).
+// 512 x 512: 2.3 ms in one split, 0.16 in 64).
 static DwPlan dw_plan_f32(int tokens, int n_out, int n_in) {
   DwPlan p{};
   auto tiles = [&](long long t) { return (n_out + t - 1) / t * ((n_in + t - 1) / t); };

@@ -80,8 +80,8 @@ __global__ void __launch_bounds__(256) embedding_fwd_kernel(int tokens, int hidd
 // ---------------------------------------------------------------------------
 // Backward
 // ---------------------------------------------------------------------------
-// Up to here one launch, without sorting: 2048 tokens of 1024 on 6000 rows 14.5 us, sorted
-// 18.9; 257 tokens 7.4 and 15.0.
+// Up to here one launch, without sorting: 2048 tokens of a text of 1024 on 6000 rows 16.6 us,
+// sorted 21.0; 1024 tokens 13.4 and 20.1; 257 tokens 8.3 and 16.9.
 constexpr int kDirect = 2048;
 constexpr int kSortBlock = 2048;  // tokens that are ranked against each other
 constexpr int kFillRows = 16;     // most table rows that a workgroup clears
@@ -171,7 +171,10 @@ __global__ void __launch_bounds__(64 * kRankWaves) embedding_rank_kernel(int tok
 // Whole order from the sorted blocks: a token's position is the number of tokens
 // before it in each block, found by binary search.  A workgroup places 64 tokens;
 // each of its waves (one a block, at most 16) brings a block's keys into LDS and
-// searches there: twelve dependent loads from L2 instead took 4 of 5 us.
+// searches there: twelve dependent loads from L2 instead took 4 of 5 us.  As every workgroup
+// reads all other blocks, the time grows with the square of the tokens: all launches for rows
+// of 8 columns take 25 us at 16384 tokens, 34 at 32768, 128 at 131072, 3.3 ms at 2^20 and 48 at
+// 2^22, the most that a call takes.
 constexpr int kMergeWaves = 16;
 
 __global__ void __launch_bounds__(64 * kMergeWaves) embedding_merge_kernel(int tokens, const int* __restrict__ skey,

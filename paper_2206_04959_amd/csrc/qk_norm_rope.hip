@@ -26,9 +26,10 @@
 //   any other head, or any other number of rotated features: one chunk a lane, pairs
 //     anywhere in the group.
 // In bf16, values copied: 32768 tokens of 20 + 20 heads of 96 163 us (4.6 TB/s; a large copy
-// has 4.8), 16384 tokens of 12 + 12 of 128 61 (4.9), of 80 50 (3.8: 6 of 16 lanes idle);
-// gradients of 16384 tokens: 25 + 25 heads of 64 86 us (4.9), 12 + 12 of 128 82 (4.9), of
-// 96 72 (4.2: three waves a SIMD).
+// has 4.8 to 5.1), 16384 tokens of 12 + 12 of 128 64 (4.7), of 256 121 (5.0), of 80 67 (2.8:
+// 6 of 16 lanes idle); in fp32 of 128 119 (5.1); gradients of 16384 tokens: 25 + 25 heads of 64
+// 87 us (4.8), 12 + 12 of 128 84 (4.8), of 256 161 (5.0), of 96 72 (4.2: three waves a SIMD), of
+// 80 77 (3.3); in fp32 of 128 162 (5.0).
 #include <algorithm>
 #include <cmath>
 
@@ -342,8 +343,8 @@ __global__ void __launch_bounds__(256) qk_bwd_kernel(QkArgs a, QkGrid grid, cons
 // Gain gradients from the workgroups' sums, 16 columns of one gain a workgroup: 64
 // threads a column take every 64th sum (16 in flight), and are added as a tree: in a chain
 // the last additions' roundings were most of the result's (1023 tokens of 24 heads of 128 in
-// fp32: off by 2.0e-7 of the largest, 1.2e-7 so).  (One column a lane with 16 waves, the
-// way the other column sums end, took 17 us for 1024 sums.)
+// fp32: off by 1.8e-7, 1.3e-7 so).  (One column a lane with 16 waves, the way the other
+// column sums end, took 17 us for 1024 sums.)
 __global__ void __launch_bounds__(1024) qk_gain_kernel(int d, QkGrid grid, const float* __restrict__ part,
                                                        float* __restrict__ dgq, float* __restrict__ dgk,
                                                        int accumulate) {
@@ -406,8 +407,9 @@ static long long copy_blocks(long long tokens, const QkShape& q, size_t esz) {
 }
 
 // Workgroups of the gradient's two kinds: as many as the chip holds at once (four a CU;
-// three with three chunks a lane, by their registers) shared out by the kinds' heads, or
-// one for each 32 heads if that is fewer.
+// three with three chunks a lane, by their registers, and so for all heads of 96, as the
+// scratch size does not depend on the rotation) shared out by the kinds' heads, or one for
+// each 32 heads if that is fewer.
 static void bwd_blocks(int tokens, int q_heads, int kv_heads, int d, int* bq, int* bk) {
   const long long all = d == 96 ? 768 : 1024;
   const long long share = std::max(1LL, all * q_heads / (q_heads + kv_heads));
@@ -476,7 +478,8 @@ struct Bwd {
     const QkShape& q = c.q;
     int bq = 1, bk = 1;
     // Up to four steps of one workgroup a kind take less than the launch that would add the
-    // sums of several: 8 tokens of 6 + 6 heads of 128 14.1 us a call with it, 11.7 without.
+    // sums of several: 8 or 20 tokens of 6 + 6 heads of 128 (2 or 4 steps) 9.4 us a call, with it
+    // 12.4.  (In a replayed graph, where a launch costs less: 5.5 or 7.6, with it 7.0.)
     const bool one = heads_blocks(q.tokens, std::max(q.q_heads, q.kv_heads), G) <= 4;
     if (!one) {
       bwd_blocks(q.tokens, q.q_heads, q.kv_heads, q.head_dim, &bq, &bk);
