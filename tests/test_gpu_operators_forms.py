@@ -182,3 +182,139 @@ def test_gelu_gradient_without_its_output(dtype):
     B.act8_gelu_bwd(dg, q, s, dg)
     torch.cuda.synchronize()
     assert torch.equal(du, alone) and torch.equal(du, dg)
+
+
+# ---------------------------------------------------------------------------
+# Values that are not finite, in the arrays and behind them
+# ---------------------------------------------------------------------------
+
+def _before(torch, t, bad):
+    """t at the start of an allocation whose rest holds `bad`."""
+    whole = torch.full((t.numel() + 4096 * t.shape[-1],), bad, dtype=t.dtype, device="cuda")
+    out = whole[:t.numel()].view(t.shape)
+    out.copy_(t)
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("tokens,n_out,n_in", [(301, 2056, 4128), (333, 264, 288), (601, 1000, 512), (1025, 6000, 2560),
+                                               (5001, 1928, 1056), (2001, 5000, 640), (6001, 1600, 1600), (1, 8, 32)])
+def test_weight_gradient_keeps_non_finite_values_apart(dtype, tokens, n_out, n_in):
+    """NaN behind the last token changes nothing; a NaN or an infinity of dy is in its output's row of dw,
+    a NaN of X in its input's column, and every other element keeps its bits."""
+    torch = need_gpu()
+    print(f"[act8 dw] {dtype} {tokens} tokens, {n_out} x {n_in}", flush=True)
+    torch.manual_seed(tokens)
+    dt = getattr(torch, dtype)
+    x, dy = torch.randn(tokens, n_in, device="cuda").to(dt), torch.randn(tokens, n_out, device="cuda").to(dt)
+    scratch = torch.empty(max(B.act8_gemm_dw_scratch_bytes(dt, tokens, n_out, n_in), 1), dtype=torch.uint8, device="cuda")
+
+    def run(dy, x, behind):
+        q = torch.empty((tokens, n_in), dtype=torch.uint8, device="cuda")
+        s = torch.empty((tokens, n_in // 32), dtype=torch.uint8, device="cuda")
+        B.act8_save(x, q, s)
+        if behind:
+            dy, q, s = _before(torch, dy, float("nan")), _before(torch, q, 0x7F), _before(torch, s, 200)
+        scratch.fill_(0xFF)
+        dw = torch.empty((n_out, n_in), device="cuda")
+        B.act8_gemm_dw(dy, q, s, dw, scratch)
+        torch.cuda.synchronize()
+        return dw
+
+    clean = run(dy, x, False)
+    assert torch.isfinite(clean).all() and torch.equal(run(dy, x, True), clean)
+    dy[0, n_out - 1], dy[tokens // 2, n_out // 2], x[tokens - 1, n_in - 1] = float("nan"), float("inf"), float("nan")
+    got = run(dy, x, True)
+    rows, cols = [n_out - 1, n_out // 2], n_in - 1
+    bad = torch.zeros_like(got, dtype=torch.bool)
+    bad[rows] = True
+    bad[:, cols] = True
+    assert not torch.isfinite(got[bad]).any() and torch.equal(got[~bad], clean[~bad])
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("tokens,hidden,rows", [(70, 72, 9), (2048, 8, 40), (5003, 520, 60)])
+def test_embedding_keeps_non_finite_values_apart(dtype, tokens, hidden, rows):
+    torch = need_gpu()
+    print(f"[embedding] {dtype} {tokens}x{hidden} rows {rows}", flush=True)
+    torch.manual_seed(tokens)
+    dt = getattr(torch, dtype)
+    ids = (torch.rand(tokens, device="cuda") ** 2 * (rows + 3)).long()
+    ids[tokens // 3] = -1
+    dy = _before(torch, torch.randn(tokens, hidden, device="cuda").to(dt), float("nan"))
+    scratch = torch.empty(max(B.embedding_scratch_bytes(tokens, hidden), 1), dtype=torch.uint8, device="cuda")
+
+    def run():
+        d = torch.full((rows, hidden), float("nan"), device="cuda")
+        scratch.fill_(0xFF)
+        B.embedding_bwd(ids, dy, d, scratch)
+        torch.cuda.synchronize()
+        return d
+
+    clean = run()
+    assert torch.isfinite(clean).all()
+    mine = ((ids >= 0) & (ids < rows)).nonzero()[:, 0]
+    t = int(mine[mine.numel() // 2])
+    dy[t, 3], dy[tokens // 3] = float("inf"), float("nan")  # one that counts, one of padding
+    got = run()
+    bad = torch.zeros_like(got, dtype=torch.bool)
+    bad[ids[t], 3] = True
+    assert torch.isinf(got[bad]).all() and torch.equal(got[~bad], clean[~bad])
+    table = torch.randn(rows, hidden, device="cuda").to(dt)
+    table[1, 2] = float("nan")
+    y = torch.empty((tokens, hidden), dtype=dt, device="cuda")
+    B.embedding_fwd(ids, table, y)
+    torch.cuda.synchronize()
+    want = torch.zeros_like(y)
+    want[:, 2] = (ids == 1).to(dt)
+    assert torch.equal(torch.isnan(y), want.bool()) and not y[(ids < 0) | (ids >= rows)].any()
+
+
+# ---------------------------------------------------------------------------
+# The widest rows and the most heads that the entry points take
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("tokens", [70, 2100])
+def test_embedding_of_the_widest_rows(tokens):
+    torch = need_gpu()
+    h, rows = 1 << 20, 6
+    print(f"[embedding] {tokens}x{h}", flush=True)
+    torch.manual_seed(tokens)
+    ids = torch.randint(0, rows - 1, (tokens,), device="cuda")
+    dy = torch.randint(-4, 5, (tokens, h), device="cuda", dtype=torch.int8).bfloat16()
+    dtable = torch.full((rows, h), float("nan"), device="cuda")
+    scratch = torch.empty(max(B.embedding_scratch_bytes(tokens, h), 1), dtype=torch.uint8, device="cuda")
+    B.embedding_bwd(ids, dy, dtable, scratch)
+    torch.cuda.synchronize()
+    for r in range(rows):
+        assert torch.equal(dtable[r], dy[ids == r].float().sum(0))
+    table = dtable.bfloat16()
+    y = torch.empty_like(dy)
+    B.embedding_fwd(ids, table, y)
+    torch.cuda.synchronize()
+    assert torch.equal(y, table[ids])
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("tokens,n_out,n_in", [(3, 8, 1 << 20), (3, 1 << 20, 32), (130, 264, 1 << 18), (130, 1 << 18, 96)])
+def test_weight_gradient_of_the_widest_layers(dtype, tokens, n_out, n_in):
+    torch = need_gpu()
+    print(f"[act8 dw] {dtype} {tokens} tokens, {n_out} x {n_in}", flush=True)
+    torch.manual_seed(tokens)
+    dt = getattr(torch, dtype)
+    x = torch.randint(-8, 9, (tokens, n_in), device="cuda").to(dt)
+    dy = torch.randint(-4, 5, (tokens, n_out), device="cuda").to(dt)
+    q, s = torch.empty((tokens, n_in), dtype=torch.uint8, device="cuda"), torch.empty((tokens, n_in // 32), dtype=torch.uint8,
+                                                                                     device="cuda")
+    B.act8_save(x, q, s)
+    scratch = torch.empty(max(B.act8_gemm_dw_scratch_bytes(dt, tokens, n_out, n_in), 1), dtype=torch.uint8, device="cuda")
+    dw = torch.full((n_out, n_in), float("nan"), device="cuda")
+    B.act8_gemm_dw(dy, q, s, dw, scratch)
+    torch.cuda.synchronize()
+    assert torch.equal(dw, torch.mm(dy.float().t().contiguous(), x.float()))  # integers: exact
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("tokens,q,kv,d", [(1, 4096, 4096, 256), (3, 4096, 1, 8), (2, 1, 4096, 64)])
+def test_qk_of_the_most_heads(dtype, tokens, q, kv, d):
+    G.test_qk_norm_rope(dtype, tokens, q, kv, d, d // 16 * 16, False, True)
