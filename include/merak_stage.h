@@ -578,6 +578,92 @@ size_t merak_act8_gemm_dw_scratch_bytes(int dtype, int tokens, int n_out, int n_
 int merak_act8_gemm_dw(int dtype, int tokens, int n_out, int n_in, const void* dy, const uint8_t* q,
                        const uint8_t* scales, float* dw, int accumulate, void* scratch, void* stream);
 
+/* Residual addition and root-mean-square norm of the sum, row by row of [rows, cols]:
+ *   sum = x + resid, rounded to dtype;  y = gamma * sum / sqrt(mean(sum^2) + eps)
+ * Without resid (NULL) the norm is x's.  Each output may be NULL, but not all of y, q and
+ * scales:
+ *   sum        [rows, cols] of dtype: the residual stream, and what the gradient needs (with
+ *              resid only; without it that is x).  May be x or resid itself.
+ *   y          [rows, cols] of dtype
+ *   q, scales  y as an activation checkpoint in 8 bits (above; cols % 32 == 0), taken from
+ *              the unrounded y: what merak_act8_gemm_dw reads as its X.
+ * Squares are summed in fp32: magnitudes above 2^63 overflow (y is then 0).  cols % 8 == 0, at
+ * most 32768 (else MERAK_ERR_UNSUPPORTED); rows at most 2^30; eps > 0; with q rows * cols at
+ * most 2^40. */
+int merak_add_rms_norm_fwd(int dtype, int rows, int cols, float eps, const void* x, const void* resid,
+                           const void* gamma, void* sum, void* y, uint8_t* q, uint8_t* scales, void* stream);
+
+/* Its gradient, from the gradient dy of y, the gradient dsum that reaches the sum from its other
+ * readers (NULL: none) and the sum itself: dx = dsum + (the norm's gradient), which is the
+ * gradient of x and of resid, and dgamma fp32 [cols], summed over the rows and written
+ * (accumulate = 0) or added (accumulate = 1).  dx may be dy or dsum itself.  scratch: fp32,
+ * merak_add_rms_norm_scratch_elems(rows, cols) elements (may be NULL when that is 0). */
+size_t merak_add_rms_norm_scratch_elems(int rows, int cols);
+int merak_add_rms_norm_bwd(int dtype, int rows, int cols, float eps, const void* dy, const void* dsum,
+                           const void* sum, const void* gamma, void* dx, float* dgamma, int accumulate,
+                           float* scratch, void* stream);
+
+/* Loss of a student that learns from a teacher's largest logits and from labels.  For each
+ * token, with the student's logits z over the vocabulary, the teacher's entries (id_k, t_k), a
+ * label c, the temperature T and the weight alpha:
+ *   p = softmax(t / T) over the token's entries (its own normalisation, whatever the teacher's
+ *       other logits are)
+ *   loss = alpha T^2 sum_k p_k (log p_k - log softmax(z / T)[id_k])
+ *          - (1 - alpha) log softmax(z)[c]
+ *   logits          [tokens, ld] of dtype, the first `vocab` columns of a row (ld % 8 == 0, at
+ *                   most 2^28; the columns behind them are not used)
+ *   teacher_ids     [tokens, top] of id_type (merak_id_type); an id outside 0 ..
+ *                   vocab_total - 1, such as -1, is no entry; ids may repeat (their p add up)
+ *   teacher_logits  [tokens, top] of teacher_dtype (merak_dtype), in any order; -infinity is
+ *                   no entry
+ *   labels          [tokens] of label_type; a label outside 0 .. vocab_total - 1, such as
+ *                   -100, adds no label term
+ * top is at most 1024.  With top = 0 or alpha = 0 there is no teacher term (its arrays may be
+ * NULL and are not read), with labels NULL or alpha = 1 no label term; one of them must be
+ * there.  0 <= alpha <= 1, T > 0.  A token without entry and label has the loss 0, and a
+ * gradient of zeros, whatever its logits are.  A logit of -infinity has the probability 0; a
+ * NaN or +infinity makes its token's loss and gradient NaN, as does a row of -infinity only.
+ *
+ * The logits may be one tensor-parallel rank's share, the columns first_id .. first_id + vocab
+ * - 1 of vocab_total; entries and labels are the whole vocabulary's, the same on every rank.
+ * The call then gives the share's statistics, stats fp32 [tokens, 8], which
+ * merak_distill_loss_join turns into the whole vocabulary's and the loss.
+ *   stats  NULL: not wanted.  Per token: maximum m of the logits; sum of exp(z - m) and of
+ *          exp((z - m) / T) (0 where the loss does not need it); the share's part of the loss
+ *          that is linear in z - m; teacher's mass and labels in the share; maximum of t and
+ *          sum of exp((t - max) / T).
+ *   loss   fp32 [tokens]; NULL if vocab < vocab_total. */
+int merak_distill_loss_fwd(int dtype, int tokens, int vocab, int ld, int64_t first_id, int64_t vocab_total,
+                           int top, int id_type, int teacher_dtype, int label_type, float alpha,
+                           float temperature, const void* logits, const void* teacher_ids,
+                           const void* teacher_logits, const void* labels, float* stats, float* loss,
+                           void* stream);
+
+/* The ranks' statistics, parts [ranks, tokens, 8] in the order of the ranks, as the whole
+ * vocabulary's: stats [tokens, 8], which every rank's gradient needs, and loss [tokens].  alpha
+ * and temperature as in the calls that made them; at most 2^16 ranks. */
+int merak_distill_loss_join(int tokens, int ranks, float alpha, float temperature, const float* parts,
+                            float* stats, float* loss, void* stream);
+
+/* Gradient of the logits (of a rank's share of them) from the whole vocabulary's stats (joined,
+ * or of a call whose vocab is vocab_total) and the gradient dloss fp32 [tokens] of each token's
+ * loss; the other arguments as in the forward call.  dlogits [tokens, ld] of dtype may be logits
+ * itself.  Columns behind `vocab` get zeros, and so does the row of a token whose dloss is 0,
+ * whatever its logits are. */
+int merak_distill_loss_bwd(int dtype, int tokens, int vocab, int ld, int64_t first_id, int64_t vocab_total,
+                           int top, int id_type, int teacher_dtype, int label_type, float alpha,
+                           float temperature, const void* logits, const void* teacher_ids,
+                           const void* teacher_logits, const void* labels, const float* stats,
+                           const float* dloss, void* dlogits, void* stream);
+
+/* Loss and gradient in one call, over the whole vocabulary, where dloss is known before the
+ * loss (a training step's 1 / tokens, 0 for masked ones): the logits are read once. */
+int merak_distill_loss_fwd_bwd(int dtype, int tokens, int vocab, int ld, int top, int id_type,
+                               int teacher_dtype, int label_type, float alpha, float temperature,
+                               const void* logits, const void* teacher_ids, const void* teacher_logits,
+                               const void* labels, const float* dloss, float* loss, void* dlogits,
+                               void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -90,6 +90,13 @@ _SIGS = {
     "merak_act8_gelu_bwd": ([_I, _I, _I, _P, _P, _P, _P, _P, _P], _I),
     "merak_act8_gemm_dw_scratch_bytes": ([_I, _I, _I, _I], _SZ),
     "merak_act8_gemm_dw": ([_I, _I, _I, _I, _P, _P, _P, _P, _I, _P, _P], _I),
+    "merak_add_rms_norm_fwd": ([_I, _I, _I, _F, _P, _P, _P, _P, _P, _P, _P, _P], _I),
+    "merak_add_rms_norm_scratch_elems": ([_I, _I], _SZ),
+    "merak_add_rms_norm_bwd": ([_I, _I, _I, _F, _P, _P, _P, _P, _P, _P, _I, _P, _P], _I),
+    "merak_distill_loss_fwd": ([_I, _I, _I, _I, _L, _L, _I, _I, _I, _I, _F, _F, _P, _P, _P, _P, _P, _P, _P], _I),
+    "merak_distill_loss_join": ([_I, _I, _F, _F, _P, _P, _P, _P], _I),
+    "merak_distill_loss_bwd": ([_I, _I, _I, _I, _L, _L, _I, _I, _I, _I, _F, _F, _P, _P, _P, _P, _P, _P, _P, _P], _I),
+    "merak_distill_loss_fwd_bwd": ([_I, _I, _I, _I, _I, _I, _I, _I, _F, _F, _P, _P, _P, _P, _P, _P, _P, _P], _I),
 }
 
 
@@ -693,3 +700,184 @@ def act8_gemm_dw(dy, q, scales, dw, scratch=None, accumulate=False, stream=None)
     _call(what, "merak_act8_gemm_dw", (dt, tokens, n_out, n_in, dy.data_ptr(), q.data_ptr(), scales.data_ptr(),
                                        dw.data_ptr(), int(accumulate), sp), stream,
           "dy q scales dw scratch", dy, q, scales, dw, scratch)
+
+
+def _norm_rows(what, x, gamma) -> tuple:
+    """(element type, rows, cols) of a row norm's input."""
+    dt = _element(what, x, gamma)
+    cols, n = gamma.numel(), x.numel()
+    if x.dim() == 0 or cols <= 0 or x.shape[-1] != cols:
+        raise ValueError(f"{what}: gamma holds one row's features")
+    rows = n // cols
+    if (rows | cols) > _INT:
+        _too_large(what, rows=rows, cols=cols)
+    return dt, rows, cols
+
+
+def _same(what, x, names, *tensors) -> None:
+    for t in tensors:
+        if t is not None and (t.dtype is not x.dtype or t.numel() != x.numel() or t.shape[-1] != x.shape[-1]):
+            raise ValueError(f"{what}: {names}")
+
+
+def add_rms_norm_fwd(x, gamma, y=None, resid=None, sum=None, q=None, scales=None, eps=1e-6, stream=None) -> None:
+    """sum = x + resid (kept in x's type; may be x or resid itself) and its root-mean-square norm
+    with the gain gamma [cols]: y in x's type, q and scales uint8 as an activation checkpoint in 8
+    bits, or both.  Without resid the norm is x's."""
+    what = "add_rms_norm_fwd"
+    dt, rows, cols = _norm_rows(what, x, gamma)
+    _same(what, x, "resid, sum and y have x's type and shape", resid, sum, y)
+    if (q is None) != (scales is None):
+        raise ValueError(f"{what}: q and scales go together")
+    if q is not None:
+        if _act8(what, q, scales) != (rows, cols):
+            raise ValueError(f"{what}: q has x's shape")
+    elif y is None:
+        raise ValueError(f"{what}: y, or q and scales, needed")
+    if sum is not None and resid is None:
+        raise ValueError(f"{what}: without resid there is no sum to keep")
+    _call(what, "merak_add_rms_norm_fwd", (dt, rows, cols, eps, x.data_ptr(), _ptr(resid), gamma.data_ptr(), _ptr(sum),
+                                           _ptr(y), _ptr(q), _ptr(scales)), stream,
+          "x resid gamma sum y q scales", x, resid, gamma, sum, y, q, scales)
+
+
+@functools.lru_cache(maxsize=256)
+def add_rms_norm_scratch_elems(rows: int, cols: int) -> int:
+    if max(abs(rows), abs(cols)) > _INT:
+        _too_large("add_rms_norm_scratch_elems", rows=rows, cols=cols)
+    return int(lib().merak_add_rms_norm_scratch_elems(rows, cols))
+
+
+def add_rms_norm_bwd(dy, sum, gamma, dx, dgamma, scratch=None, dsum=None, eps=1e-6, accumulate=False,
+                     stream=None) -> None:
+    """Gradient of add_rms_norm_fwd from its sum (x, without a residual): dx (dy or dsum itself, or
+    another tensor), the gradient of x and of resid, with dsum, the gradient that reaches the sum
+    from elsewhere, added; and the gain's fp32 gradient, written or added."""
+    torch = _torch or _load_torch()
+    what = "add_rms_norm_bwd"
+    dt, rows, cols = _norm_rows(what, sum, gamma)
+    _same(what, sum, "dy, dsum and dx have the sum's type and shape", dy, dsum, dx)
+    if dgamma.dtype is not torch.float32 or dgamma.numel() != cols:
+        raise ValueError(f"{what}: dgamma is fp32 [cols]")
+    sp = _scratch(what, scratch, 4 * add_rms_norm_scratch_elems(rows, cols))
+    _call(what, "merak_add_rms_norm_bwd", (dt, rows, cols, eps, dy.data_ptr(), _ptr(dsum), sum.data_ptr(),
+                                           gamma.data_ptr(), dx.data_ptr(), dgamma.data_ptr(), int(accumulate), sp),
+          stream, "dy dsum sum gamma dx dgamma scratch", dy, dsum, sum, gamma, dx, dgamma, scratch)
+
+
+DISTILL_STATS = 8  # floats of a token's statistics
+
+
+def _distill(what, logits, teacher_ids, teacher_logits, labels, vocab):
+    """(element type, tokens, vocab, ld), (top, id type, teacher's type, label type) of a loss."""
+    dt = _element(what, logits)
+    if logits.dim() == 0:
+        raise ValueError(f"{what}: logits is [tokens, columns]")
+    ld, n = logits.shape[-1], logits.numel()
+    tokens = n // ld if ld else 0
+    vocab = ld if vocab is None else vocab
+    if not 0 <= vocab <= ld:
+        raise ValueError(f"{what}: vocab is at most the logits' columns")
+    if (teacher_ids is None) != (teacher_logits is None):
+        raise ValueError(f"{what}: teacher_ids and teacher_logits go together")
+    top = it = tt = lt = 0
+    if teacher_ids is not None:
+        it, tt = _id_type(what, teacher_ids), _element(what, teacher_logits)
+        count = teacher_ids.numel()
+        top = count // tokens if tokens else 0
+        if teacher_logits.numel() != count or count != top * tokens or (
+                count and (teacher_ids.shape[-1] != top or teacher_logits.shape[-1] != top)):
+            raise ValueError(f"{what}: teacher_ids and teacher_logits are [tokens, top]")
+    if labels is not None:
+        lt = _id_type(what, labels)
+        if labels.numel() != tokens:
+            raise ValueError(f"{what}: labels has one id for each token")
+    if (tokens | ld | top) > _INT:
+        _too_large(what, tokens=tokens, columns=ld, top=top)
+    return (dt, tokens, vocab, ld), (top, it, tt, lt)
+
+
+def _share(what, vocab: int, first_id: int, vocab_total) -> tuple:
+    """(first id, ids of the whole vocabulary) of a rank's columns."""
+    total = vocab if vocab_total is None else vocab_total
+    if not (-1 << 63 <= first_id < 1 << 63 and -1 << 63 <= total < 1 << 63):
+        _too_large(what, first_id=first_id, vocab_total=total)
+    return first_id, total
+
+
+def _per_token(what, tokens: int, **tensors) -> None:
+    torch = _torch or _load_torch()
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        wide = DISTILL_STATS if name == "stats" else 1
+        if t.dtype is not torch.float32 or t.numel() != tokens * wide or (wide > 1 and t.shape[-1] != wide):
+            raise ValueError(f"{what}: {name} is fp32 [tokens{', 8' if wide > 1 else ''}]")
+
+
+def distill_loss_fwd(logits, stats=None, loss=None, teacher_ids=None, teacher_logits=None, labels=None, alpha=0.5,
+                     temperature=1.0, vocab=None, first_id=0, vocab_total=None, stream=None) -> None:
+    """Loss of each token, fp32: alpha times the divergence of the student's logits from a teacher's
+    entries (teacher_ids and teacher_logits [.., top]) at a temperature, and 1 - alpha times the
+    cross entropy of its label.  logits [.., columns], of which the first `vocab` (default: all)
+    count.  On a rank's share, the columns from first_id on of vocab_total, there are only the
+    statistics (stats fp32 [.., 8]), for distill_loss_join."""
+    what = "distill_loss_fwd"
+    head, tail = _distill(what, logits, teacher_ids, teacher_logits, labels, vocab)
+    share = _share(what, head[2], first_id, vocab_total)
+    _per_token(what, head[1], stats=stats, loss=loss)
+    if stats is None and loss is None:
+        raise ValueError(f"{what}: stats or loss needed")
+    if loss is not None and share != (0, head[2]):
+        raise ValueError(f"{what}: a share of the vocabulary has no loss of its own")
+    _call(what, "merak_distill_loss_fwd", (*head, *share, *tail, alpha, temperature, logits.data_ptr(),
+                                           _ptr(teacher_ids), _ptr(teacher_logits), _ptr(labels), _ptr(stats),
+                                           _ptr(loss)), stream,
+          "logits teacher_ids teacher_logits labels stats loss", logits, teacher_ids, teacher_logits, labels, stats,
+          loss)
+
+
+def distill_loss_join(parts, stats, loss, alpha=0.5, temperature=1.0, stream=None) -> None:
+    """The ranks' statistics, parts [ranks, .., 8], as the whole vocabulary's stats [.., 8], and
+    the loss of each token."""
+    what = "distill_loss_join"
+    tokens, ranks = loss.numel(), parts.shape[0] if parts.dim() else 0
+    _per_token(what, tokens, stats=stats, loss=loss)
+    if parts.dtype is not stats.dtype or parts.numel() != ranks * stats.numel() or parts.shape[-1] != DISTILL_STATS:
+        raise ValueError(f"{what}: parts is fp32 [ranks, tokens, 8]")
+    if (tokens | ranks) > _INT:
+        _too_large(what, tokens=tokens, ranks=ranks)
+    _call(what, "merak_distill_loss_join", (tokens, ranks, alpha, temperature, parts.data_ptr(), stats.data_ptr(),
+                                            loss.data_ptr()), stream, "parts stats loss", parts, stats, loss)
+
+
+def distill_loss_bwd(logits, stats, dloss, dlogits, teacher_ids=None, teacher_logits=None, labels=None, alpha=0.5,
+                     temperature=1.0, vocab=None, first_id=0, vocab_total=None, stream=None) -> None:
+    """Gradient of the logits (dlogits: logits itself or another tensor) from the whole vocabulary's
+    statistics and the gradient dloss fp32 of each token's loss; the rest as in the forward
+    call.  Columns behind `vocab` get zeros."""
+    what = "distill_loss_bwd"
+    head, tail = _distill(what, logits, teacher_ids, teacher_logits, labels, vocab)
+    share = _share(what, head[2], first_id, vocab_total)
+    _per_token(what, head[1], stats=stats, dloss=dloss)
+    _same(what, logits, "dlogits has the logits' type and shape", dlogits)
+    _call(what, "merak_distill_loss_bwd", (*head, *share, *tail, alpha, temperature, logits.data_ptr(),
+                                           _ptr(teacher_ids), _ptr(teacher_logits), _ptr(labels), stats.data_ptr(),
+                                           dloss.data_ptr(), dlogits.data_ptr()), stream,
+          "logits teacher_ids teacher_logits labels stats dloss dlogits", logits, teacher_ids, teacher_logits, labels,
+          stats, dloss, dlogits)
+
+
+def distill_loss_fwd_bwd(logits, dloss, loss, dlogits, teacher_ids=None, teacher_logits=None, labels=None, alpha=0.5,
+                         temperature=1.0, vocab=None, stream=None) -> None:
+    """Loss and gradient in one pass over the logits of the whole vocabulary, where dloss fp32 (each
+    token's weight in the step) is known before the loss.  dlogits may be logits itself."""
+    what = "distill_loss_fwd_bwd"
+    head, tail = _distill(what, logits, teacher_ids, teacher_logits, labels, vocab)
+    _per_token(what, head[1], dloss=dloss, loss=loss)
+    _same(what, logits, "dlogits has the logits' type and shape", dlogits)
+    _call(what, "merak_distill_loss_fwd_bwd", (*head, *tail, alpha, temperature, logits.data_ptr(), _ptr(teacher_ids),
+                                               _ptr(teacher_logits), _ptr(labels), dloss.data_ptr(), loss.data_ptr(),
+                                               dlogits.data_ptr()), stream,
+          "logits teacher_ids teacher_logits labels dloss loss dlogits", logits, teacher_ids, teacher_logits, labels,
+          dloss, loss, dlogits)

@@ -18,7 +18,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libmerak_stage.so")
 SOURCES = ("gemm.hip", "attention.hip", "attention_d128.hip", "norm.hip", "embedding.hip", "qk_norm_rope.hip",
-           "act8.hip", "stage.cpp", "operators.cpp", "graph_shard.cpp")
+           "act8.hip", "rms_norm.hip", "distill.hip", "stage.cpp", "operators.cpp", "graph_shard.cpp")
 
 ARCH = "gfx950"
 # Packed fp32 instructions are kept out of every code object.

@@ -183,4 +183,33 @@ size_t act8_gemm_dw_scratch_bytes(int dtype, int tokens, int n_out, int n_in);
 hipError_t launch_act8_gemm_dw(int dtype, int tokens, int n_out, int n_in, const void* dy, const uint8_t* q,
                                const uint8_t* scales, float* dw, int accumulate, void* scratch, hipStream_t stream);
 
+// Residual addition and RMS norm of the sum (rms_norm.hip): r, sum, y and q with scales may be
+// null.  The gradient's scratch: add_rms_norm_scratch_elems floats.
+constexpr int kMaxNormCols = 32768;
+hipError_t launch_add_rms_norm_fwd(int dtype, int rows, int cols, float eps, const void* x, const void* r,
+                                   const void* g, void* sum, void* y, uint8_t* q, uint8_t* scales, hipStream_t stream);
+size_t add_rms_norm_scratch_elems(int rows, int cols);
+hipError_t launch_add_rms_norm_bwd(int dtype, int rows, int cols, float eps, const void* dy, const void* ds,
+                                   const void* h, const void* g, void* dx, float* dg, int accumulate, float* scratch,
+                                   hipStream_t stream);
+
+// Distillation loss and its gradient (distill.hip) on a rank's columns
+// [first, first + vocab) of a vocabulary of `total`; rows of ld columns.
+constexpr int kDistillStats = 8;  // floats of a token's statistics
+constexpr int kMaxTop = 1024;     // teacher's entries of a token
+struct DistillShape {
+  int tokens, vocab, ld, top;
+  long long first, total;
+  int id_type, teacher_type, label_type;
+  float alpha, tau;
+  const void *ids, *teacher, *labels;
+};
+// Statistics and loss (either may be null); with dz the gradient too.
+hipError_t launch_distill(int dtype, const DistillShape& q, const void* z, float* stats, float* loss,
+                          const float* dloss, void* dz, hipStream_t stream);
+hipError_t launch_distill_join(int tokens, int ranks, float alpha, float tau, const float* parts, float* stats,
+                               float* loss, hipStream_t stream);
+hipError_t launch_distill_bwd(int dtype, const DistillShape& q, const void* z, const float* stats, const float* dloss,
+                              void* dz, hipStream_t stream);
+
 }  // namespace merak

@@ -1,5 +1,6 @@
 // C entry points of the operators around the blocks (include/merak_stage.h):
-// embedding, query/key norm with rotation, 8-bit activation checkpoints.
+// embedding, query/key norm with rotation, 8-bit activation checkpoints, residual norm,
+// distillation loss.
 // Arguments are checked here, before anything is enqueued.
 #include <cmath>
 #include <initializer_list>
@@ -95,6 +96,47 @@ int check_act8(int dtype, int rows, int cols, const uint8_t* q, const uint8_t* s
   TRY(check_ptr(q));
   return check_ptr(scales);
 }
+
+int check_norm(int dtype, int rows, int cols, float eps) {
+  TRY(check_dtype(dtype));
+  if (rows <= 0 || rows > kMaxRows || cols <= 0 || cols % 8) return MERAK_ERR_SHAPE;
+  if (cols > kMaxNormCols) return MERAK_ERR_UNSUPPORTED;
+  return eps > 0.0f && std::isfinite(eps) ? MERAK_OK : MERAK_ERR_SHAPE;
+}
+
+int check_mix(float alpha, float tau) {
+  if (!(alpha >= 0.0f && alpha <= 1.0f) || !(tau > 0.0f) || !std::isfinite(tau)) return MERAK_ERR_INVALID_ARG;
+  return MERAK_OK;
+}
+
+int check_id_type(int t) { return t == MERAK_I32 || t == MERAK_I64 ? MERAK_OK : MERAK_ERR_INVALID_ARG; }
+
+int check_distill(int dtype, const DistillShape& q, const void* logits) {
+  TRY(check_dtype(dtype));
+  TRY(check_mix(q.alpha, q.tau));
+  if (q.tokens <= 0 || q.tokens > kMaxRows || q.vocab <= 0 || q.ld < q.vocab || q.ld % 8 || q.ld > (1 << 28) ||
+      q.top < 0 || q.top > kMaxTop)
+    return MERAK_ERR_SHAPE;
+  if (q.first < 0 || q.total < q.vocab || q.first > q.total - q.vocab) return MERAK_ERR_INVALID_ARG;
+  TRY(check_ptr(logits));
+  if (q.top > 0) {
+    TRY(check_id_type(q.id_type));
+    TRY(check_dtype(q.teacher_type));
+    TRY(check_ptr(q.ids)); TRY(check_ptr(q.teacher));
+  }
+  if (q.labels) {
+    TRY(check_id_type(q.label_type));
+    TRY(check_ptr(q.labels));
+  }
+  const bool teacher = q.top > 0 && q.alpha > 0.0f, labels = q.labels && q.alpha < 1.0f;
+  return teacher || labels ? MERAK_OK : MERAK_ERR_INVALID_ARG;  // else nothing to learn from
+}
+
+size_t logits_bytes(int dtype, const DistillShape& q) { return (size_t)q.tokens * q.ld * elem(dtype); }
+size_t stats_bytes(int tokens) { return (size_t)tokens * kDistillStats * sizeof(float); }
+Span ids_span(const DistillShape& q) { return {q.ids, (size_t)q.tokens * q.top * id_bytes(q.id_type)}; }
+Span teacher_span(const DistillShape& q) { return {q.teacher, (size_t)q.tokens * q.top * elem(q.teacher_type)}; }
+Span labels_span(const DistillShape& q) { return {q.labels, (size_t)q.tokens * id_bytes(q.label_type)}; }
 
 }  // namespace
 
@@ -228,6 +270,103 @@ int merak_act8_gemm_dw(int dtype, int tokens, int n_out, int n_in, const void* d
                   {{dy, (size_t)tokens * n_out * elem(dtype)}, {q, n}, {scales, n / 32}}));
   LAUNCH_TRY(launch_act8_gemm_dw(dtype, tokens, n_out, n_in, dy, q, scales, dw, accumulate, scratch,
                                  (hipStream_t)stream));
+  return MERAK_OK;
+}
+
+int merak_add_rms_norm_fwd(int dtype, int rows, int cols, float eps, const void* x, const void* resid,
+                           const void* gamma, void* sum, void* y, uint8_t* q, uint8_t* scales, void* stream) {
+  TRY(check_norm(dtype, rows, cols, eps));
+  TRY(check_ptr(x)); TRY(check_ptr(gamma));
+  if (resid) TRY(check_ptr(resid));
+  if (!resid && sum) return MERAK_ERR_INVALID_ARG;
+  if (sum) TRY(check_ptr(sum));
+  if ((!y && !q) || !q != !scales) return MERAK_ERR_INVALID_ARG;
+  if (y) TRY(check_ptr(y));
+  const size_t n = (size_t)rows * cols, nb = n * elem(dtype);
+  if (q) TRY(check_act8(dtype, rows, cols, q, scales));
+  TRY(check_apart({{sum, nb}, {y, nb}, {q, n}, {scales, n / 32}},
+                  {{sum == x ? nullptr : x, nb}, {sum == resid ? nullptr : resid, nb}, {gamma, cols * elem(dtype)}}));
+  LAUNCH_TRY(launch_add_rms_norm_fwd(dtype, rows, cols, eps, x, resid, gamma, sum, y, q, scales, (hipStream_t)stream));
+  return MERAK_OK;
+}
+
+size_t merak_add_rms_norm_scratch_elems(int rows, int cols) {
+  if (rows <= 0 || cols <= 0) return 0;
+  return add_rms_norm_scratch_elems(rows, cols);
+}
+
+int merak_add_rms_norm_bwd(int dtype, int rows, int cols, float eps, const void* dy, const void* dsum, const void* sum,
+                           const void* gamma, void* dx, float* dgamma, int accumulate, float* scratch, void* stream) {
+  TRY(check_norm(dtype, rows, cols, eps));
+  TRY(check_flag(accumulate));
+  TRY(check_ptr(dy)); TRY(check_ptr(sum)); TRY(check_ptr(gamma)); TRY(check_ptr(dx)); TRY(check_ptr(dgamma));
+  if (dsum) TRY(check_ptr(dsum));
+  const size_t se = add_rms_norm_scratch_elems(rows, cols);
+  if (se > 0) TRY(check_ptr(scratch));
+  const size_t nb = (size_t)rows * cols * elem(dtype);
+  TRY(check_apart({{dx, nb}, {dgamma, cols * sizeof(float)}, {scratch, se * sizeof(float)}},
+                  {{dx == dy ? nullptr : dy, nb}, {dx == dsum ? nullptr : dsum, nb}, {sum, nb},
+                   {gamma, cols * elem(dtype)}}));
+  LAUNCH_TRY(launch_add_rms_norm_bwd(dtype, rows, cols, eps, dy, dsum, sum, gamma, dx, dgamma, accumulate, scratch,
+                                     (hipStream_t)stream));
+  return MERAK_OK;
+}
+
+int merak_distill_loss_fwd(int dtype, int tokens, int vocab, int ld, int64_t first_id, int64_t vocab_total, int top,
+                           int id_type, int teacher_dtype, int label_type, float alpha, float temperature,
+                           const void* logits, const void* teacher_ids, const void* teacher_logits, const void* labels,
+                           float* stats, float* loss, void* stream) {
+  const DistillShape q{tokens, vocab, ld, top, first_id, vocab_total, id_type, teacher_dtype, label_type, alpha,
+                       temperature, teacher_ids, teacher_logits, labels};
+  TRY(check_distill(dtype, q, logits));
+  if (!stats && !loss) return MERAK_ERR_INVALID_ARG;
+  if (loss && vocab != vocab_total) return MERAK_ERR_INVALID_ARG;  // a share has no loss of its own
+  if (stats) TRY(check_ptr(stats));
+  if (loss) TRY(check_ptr(loss));
+  TRY(check_apart({{stats, stats_bytes(tokens)}, {loss, tokens * sizeof(float)}},
+                  {{logits, logits_bytes(dtype, q)}, ids_span(q), teacher_span(q), labels_span(q)}));
+  LAUNCH_TRY(launch_distill(dtype, q, logits, stats, loss, nullptr, nullptr, (hipStream_t)stream));
+  return MERAK_OK;
+}
+
+int merak_distill_loss_join(int tokens, int ranks, float alpha, float temperature, const float* parts, float* stats,
+                            float* loss, void* stream) {
+  TRY(check_mix(alpha, temperature));
+  if (tokens <= 0 || tokens > kMaxRows || ranks <= 0 || ranks > (1 << 16)) return MERAK_ERR_SHAPE;
+  TRY(check_ptr(parts)); TRY(check_ptr(stats)); TRY(check_ptr(loss));
+  TRY(check_apart({{stats, stats_bytes(tokens)}, {loss, tokens * sizeof(float)}}, {{parts, ranks * stats_bytes(tokens)}}));
+  LAUNCH_TRY(launch_distill_join(tokens, ranks, alpha, temperature, parts, stats, loss, (hipStream_t)stream));
+  return MERAK_OK;
+}
+
+int merak_distill_loss_bwd(int dtype, int tokens, int vocab, int ld, int64_t first_id, int64_t vocab_total, int top,
+                           int id_type, int teacher_dtype, int label_type, float alpha, float temperature,
+                           const void* logits, const void* teacher_ids, const void* teacher_logits, const void* labels,
+                           const float* stats, const float* dloss, void* dlogits, void* stream) {
+  const DistillShape q{tokens, vocab, ld, top, first_id, vocab_total, id_type, teacher_dtype, label_type, alpha,
+                       temperature, teacher_ids, teacher_logits, labels};
+  TRY(check_distill(dtype, q, logits));
+  TRY(check_ptr(stats)); TRY(check_ptr(dloss)); TRY(check_ptr(dlogits));
+  const size_t nb = logits_bytes(dtype, q);
+  TRY(check_apart({{dlogits, nb}}, {{dlogits == logits ? nullptr : logits, nb}, ids_span(q), teacher_span(q),
+                                    labels_span(q), {stats, stats_bytes(tokens)}, {dloss, tokens * sizeof(float)}}));
+  LAUNCH_TRY(launch_distill_bwd(dtype, q, logits, stats, dloss, dlogits, (hipStream_t)stream));
+  return MERAK_OK;
+}
+
+int merak_distill_loss_fwd_bwd(int dtype, int tokens, int vocab, int ld, int top, int id_type, int teacher_dtype,
+                               int label_type, float alpha, float temperature, const void* logits,
+                               const void* teacher_ids, const void* teacher_logits, const void* labels,
+                               const float* dloss, float* loss, void* dlogits, void* stream) {
+  const DistillShape q{tokens, vocab, ld, top, 0, vocab, id_type, teacher_dtype, label_type, alpha, temperature,
+                       teacher_ids, teacher_logits, labels};
+  TRY(check_distill(dtype, q, logits));
+  TRY(check_ptr(dloss)); TRY(check_ptr(loss)); TRY(check_ptr(dlogits));
+  const size_t nb = logits_bytes(dtype, q);
+  TRY(check_apart({{dlogits, nb}, {loss, tokens * sizeof(float)}},
+                  {{dlogits == logits ? nullptr : logits, nb}, ids_span(q), teacher_span(q), labels_span(q),
+                   {dloss, tokens * sizeof(float)}}));
+  LAUNCH_TRY(launch_distill(dtype, q, logits, nullptr, loss, dloss, dlogits, (hipStream_t)stream));
   return MERAK_OK;
 }
 
