@@ -133,3 +133,64 @@ def gelu_parts(u):
     near, far = 1.0 / (1.0 + e), e / (1.0 + e)
     s, t = np.where(z2 >= 0, near, far), np.where(z2 >= 0, far, near)
     return u * s, s + u * s * t * 2.0 * c * (1.0 + 3.0 * a * u * u)
+
+
+# -- residual addition and root-mean-square norm --------------------------------
+
+def rms_norm(h, gamma, eps=1e-6):
+    """gamma * h / sqrt(mean(h^2) + eps) of each row."""
+    return gamma * h / np.sqrt((h * h).mean(-1, keepdims=True) + eps)
+
+
+def rms_norm_backward(dy, h, gamma, dsum=None, eps=1e-6):
+    """(gradient of h, of gamma, magnitudes that went into each): dsum is the gradient that
+    reaches h from elsewhere."""
+    rstd = 1.0 / np.sqrt((h * h).mean(-1, keepdims=True) + eps)
+    n, dn = h * rstd, dy * gamma
+    ds = np.zeros_like(h) if dsum is None else dsum
+    dx = ds + rstd * (dn - n * (dn * n).mean(-1, keepdims=True))
+    mag = np.abs(ds) + rstd * (np.abs(dn) + np.abs(n) * np.abs(dn * n).mean(-1, keepdims=True))
+    return dx, (dy * n).sum(0), mag, np.abs(dy * n).sum(0)
+
+
+# -- distillation from a teacher's top logits ---------------------------------
+
+def distill(z, ids=None, t=None, labels=None, alpha=0.5, tau=1.0, total=None):
+    """Loss of each token and its gradient by the logits z [tokens, vocab]; ids and t [tokens, top] are
+    the teacher's entries (ids outside the vocabulary are none), labels [tokens].  Third comes a
+    dict of what the tolerances need: the magnitudes that went into the loss, and the gradient's
+    positive and negative parts."""
+    z = np.asarray(z, dtype=np.float64)
+    tokens, vocab = z.shape
+    total = vocab if total is None else total
+    loss, grad, size = np.zeros(tokens), np.zeros_like(z), np.zeros(tokens)
+    plus, minus = np.zeros_like(z), np.zeros_like(z)
+
+    def log_softmax(v):
+        m = v.max()
+        with np.errstate(invalid="ignore"):
+            d = v - m
+        return d - np.log(np.exp(d).sum()), d
+
+    for i in range(tokens):
+        if ids is not None and alpha > 0:
+            keep = [(int(c), float(x)) for c, x in zip(ids[i], t[i]) if 0 <= c < total and x != -np.inf]
+            if keep:
+                x = np.array([x for _, x in keep]) / tau
+                lp, _ = log_softmax(x)
+                lq, d = log_softmax(z[i] / tau)
+                p, q = np.exp(lp), np.exp(lq)
+                cols = [c for c, _ in keep]
+                use = p > 0
+                loss[i] += alpha * tau ** 2 * (p[use] * (lp[use] - lq[cols][use])).sum()
+                size[i] += alpha * tau ** 2 * (p[use] * (np.abs(lp[use]) + np.abs(d[cols][use]) + 1)).sum()
+                plus[i] += alpha * tau * q
+                np.add.at(minus[i], cols, alpha * tau * p)
+        if labels is not None and alpha < 1 and 0 <= labels[i] < total:
+            lq, d = log_softmax(z[i])
+            loss[i] -= (1 - alpha) * lq[labels[i]]
+            size[i] += (1 - alpha) * (np.abs(d[labels[i]]) + 1)
+            plus[i] += (1 - alpha) * np.exp(lq)
+            minus[i, labels[i]] += 1 - alpha
+    grad = plus - minus
+    return loss, grad, {"loss": size, "plus": plus, "minus": minus}

@@ -16,13 +16,13 @@
 // statistics.  Ranks' rows join by moving to the largest m.
 //
 // Bound by memory: the logits are read once (maximum and sums in one pass, the sums rescaled
-// when the maximum grows), the gradient is written once.  Its columns with entries or the label
-// are then written once more, each by one thread that adds all that lies on it in the entries'
-// order, so nothing depends on timing and each value is rounded once.  Sums are fp32.
+// when the maximum grows), the gradient is written once.  Sums are fp32, each value of the gradient
+// is formed in fp32 and rounded once, nothing depends on timing.
 #include <algorithm>
 
 #include "common.h"
 #include "kernels.h"
+#include "wave.h"
 
 namespace merak {
 
@@ -35,9 +35,10 @@ struct DistillArgs {
   int tokens, vocab, ld, top;
   long long first, total;
   float alpha, tau;
-  float rate_t, rate_1;          // log2(e) / T, log2(e); with one sum (TWO = false) rate_t is its rate
+  float rate_t, rate_1;          // log2(e) / T, log2(e); with one sum rate_t is its rate
   bool want_t, want_1;           // sums that the loss needs
   bool id64, label64, teacher_bf16;
+  bool past;                     // the gradient is written past the caches
   const void* ids;               // [tokens][top], null without entries
   const void* teacher;
   const void* labels;            // null without labels
@@ -53,29 +54,33 @@ __device__ __forceinline__ int column_of(const DistillArgs& a, long long id) {
   return id >= 0 && id < a.total && c >= 0 && c < a.vocab ? (int)c : -1;
 }
 
-// The teacher's logit k of a token; -infinity for an entry that is not there.
-__device__ __forceinline__ float teacher_at(const DistillArgs& a, size_t i, long long id) {
-  const float t = a.teacher_bf16 ? bf2f(static_cast<const bf16_t*>(a.teacher)[i])
-                                 : static_cast<const float*>(a.teacher)[i];
-  return id >= 0 && id < a.total ? t : -INFINITY;
+__device__ __forceinline__ float teacher_at(const DistillArgs& a, size_t i) {
+  return a.teacher_bf16 ? bf2f(static_cast<const bf16_t*>(a.teacher)[i]) : static_cast<const float*>(a.teacher)[i];
 }
 
-// A token's entries and its label (entry `top`) in LDS.
+// A token's entries and its label (entry `top`) in LDS, with room for whole groups of four.  The
+// gradient's values at their columns go to the threads that write those columns' 16 bytes,
+// as a list for each thread.
 struct Entries {
   int* col;    // own column, or -1
-  float* t;    // teacher's logit; then weight in the gradient
-  float* z;    // student's logit at the column
+  float* t;    // teacher's logit; then exp((t - max) / T)
+  float* z;    // student's logit at the column; then the gradient there
+  int* next;   // the next entry of the thread, -1 at the end
+  int* head;   // [threads] the first one
 };
+__host__ __device__ constexpr int entry_room(int top) { return (top + 4) & ~3; }
+__host__ __device__ constexpr size_t entries_bytes(int top, int nt) { return (size_t)entry_room(top) * 16 + nt * 4; }
 __device__ __forceinline__ Entries entries_in(char* lds, int top) {
-  const int n = (top + 4) & ~3;  // whole groups of four
-  return Entries{reinterpret_cast<int*>(lds), reinterpret_cast<float*>(lds) + n, reinterpret_cast<float*>(lds) + 2 * n};
+  const int n = entry_room(top);
+  int* p = reinterpret_cast<int*>(lds);
+  return Entries{p, reinterpret_cast<float*>(p + n), reinterpret_cast<float*>(p + 2 * n), p + 3 * n, p + 4 * n};
 }
-static size_t entries_bytes(int top) { return (size_t)((top + 4) & ~3) * 12; }
 
-// 16 bytes of logits as floats.
+// 16 bytes of logits as floats; NONE is -infinity in each of them.
 template <typename T> struct Vec;
 template <> struct Vec<bf16_t> {
   static constexpr int N = 8;
+  static constexpr uint32_t NONE = 0xff80ff80u;
   static __device__ __forceinline__ void get(u32x4_t r, float (&v)[8]) { unpack8(r, v); }
   static __device__ __forceinline__ u32x4_t put(const float (&v)[8]) {
     return u32x4_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
@@ -83,6 +88,7 @@ template <> struct Vec<bf16_t> {
 };
 template <> struct Vec<float> {
   static constexpr int N = 4;
+  static constexpr uint32_t NONE = 0xff800000u;
   static __device__ __forceinline__ void get(u32x4_t r, float (&v)[4]) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(r[e]);
@@ -92,48 +98,25 @@ template <> struct Vec<float> {
   }
 };
 
+// The first `n` values of r, `rest` in the places of the others.
+template <typename T>
+__device__ __forceinline__ u32x4_t first_values(u32x4_t r, int n, float rest) {
+  float v[Vec<T>::N];
+  Vec<T>::get(r, v);
+#pragma unroll
+  for (int e = 0; e < Vec<T>::N; ++e) v[e] = e < n ? v[e] : rest;
+  return Vec<T>::put(v);
+}
+
 // What a maximum's differences are formed from: 0 where nothing was above -infinity.
 __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.0f : m; }
+
+// The same within 2^50 on both sides, where 2^(z rate - base rate) is formed in one step.
+__device__ __forceinline__ float near_base(float m) { return m == -INFINITY ? 0.0f : fminf(fmaxf(m, -0x1p50f), 0x1p50f); }
 
 // By how much sums relative to the maximum m move to those relative to `base` (sums that are 0
 // stay 0: the difference from a base far below 0 would have no finite exponential).
 __device__ __forceinline__ float moved(float m, float base) { return m == -INFINITY ? 0.0f : m - base; }
-
-template <int NT, int N>
-__device__ __forceinline__ void block_max(float (&v)[N], float* red) {
-  constexpr int W = NT / 64;
-#pragma unroll
-  for (int n = 0; n < N; ++n) v[n] = wave_max(v[n]);
-  if ((threadIdx.x & 63) == 0) {
-#pragma unroll
-    for (int n = 0; n < N; ++n) red[(threadIdx.x >> 6) * N + n] = v[n];
-  }
-  __syncthreads();
-#pragma unroll
-  for (int n = 0; n < N; ++n) {
-    v[n] = red[n];
-#pragma unroll
-    for (int w = 1; w < W; ++w) v[n] = fmaxf(v[n], red[w * N + n]);
-  }
-}
-
-template <int NT, int N>
-__device__ __forceinline__ void block_sum(float (&v)[N], float* red) {
-  constexpr int W = NT / 64;
-#pragma unroll
-  for (int n = 0; n < N; ++n) v[n] = wave_sum(v[n]);
-  if ((threadIdx.x & 63) == 0) {
-#pragma unroll
-    for (int n = 0; n < N; ++n) red[(threadIdx.x >> 6) * N + n] = v[n];
-  }
-  __syncthreads();
-#pragma unroll
-  for (int n = 0; n < N; ++n) {
-    v[n] = red[n];
-#pragma unroll
-    for (int w = 1; w < W; ++w) v[n] += red[w * N + n];
-  }
-}
 
 struct Stats {
   float m, s1, st, lin, mass, label, tm, ts;
@@ -155,35 +138,152 @@ __device__ __forceinline__ Stats load_stats(const float* p) {
   return Stats{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
 }
 
-// The gradient's factors of exp((z - m) / T) and exp(z - m); with one sum (TWO = false) the first
-// is the factor of both.
-template <bool TWO>
-__device__ __forceinline__ void factors(const DistillArgs& a, const Stats& s, float w, float* ft, float* f1) {
-  *ft = s.mass != 0.0f ? w * a.alpha * a.tau * s.mass / s.st : 0.0f;
-  *f1 = s.label != 0.0f ? w * (1.0f - a.alpha) * s.label / s.s1 : 0.0f;
-  if (!TWO) *ft += *f1;
+// exp((z - base) / T) as 2^(z rate - c), c = base * rate rounded: one fused step an element.  What c
+// is off by, the same for every z, is put back into the sum of them (`off`, a factor next to 1).
+struct Exponent {
+  float rate, c, base;
+  __device__ __forceinline__ Exponent(float base, float rate) : rate(rate), c(base * rate), base(base) {}
+  __device__ __forceinline__ float of(float z) const { return exp2_fast(fmaf(z, rate, -c)); }
+  __device__ __forceinline__ float off() const { return exp2_fast(fmaf(-base, rate, c)); }
+};
+
+// A maximum beyond 2^50, such as that of a row that is masked with the type's lowest value, would
+// leave the range on the way.  Any logit below it is so far below that its exponential is 0, at
+// every temperature (2^-10 to 2^10), so there 0 and -infinity stand for the maximum and the rest.
+constexpr float kFar = 0x1p50f;
+__device__ __forceinline__ bool is_far(float base) { return fabsf(base) > kFar && fabsf(base) < INFINITY; }
+__device__ __forceinline__ float near_logit(float z, float base) {
+  return z == base ? 0.0f : z != z ? z : -INFINITY;
 }
 
-template <bool TWO>
-__device__ __forceinline__ float slope(const DistillArgs& a, float z, float m, float ft, float f1) {
-  const float d = z - m;
-  float g = ft * exp2_fast(d * a.rate_t);
-  if (TWO) g += f1 * exp2_fast(d * a.rate_1);
-  return g;
-}
-
-// Columns [lo, hi) of a row: dz from z (the same memory, or another row's).
-template <typename T, int NT, bool TWO>
-__device__ __forceinline__ void write_slopes(const DistillArgs& a, const T* z, T* dz, int lo, int hi, float m, float ft,
-                                             float f1) {
-  constexpr int N = Vec<T>::N;
-  for (int c = lo + (int)threadIdx.x * N; c < hi; c += NT * N) {
-    float v[N];
-    Vec<T>::get(*reinterpret_cast<const u32x4_t*>(z + c), v);
+template <typename T>
+__device__ __forceinline__ u32x4_t near_logits(u32x4_t r, float base) {
+  float v[Vec<T>::N];
+  Vec<T>::get(r, v);
 #pragma unroll
-    for (int e = 0; e < N; ++e) v[e] = c + e < a.vocab ? slope<TWO>(a, v[e], m, ft, f1) : 0.0f;
-    *reinterpret_cast<u32x4_t*>(dz + c) = Vec<T>::put(v);
+  for (int e = 0; e < Vec<T>::N; ++e) v[e] = near_logit(v[e], base);
+  return Vec<T>::put(v);
+}
+
+// The two exponentials, exp((z - base) / T) and exp(z - base): ONE is enough where the loss needs
+// one or T = 1, at T = 2 and T = 4 the second is the first's square or its square's (their c and
+// off are exact multiples then), else there are TWO.  In bf16 the second one is a quarter of the
+// work: loss of 8192 x 50304 162 us with both, 147 so.
+enum Sums { ONE = 0, TWO = 1, SQUARE = 2, FOURTH = 4 };
+template <int M>
+struct Exponents {
+  Exponent t, one;
+  __device__ __forceinline__ Exponents(const DistillArgs& a, float base) : t(base, a.rate_t), one(base, a.rate_1) {}
+  __device__ __forceinline__ void of(float z, float* et, float* e1) const {
+    *et = t.of(z);
+    if (M == ONE) *e1 = *et;
+    else if (M == TWO) *e1 = one.of(z);
+    else if (M == SQUARE) *e1 = *et * *et;
+    else *e1 = (*et * *et) * (*et * *et);
   }
+};
+
+// The gradient's factors of the two exponentials (with one, `t` is that of both).
+template <int M>
+struct Slopes {
+  Exponents<M> exps;
+  float t, one;
+  __device__ __forceinline__ Slopes(const DistillArgs& a, const Stats& s, float w, bool far)
+      : exps(a, far ? 0.0f : base_of(s.m)) {
+    t = s.mass != 0.0f ? w * a.alpha * a.tau * s.mass / s.st : 0.0f;
+    one = s.label != 0.0f ? w * (1.0f - a.alpha) * s.label / s.s1 : 0.0f;
+    if (M == ONE) t += one;
+    t *= exps.t.off();
+    one *= exps.one.off();
+  }
+  __device__ __forceinline__ float of(float z) const {
+    float et, e1;
+    exps.of(z, &et, &e1);
+    if (M == ONE) return t * et;
+    if (M == SQUARE) return et * fmaf(one, et, t);
+    return fmaf(one, e1, t * et);
+  }
+};
+
+// 16 bytes of the gradient from those of the logits, of which `n` are columns of the vocabulary.
+template <typename T, int M>
+__device__ __forceinline__ u32x4_t slopes_of(const Slopes<M>& f, u32x4_t z, int n) {
+  constexpr int N = Vec<T>::N;
+  float v[N];
+  Vec<T>::get(z, v);
+#pragma unroll
+  for (int e = 0; e < N; ++e) v[e] = f.of(v[e]);
+  if (n < N) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = e < n ? v[e] : 0.0f;
+  }
+  return Vec<T>::put(v);
+}
+
+// Which of a thread's chunks (NT threads, from column lo on) have entries: bit i for chunk i, at most 32.
+template <typename T, int NT>
+__device__ __forceinline__ uint32_t chunks_with_entries(const Entries& en, int lo) {
+  uint32_t m = 0;
+  for (int k = en.head[threadIdx.x]; k >= 0; k = en.next[k]) m |= 1u << ((en.col[k] - lo) / (Vec<T>::N * NT));
+  return m;
+}
+
+// The thread's 16 bytes from column c on, with the entries' values in their places.
+__device__ __forceinline__ void put_value(u32x4_t& v, int e, float x, bf16_t) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (e == 2 * i) v[i] = (v[i] & 0xffff0000u) | f2bf(x);
+    if (e == 2 * i + 1) v[i] = (v[i] & 0xffffu) | (uint32_t)f2bf(x) << 16;
+  }
+}
+__device__ __forceinline__ void put_value(u32x4_t& v, int e, float x, float) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (e == i) v[i] = __float_as_uint(x);
+}
+template <typename T>
+__device__ __forceinline__ u32x4_t with_entries(const Entries& en, u32x4_t v, int c) {
+  for (int k = en.head[threadIdx.x]; k >= 0; k = en.next[k]) put_value(v, en.col[k] - c, en.z[k], T());
+  return v;
+}
+
+// Columns [lo, hi) of a row: dz from z (the same memory, or another row's), U loads in flight.
+template <typename T, int NT, int M, bool FAR>
+__device__ __forceinline__ void write_slopes(const DistillArgs& a, const Slopes<M>& f, const Entries& en, const T* z,
+                                             T* dz, int lo, int hi, float base) {
+  constexpr int N = Vec<T>::N, U = 4;
+  for (int c0 = lo + (int)threadIdx.x * N; c0 < hi; c0 += NT * N * U) {
+    u32x4_t r[U] = {};
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (c0 + NT * N * u < hi) r[u] = *reinterpret_cast<const u32x4_t*>(z + c0 + NT * N * u);
+    if (FAR) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) r[u] = near_logits<T>(r[u], base);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int c = c0 + NT * N * u;
+      if (c < hi) *reinterpret_cast<u32x4_t*>(dz + c) = with_entries<T>(en, slopes_of<T, M>(f, r[u], a.vocab - c), c);
+    }
+  }
+}
+
+// Zeros behind the vocabulary in the 16 bytes that hold its end (where the row's factors are NaN
+// the -infinity there has become NaN too), by the thread that has written them.
+template <typename T, int NT>
+__device__ __forceinline__ void write_padding(const DistillArgs& a, T* dz, int lo) {
+  constexpr int N = Vec<T>::N;
+  if (a.vocab % N && (int)threadIdx.x == (a.vocab - lo) / N % NT)
+    for (int c = a.vocab; c % N; ++c) dz[c] = T(0);
+}
+
+// A thread's sum of exponentials where the maximum is far.
+template <typename T, int NT>
+__device__ __forceinline__ float far_sum(const DistillArgs& a, const T* z, float base) {
+  float s = 0.0f;
+  for (int c = threadIdx.x; c < a.vocab; c += NT) s += exp2_fast(near_logit(Elem<T>::to_f(z[c]), base));
+  return s;
 }
 
 template <typename T, int NT>
@@ -192,83 +292,73 @@ __device__ __forceinline__ void write_zeros(T* dz, int lo, int hi) {
     *reinterpret_cast<u32x4_t*>(dz + c) = u32x4_t{0, 0, 0, 0};
 }
 
-// The columns that have entries: each is written by its first entry's thread.
-template <typename T, int NT, bool TWO>
-__device__ __forceinline__ void write_entries(const DistillArgs& a, const Entries& en, T* dz, float m, float ft,
-                                              float f1) {
+// The gradient at the columns that have entries, each formed by its first entry's thread from all
+// that lies on it in the entries' order (columns are compared four at a time: 64 entries cost a
+// thread 16 LDS reads) and listed for the thread that writes the 16 bytes around it, which puts
+// it there.  A column's place in a list is the one thing that depends on timing, and it changes
+// nothing.  (Written by a store of its own behind that of the 16 bytes, each entry cost a part of
+// a line once more: loss and gradient of 32768 x 6288 with 64 entries 266 us, 201 so.)
+// wt: weight of exp((t - max) / T), wl: of the label.  A barrier follows.
+template <typename T, int NT, int M>
+__device__ __forceinline__ void resolve_entries(const DistillArgs& a, const Slopes<M>& f, const Entries& en, float wt,
+                                                float wl, int lo, bool far, float base) {
+  typedef int i32x4 __attribute__((ext_vector_type(4)));
   for (int e = threadIdx.x; e <= a.top; e += NT) {
     const int c = en.col[e];
     if (c < 0) continue;
-    float total = 0.0f;
+    float p = 0.0f, l = 0.0f;
     bool first = true;
-    for (int k = 0; k <= a.top; ++k)
-      if (en.col[k] == c) {
-        first = first && k >= e;
-        total += en.t[k];
-      }
-    if (first) dz[c] = Elem<T>::from_f(slope<TWO>(a, en.z[e], m, ft, f1) - total);
+    for (int k = 0; k <= a.top; k += 4) {
+      const i32x4 four = *reinterpret_cast<const i32x4*>(en.col + k);
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (four[u] == c) {
+          first = first && k + u >= e;
+          if (k + u < a.top) p += en.t[k + u];
+          else l = wl;
+        }
+    }
+    if (!first) continue;
+    const float z = en.z[e];
+    en.z[e] = f.of(far ? near_logit(z, base) : z) - (wt * p + l);
+    en.next[e] = atomicExch(&en.head[(c - lo) / Vec<T>::N % NT], e);
   }
 }
 
-// One workgroup a token: statistics, loss and, with GRAD, the gradient (a second look at the
-// row).
-template <typename T, int NT, bool TWO, bool GRAD>
-__global__ void __launch_bounds__(NT) distill_kernel(DistillArgs a, const T* z, float* __restrict__ stats,
-                                                     float* __restrict__ loss, const float* __restrict__ dloss, T* dz) {
-  extern __shared__ __align__(16) char smem[];
-  __shared__ float red[2][NT / 64 * 6];
-  const Entries en = entries_in(smem, a.top);
-  const size_t row = blockIdx.x;
-  const T* zr = z + row * a.ld;
+// Entry k of the token `row` into LDS, from its loaded id and logit; the teacher's logit for the
+// maximum.
+template <typename T>
+__device__ __forceinline__ float keep_entry(const DistillArgs& a, const Entries& en, const T* zr, int k, long long id,
+                                            float t) {
+  const int c = column_of(a, id);
+  if (id < 0 || id >= a.total) t = -INFINITY;
+  en.col[k] = c;
+  en.t[k] = t;
+  en.z[k] = c >= 0 ? Elem<T>::to_f(zr[c]) : 0.0f;
+  return t != t ? INFINITY : t;  // NaN: no probabilities
+}
 
-  // entries and label
-  float mx[2] = {-INFINITY, -INFINITY};  // of the student's logits, of the teacher's
-  for (int k = threadIdx.x; k < a.top; k += NT) {
-    const size_t i = row * a.top + k;
-    const long long id = id_at(a.ids, a.id64, i);
-    const int c = column_of(a, id);
-    const float t = teacher_at(a, i, id);
-    en.col[k] = c;
-    en.t[k] = t;
-    en.z[k] = c >= 0 ? Elem<T>::to_f(zr[c]) : 0.0f;
-    mx[1] = fmaxf(mx[1], t != t ? INFINITY : t);  // NaN: no probabilities
-  }
-  const long long label = a.labels ? id_at(a.labels, a.label64, row) : -1;
-  const bool labelled = label >= 0 && label < a.total;
+// The token's label as entry `top`, and no columns in the places behind it.
+template <typename T>
+__device__ __forceinline__ void keep_label(const DistillArgs& a, const Entries& en, const T* zr, long long label) {
   if (threadIdx.x == 0) {
     const int c = column_of(a, label);
     en.col[a.top] = c;
     en.z[a.top] = c >= 0 ? Elem<T>::to_f(zr[c]) : 0.0f;
+    for (int k = a.top + 1; k & 3; ++k) en.col[k] = -1;
   }
+}
 
-  // maximum and sums of the logits
-  constexpr int N = Vec<T>::N;
-  float st = 0.0f, s1 = 0.0f;
-  for (int c = (int)threadIdx.x * N; c < a.vocab; c += NT * N) {
-    float v[N];
-    Vec<T>::get(*reinterpret_cast<const u32x4_t*>(zr + c), v);
-    float m = mx[0];
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-      if (c + e >= a.vocab) v[e] = -INFINITY;
-      m = fmaxf(m, v[e]);
-    }
-    const float base = base_of(m), old = moved(mx[0], base);
-    st *= exp2_fast(old * a.rate_t);
-    if (TWO) s1 *= exp2_fast(old * a.rate_1);
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-      st += exp2_fast((v[e] - base) * a.rate_t);
-      if (TWO) s1 += exp2_fast((v[e] - base) * a.rate_1);
-    }
-    mx[0] = m;
-  }
-  const float own = mx[0];
-  block_max<NT>(mx, red[0]);
-  const float base = base_of(mx[0]), tm = base_of(mx[1]);
+// The sums of a token over its workgroup, once its maxima are known: st and s1 are the thread's
+// (relative to base), the rest comes from the entries, which keep exp((t - max) / T).
+template <int NT, int M>
+__device__ __forceinline__ Stats token_stats(const DistillArgs& a, const Entries& en, float m, float base, float tmax,
+                                             float st, float s1, bool labelled, float* red, float* inv_teacher,
+                                             bool* idle) {
+  const float tm = base_of(tmax);
+  const float zl = en.z[a.top];  // (its place is used again behind the next barrier)
   // S_T, S_1, teacher's sum, mass here, sum p (z - m), sum p t
-  const float d0 = moved(own, base);
-  float s[6] = {st * exp2_fast(d0 * a.rate_t), TWO ? s1 * exp2_fast(d0 * a.rate_1) : 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+  float s[6] = {st, s1, 0.0f, 0.0f, 0.0f, 0.0f};
   for (int k = threadIdx.x; k < a.top; k += NT) {
     const float d = en.t[k] - tm, p = exp2_fast(d * a.rate_t);
     en.t[k] = p;
@@ -283,22 +373,101 @@ __global__ void __launch_bounds__(NT) distill_kernel(DistillArgs a, const T* z, 
       s[5] += p * d;
     }
   }
-  block_sum<NT>(s, red[1]);
+  block_reduce<AddOp, NT>(s, red);
   Stats r;
-  r.m = mx[0];
+  r.m = m;
   r.st = a.want_t ? s[0] : 0.0f;
-  r.s1 = a.want_1 ? (TWO ? s[1] : s[0]) : 0.0f;
+  r.s1 = a.want_1 ? (M != ONE ? s[1] : s[0]) : 0.0f;
   r.tm = tm;
   r.ts = s[2];
-  const int lc = en.col[a.top];
   const float inv = s[2] != 0.0f ? 1.0f / s[2] : 0.0f;
   r.mass = s[3] * inv;
-  r.label = labelled && lc >= 0 ? 1.0f : 0.0f;
+  r.label = labelled && en.col[a.top] >= 0 ? 1.0f : 0.0f;
   r.lin = 0.0f;
-  if (s[2] != 0.0f)
-    r.lin = a.alpha * a.tau * inv * s[4] - a.alpha * a.tau * (inv * s[5] - a.tau * r.mass * logf(s[2]));
-  if (r.label != 0.0f) r.lin += (1.0f - a.alpha) * (en.z[a.top] - base);
-  const bool idle = s[2] == 0.0f && !labelled;  // nothing to learn here
+  if (s[2] != 0.0f) r.lin = a.alpha * a.tau * (inv * s[4] - inv * s[5] + a.tau * r.mass * logf(s[2]));
+  if (r.label != 0.0f) r.lin += (1.0f - a.alpha) * (zl - base);
+  *inv_teacher = inv;
+  *idle = s[2] == 0.0f && !labelled;  // nothing to learn here
+  return r;
+}
+
+// One workgroup a token: statistics, loss and, with GRAD, the gradient (a second look at the
+// row).
+template <typename T, int NT, int M, bool GRAD>
+__global__ void __launch_bounds__(NT) distill_kernel(DistillArgs a, const T* z, float* __restrict__ stats,
+                                                     float* __restrict__ loss, const float* __restrict__ dloss, T* dz) {
+  extern __shared__ __align__(16) char smem[];
+  __shared__ float red[2][NT / 64 * 6];
+  const Entries en = entries_in(smem, a.top);
+  if (GRAD) en.head[threadIdx.x] = -1;
+  const size_t row = blockIdx.x;
+  const T* zr = z + row * a.ld;
+
+  float mx[2] = {-INFINITY, -INFINITY};  // of the student's logits, of the teacher's
+  for (int k = threadIdx.x; k < a.top; k += NT) {
+    const size_t i = row * a.top + k;
+    mx[1] = fmaxf(mx[1], keep_entry(a, en, zr, k, id_at(a.ids, a.id64, i), teacher_at(a, i)));
+  }
+  const long long label = a.labels ? id_at(a.labels, a.label64, row) : -1;
+  const bool labelled = label >= 0 && label < a.total;
+  keep_label(a, en, zr, label);
+
+  // Maximum and sums of the logits in one pass: a thread's sums are relative to the maximum of what
+  // it has seen (kept within 2^50: see Exponent), of a batch of U loads at a time.
+  constexpr int N = Vec<T>::N, U = 4;
+  float st = 0.0f, s1 = 0.0f;
+  for (int c0 = (int)threadIdx.x * N; c0 < a.vocab; c0 += NT * N * U) {
+    u32x4_t raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int c = c0 + NT * N * u;
+      if (c < a.vocab) raw[u] = *reinterpret_cast<const u32x4_t*>(zr + c);
+      else raw[u] = u32x4_t{Vec<T>::NONE, Vec<T>::NONE, Vec<T>::NONE, Vec<T>::NONE};
+    }
+    float m = mx[0];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int c = c0 + NT * N * u;
+      if (c < a.vocab && c + N > a.vocab) raw[u] = first_values<T>(raw[u], a.vocab - c, -INFINITY);
+      float v[N];
+      Vec<T>::get(raw[u], v);
+#pragma unroll
+      for (int e = 0; e < N; ++e) m = fmaxf(m, v[e]);
+    }
+    const float base = near_base(m);
+    const Exponents<M> exps(a, base);
+    if (m > mx[0] && mx[0] != -INFINITY) {  // (a sum of nothing stays 0, wherever the base goes)
+      const Exponents<M> old(a, near_base(mx[0]));
+      st *= exp2_fast(old.t.c - exps.t.c);
+      if (M != ONE) s1 *= exp2_fast(old.one.c - exps.one.c);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float v[N];
+      Vec<T>::get(raw[u], v);
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        float et, e1;
+        exps.of(v[e], &et, &e1);
+        st += et;
+        if (M != ONE) s1 += e1;
+      }
+    }
+    mx[0] = m;
+  }
+  const float own = mx[0];
+  block_reduce<MaxOp, NT>(mx, red[0]);
+  const float base = base_of(mx[0]);
+  const bool far = is_far(base);
+  if (far) {
+    st = s1 = far_sum<T, NT>(a, zr, base);
+  } else if (own != -INFINITY) {
+    st *= exp2_fast(fmaf(-base, a.rate_t, Exponent(near_base(own), a.rate_t).c));
+    if (M != ONE) s1 *= exp2_fast(fmaf(-base, a.rate_1, Exponent(near_base(own), a.rate_1).c));
+  }
+  float inv;
+  bool idle;
+  const Stats r = token_stats<NT, M>(a, en, mx[0], base, mx[1], st, s1, labelled, red[1], &inv, &idle);
   if (threadIdx.x == 0) {
     if (stats) store_stats(stats + row * kDistillStats, r);
     if (loss) loss[row] = idle ? 0.0f : loss_of(r, a.alpha, a.tau);
@@ -310,23 +479,146 @@ __global__ void __launch_bounds__(NT) distill_kernel(DistillArgs a, const T* z, 
       write_zeros<T, NT>(dr, 0, a.ld);
       return;
     }
-    float ft, f1;
-    factors<TWO>(a, r, w, &ft, &f1);
-    for (int k = threadIdx.x; k <= a.top; k += NT)
-      en.t[k] = k < a.top ? w * a.alpha * a.tau * inv * en.t[k] : w * (1.0f - a.alpha);
-    write_slopes<T, NT, TWO>(a, zr, dr, 0, a.ld, base, ft, f1);
+    const Slopes<M> f(a, r, w, far);
+    resolve_entries<T, NT, M>(a, f, en, w * a.alpha * a.tau * inv, w * (1.0f - a.alpha), 0, far, base);
     __syncthreads();
-    write_entries<T, NT, TWO>(a, en, dr, base, ft, f1);
+    if (far) write_slopes<T, NT, M, true>(a, f, en, zr, dr, 0, a.ld, base);
+    else write_slopes<T, NT, M, false>(a, f, en, zr, dr, 0, a.ld, base);
   }
 }
 
-// The gradient from a token's (joined) statistics: a workgroup a piece of `piece` columns of a
-// row.
-template <typename T, int NT, bool TWO>
-__global__ void __launch_bounds__(NT) distill_bwd_kernel(DistillArgs a, int pieces, int piece, const T* z,
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t row_buffer(const void* p, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), (short)0, (int)bytes, 0x00020000);
+}
+
+constexpr int kPast = 2;  // a buffer access past the caches
+
+// The 16 bytes at `off` of part `i` (of `part` bytes) of a row of `bytes`; behind them nothing is
+// written.  The part moves the buffer's start and does not become the store's SGPR offset: the
+// compiler takes a store with an SGPR offset to have read its data when the next instruction
+// writes those registers, and of such stores, one multiply behind each, some had their first 4
+// bytes replaced by that product.
+__device__ __forceinline__ void store_at(bool past, u32x4_t v, void* row, uint32_t bytes, uint32_t off, int i, uint32_t part) {
+  const uint32_t start = i * part;
+  const __amdgpu_buffer_rsrc_t to = row_buffer((char*)row + start, bytes > start ? bytes - start : 0);
+  if (past) __builtin_amdgcn_raw_buffer_store_b128(v, to, off, 0, kPast);
+  else __builtin_amdgcn_raw_buffer_store_b128(v, to, off, 0, 0);
+  __builtin_amdgcn_sched_barrier(0);  // chunk by chunk: several at a time cost more registers than they gain
+}
+
+// Makes the compiler forget what it has derived of r, so that it unpacks the values again instead
+// of keeping them unpacked (twice the registers, for bf16) from one look at the row to the next.
+__device__ __forceinline__ void forget(u32x4_t& r) { asm volatile("" : "+v"(r)); }
+
+// Loss and gradient of a token whose row stays in the registers of its workgroup, CH chunks of 16
+// bytes a thread: the logits are read once.
+template <typename T, int NT, int CH, int M>
+__global__ void __launch_bounds__(NT) distill_row_kernel(DistillArgs a, const T* z, float* __restrict__ loss,
+                                                         const float* __restrict__ dloss, T* dz) {
+  extern __shared__ __align__(16) char smem[];
+  __shared__ float red[2][NT / 64 * 6];
+  constexpr int N = Vec<T>::N;
+  const Entries en = entries_in(smem, a.top);
+  en.head[threadIdx.x] = -1;
+  const size_t row = blockIdx.x;
+  const T* zr = z + row * a.ld;
+  T* dr = dz + row * a.ld;
+  // the first entries come ahead of the row
+  const int k0 = threadIdx.x;
+  long long id0 = -1;
+  float t0 = 0.0f;
+  if (k0 < a.top) {
+    id0 = id_at(a.ids, a.id64, row * a.top + k0);
+    t0 = teacher_at(a, row * a.top + k0);
+  }
+  const long long label = a.labels ? id_at(a.labels, a.label64, row) : -1;
+  const bool labelled = label >= 0 && label < a.total;
+  const float w = dloss[row];
+  // Chunks behind the vocabulary read as zeros and are not written (the buffers end there).
+  const uint32_t bytes = (uint32_t)(((unsigned)a.vocab + N - 1) / N * 16), off = threadIdx.x * 16;
+  const __amdgpu_buffer_rsrc_t zb = row_buffer(zr, bytes);
+  u32x4_t raw[CH];
+#pragma unroll
+  for (int i = 0; i < CH; ++i) raw[i] = __builtin_amdgcn_raw_buffer_load_b128(zb, off, i * NT * 16, kPast);
+  float mx[2] = {-INFINITY, -INFINITY};
+  if (k0 < a.top) mx[1] = keep_entry(a, en, zr, k0, id0, t0);
+  for (int k = k0 + NT; k < a.top; k += NT) {
+    const size_t i = row * a.top + k;
+    mx[1] = fmaxf(mx[1], keep_entry(a, en, zr, k, id_at(a.ids, a.id64, i), teacher_at(a, i)));
+  }
+  keep_label(a, en, zr, label);
+#pragma unroll
+  for (int i = 0; i < CH; ++i) {
+    if ((i + 1) * NT * N > a.vocab) {  // the same for the whole workgroup
+      const int c = ((int)threadIdx.x + NT * i) * N;
+      if (c + N > a.vocab) raw[i] = first_values<T>(raw[i], a.vocab - c, -INFINITY);
+    }
+    float v[N];
+    Vec<T>::get(raw[i], v);
+#pragma unroll
+    for (int e = 0; e < N; ++e) mx[0] = fmaxf(mx[0], v[e]);
+  }
+  block_reduce<MaxOp, NT>(mx, red[0]);
+  const float base = base_of(mx[0]);
+  const bool far = is_far(base);
+#pragma unroll
+  for (int i = 0; i < CH; ++i) forget(raw[i]);
+  float st = 0.0f, s1 = 0.0f;
+  if (far) {
+    st = s1 = far_sum<T, NT>(a, zr, base);
+  } else {
+    const Exponents<M> exps(a, base);
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      float v[N];
+      Vec<T>::get(raw[i], v);
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        float et, e1;
+        exps.of(v[e], &et, &e1);
+        st += et;
+        if (M != ONE) s1 += e1;
+      }
+    }
+    st *= exps.t.off();
+    s1 *= exps.one.off();
+  }
+  float inv;
+  bool idle;
+  const Stats r = token_stats<NT, M>(a, en, mx[0], base, mx[1], st, s1, labelled, red[1], &inv, &idle);
+  if (threadIdx.x == 0) loss[row] = idle ? 0.0f : loss_of(r, a.alpha, a.tau);
+  if (idle || w == 0.0f) {  // whatever the logits are
+    write_zeros<T, NT>(dr, 0, a.ld);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < CH; ++i) forget(raw[i]);
+  const Slopes<M> f(a, r, w, far);
+  resolve_entries<T, NT, M>(a, f, en, w * a.alpha * a.tau * inv, w * (1.0f - a.alpha), 0, far, base);
+  __syncthreads();
+  if (far) {
+    write_slopes<T, NT, M, true>(a, f, en, zr, dr, 0, a.ld, base);
+  } else {
+    const uint32_t mine = chunks_with_entries<T, NT>(en, 0);
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      u32x4_t v = slopes_of<T, M>(f, raw[i], N);
+      if (mine >> i & 1) v = with_entries<T>(en, v, ((int)threadIdx.x + NT * i) * N);
+      store_at(a.past, v, dr, bytes, off, i, NT * 16);
+    }
+    write_padding<T, NT>(a, dr, 0);
+    write_zeros<T, NT>(dr, (a.vocab + N - 1) / N * N, a.ld);
+  }
+}
+
+// The gradient from a token's (joined) statistics: a workgroup U times NT * 16 bytes of a row,
+// loaded before anything else.
+template <typename T, int NT, int U, int M>
+__global__ void __launch_bounds__(NT) distill_bwd_kernel(DistillArgs a, int pieces, const T* z,
                                                          const float* __restrict__ stats,
                                                          const float* __restrict__ dloss, T* dz) {
   extern __shared__ __align__(16) char smem[];
+  constexpr int N = Vec<T>::N, piece = NT * N * U;
   const Entries en = entries_in(smem, a.top);
   const size_t row = blockIdx.x / pieces;
   const int lo = (int)(blockIdx.x % pieces) * piece, hi = min(lo + piece, a.ld);
@@ -338,33 +630,47 @@ __global__ void __launch_bounds__(NT) distill_bwd_kernel(DistillArgs a, int piec
     write_zeros<T, NT>(dr, lo, hi);
     return;
   }
-  const float base = base_of(s.m);
-  const float inv = s.ts != 0.0f ? w * a.alpha * a.tau / s.ts : 0.0f;
-  for (int k = threadIdx.x; k <= a.top; k += NT) {
-    int c;
-    float t;
+  const int end = (a.vocab + N - 1) / N * N;  // behind it there are zeros
+  const uint32_t bytes = (uint32_t)max(min(hi, end) - lo, 0) * sizeof(T), off = threadIdx.x * 16;
+  const __amdgpu_buffer_rsrc_t zb = row_buffer(zr + lo, bytes);
+  u32x4_t raw[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) raw[u] = __builtin_amdgcn_raw_buffer_load_b128(zb, off, u * NT * 16, kPast);
+  en.head[threadIdx.x] = -1;
+  for (int k = threadIdx.x; k < entry_room(a.top); k += NT) {
+    int c = -1;
     if (k < a.top) {
       const size_t i = row * a.top + k;
-      const long long id = id_at(a.ids, a.id64, i);
-      c = column_of(a, id);
-      const float p = exp2_fast((teacher_at(a, i, id) - s.tm) * a.rate_t);
-      t = inv * p;
+      c = column_of(a, id_at(a.ids, a.id64, i));
+      const float p = exp2_fast((teacher_at(a, i) - s.tm) * a.rate_t);
+      en.t[k] = p;
       if (p == 0.0f) c = -1;
-    } else {
-      c = a.labels ? column_of(a, id_at(a.labels, a.label64, row)) : -1;
-      t = w * (1.0f - a.alpha);
+    } else if (k == a.top && a.labels) {
+      c = column_of(a, id_at(a.labels, a.label64, row));
     }
     if (c < lo || c >= hi) c = -1;
     en.col[k] = c;
-    en.t[k] = t;
-    en.z[k] = c >= 0 ? Elem<T>::to_f(zr[c]) : 0.0f;
+    if (c >= 0) en.z[k] = Elem<T>::to_f(zr[c]);
   }
+  __syncthreads();  // the entries' logits are read, too: dz may be z
+  const bool far = is_far(s.m);
+  const Slopes<M> f(a, s, w, far);
+  resolve_entries<T, NT, M>(a, f, en, s.ts != 0.0f ? w * a.alpha * a.tau / s.ts : 0.0f, w * (1.0f - a.alpha), lo, far,
+                            s.m);
   __syncthreads();
-  float ft, f1;
-  factors<TWO>(a, s, w, &ft, &f1);
-  write_slopes<T, NT, TWO>(a, zr, dr, lo, hi, base, ft, f1);
-  __syncthreads();
-  write_entries<T, NT, TWO>(a, en, dr, base, ft, f1);
+  if (far) {
+    write_slopes<T, NT, M, true>(a, f, en, zr, dr, lo, hi, s.m);
+  } else {
+    const uint32_t mine = chunks_with_entries<T, NT>(en, lo);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      u32x4_t v = slopes_of<T, M>(f, raw[u], N);
+      if (mine >> u & 1) v = with_entries<T>(en, v, lo + ((int)threadIdx.x + NT * u) * N);
+      store_at(a.past, v, dr + lo, bytes, off, u, NT * 16);
+    }
+    if (lo <= a.vocab && a.vocab < hi) write_padding<T, NT>(a, dr, lo);
+    write_zeros<T, NT>(dr, max(lo, end), hi);
+  }
 }
 
 // Ranks' statistics [ranks][tokens] to the whole vocabulary's, in the ranks' order.
@@ -423,41 +729,130 @@ static DistillArgs at_tokens(const DistillShape& q, DistillArgs a, long long t, 
   return a;
 }
 
-template <typename T, int NT, bool TWO, bool GRAD>
-static hipError_t run_rows(const DistillShape& q, const void* z, float* stats, float* loss, const float* dloss, void* dz,
-                           hipStream_t s) {
-  const DistillArgs all = distill_args(q);
-  const long long most = max_groups(NT);
+// Which exponentials a loss needs (Sums).
+static int sums_of(const DistillShape& q) {
+  const DistillArgs a = distill_args(q);
+  if (!a.want_t || !a.want_1 || q.tau == 1.0f) return ONE;
+  return q.tau == 2.0f ? SQUARE : q.tau == 4.0f ? FOURTH : TWO;
+}
+
+struct DistillCall {
+  const DistillShape& q;
+  const void* z;
+  float *stats, *loss;        // forward
+  const float *in, *dloss;    // gradient
+  void* dz;
+  hipStream_t s;
+};
+
+// Launches `run(arguments, first token)` over the call's tokens, as many at a time as a launch of
+// `groups` workgroups of `threads` for each of them can have.
+template <typename F>
+static hipError_t over_tokens(const DistillShape& q, int threads, int groups, size_t out_bytes, F run) {
+  DistillArgs all = distill_args(q);
+  all.past = out_bytes >= kStreamBytes;
+  const long long most = max_groups(threads) / groups;
   for (long long t = 0; t < q.tokens; t += most) {
-    const int n = (int)std::min(most, q.tokens - t);
-    const DistillArgs a = at_tokens(q, all, t, n);
-    hipLaunchKernelGGL((distill_kernel<T, NT, TWO, GRAD>), dim3(n), dim3(NT), entries_bytes(a.top), s, a,
-                       (const T*)z + t * q.ld, stats ? stats + t * kDistillStats : nullptr, loss ? loss + t : nullptr,
-                       dloss ? dloss + t : nullptr, dz ? (T*)dz + t * q.ld : nullptr);
+    run(at_tokens(q, all, t, (int)std::min(most, q.tokens - t)), t);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
 }
 
-static bool two_sums(const DistillShape& q) {
-  const DistillArgs a = distill_args(q);
-  return a.want_t && a.want_1 && q.tau != 1.0f;
+template <typename T>
+static size_t out_bytes(const DistillShape& q) { return (size_t)q.tokens * q.ld * sizeof(T); }
+
+template <typename T, int NT, int M, bool GRAD>
+static hipError_t run_rows(const DistillCall& c) {
+  const DistillShape& q = c.q;
+  return over_tokens(q, NT, 1, GRAD ? out_bytes<T>(q) : 0, [&](const DistillArgs& a, long long t) {
+    hipLaunchKernelGGL((distill_kernel<T, NT, M, GRAD>), dim3(a.tokens), dim3(NT), entries_bytes(a.top, NT), c.s, a,
+                       (const T*)c.z + t * q.ld, c.stats ? c.stats + t * kDistillStats : nullptr,
+                       c.loss ? c.loss + t : nullptr, GRAD ? c.dloss + t : nullptr, GRAD ? (T*)c.dz + t * q.ld : nullptr);
+  });
+}
+
+template <typename T, int NT, int CH, int M>
+static hipError_t run_kept(const DistillCall& c) {
+  const DistillShape& q = c.q;
+  return over_tokens(q, NT, 1, out_bytes<T>(q), [&](const DistillArgs& a, long long t) {
+    hipLaunchKernelGGL((distill_row_kernel<T, NT, CH, M>), dim3(a.tokens), dim3(NT), entries_bytes(a.top, NT), c.s, a,
+                       (const T*)c.z + t * q.ld, c.loss + t, c.dloss + t, (T*)c.dz + t * q.ld);
+  });
+}
+
+// Threads for a row of n chunks of 16 bytes.  A short row has few threads, so that as many bytes
+// are on their way in a CU as its registers hold: 32768 x 6288 (n = 786) loss 88 us with 128
+// threads (108 with 256), loss and gradient 197 with 128 (252 with 256).
+template <typename T, int M>
+static hipError_t run_forward(const DistillCall& c) {
+  const int n = (c.q.vocab + Vec<T>::N - 1) / Vec<T>::N;
+  if (!c.dz) {
+    if (n <= 256) return run_rows<T, 64, M, false>(c);
+    if (n <= 1024) return run_rows<T, 128, M, false>(c);
+    return n <= 2048 ? run_rows<T, 256, M, false>(c) : run_rows<T, 512, M, false>(c);
+  }
+  if (n <= 128) return run_kept<T, 64, 2, M>(c);
+  if (n <= 256) return run_kept<T, 64, 4, M>(c);
+  if (n <= 512) return run_kept<T, 64, 8, M>(c);
+  if (n <= 896) return run_kept<T, 128, 7, M>(c);
+  if (n <= 1664) return run_kept<T, 128, 13, M>(c);
+  if (n <= 3328) return run_kept<T, 256, 13, M>(c);
+  if (n <= 6656) return run_kept<T, 512, 13, M>(c);
+  if (n <= 9728) return run_kept<T, 512, 19, M>(c);
+  if (n <= 12800) return run_kept<T, 512, 25, M>(c);
+  if (n <= 16384) return run_kept<T, 512, 32, M>(c);
+  return run_rows<T, 512, M, true>(c);  // more than the registers hold: a second look at the row
+}
+
+template <typename T, int NT, int U, int M>
+static hipError_t run_pieces(const DistillCall& c) {
+  constexpr int piece = NT * Vec<T>::N * U;
+  const DistillShape& q = c.q;
+  const int pieces = (q.ld + piece - 1) / piece;
+  return over_tokens(q, NT, pieces, out_bytes<T>(q), [&](const DistillArgs& a, long long t) {
+    hipLaunchKernelGGL((distill_bwd_kernel<T, NT, U, M>), dim3((unsigned)(a.tokens * pieces)), dim3(NT),
+                       entries_bytes(a.top, NT), c.s, a, pieces, (const T*)c.z + t * q.ld, c.in + t * kDistillStats,
+                       c.dloss + t, (T*)c.dz + t * q.ld);
+  });
+}
+
+template <typename T, int M>
+static hipError_t run_backward(const DistillCall& c) {
+  const int n = c.q.ld / Vec<T>::N;
+  if (n <= 128) return run_pieces<T, 64, 2, M>(c);
+  if (n <= 896) return run_pieces<T, 128, 7, M>(c);
+  // Few rows are cut into more pieces: 1 x 50304 8.0 us with U = 4 (9.6 with 13); 2047 x 25152
+  // 50 us with U = 13 (55 with 4).
+  return c.q.tokens < 512 ? run_pieces<T, 256, 4, M>(c) : run_pieces<T, 256, 13, M>(c);
+}
+
+template <typename T, int M>
+static hipError_t run_mode(const DistillCall& c) {
+  return c.in ? run_backward<T, M>(c) : run_forward<T, M>(c);
 }
 
 template <typename T>
-static hipError_t run_forward(const DistillShape& q, const void* z, float* stats, float* loss, const float* dloss,
-                              void* dz, hipStream_t s) {
-  if (two_sums(q)) return dz ? run_rows<T, 256, true, true>(q, z, stats, loss, dloss, dz, s)
-                             : run_rows<T, 256, true, false>(q, z, stats, loss, dloss, dz, s);
-  return dz ? run_rows<T, 256, false, true>(q, z, stats, loss, dloss, dz, s)
-            : run_rows<T, 256, false, false>(q, z, stats, loss, dloss, dz, s);
+static hipError_t run_type(const DistillCall& c) {
+  switch (sums_of(c.q)) {
+    case ONE: return run_mode<T, ONE>(c);
+    case SQUARE: return run_mode<T, SQUARE>(c);
+    case FOURTH: return run_mode<T, FOURTH>(c);
+    default: return run_mode<T, TWO>(c);
+  }
 }
 
 hipError_t launch_distill(int dtype, const DistillShape& q, const void* z, float* stats, float* loss,
                           const float* dloss, void* dz, hipStream_t s) {
-  return dtype == DT_BF16 ? run_forward<bf16_t>(q, z, stats, loss, dloss, dz, s)
-                          : run_forward<float>(q, z, stats, loss, dloss, dz, s);
+  const DistillCall c{q, z, stats, loss, nullptr, dloss, dz, s};
+  return dtype == DT_BF16 ? run_type<bf16_t>(c) : run_type<float>(c);
+}
+
+hipError_t launch_distill_bwd(int dtype, const DistillShape& q, const void* z, const float* stats, const float* dloss,
+                              void* dz, hipStream_t s) {
+  const DistillCall c{q, z, nullptr, nullptr, stats, dloss, dz, s};
+  return dtype == DT_BF16 ? run_type<bf16_t>(c) : run_type<float>(c);
 }
 
 hipError_t launch_distill_join(int tokens, int ranks, float alpha, float tau, const float* parts, float* stats,
@@ -465,34 +860,6 @@ hipError_t launch_distill_join(int tokens, int ranks, float alpha, float tau, co
   hipLaunchKernelGGL(distill_join_kernel, dim3((unsigned)(((long long)tokens + 255) / 256)), dim3(256), 0, s, tokens,
                      ranks, alpha, tau, kLog2e / tau, parts, stats, loss);
   return hipGetLastError();
-}
-
-template <typename T, bool TWO>
-static hipError_t run_backward(const DistillShape& q, const void* z, const float* stats, const float* dloss, void* dz,
-                               hipStream_t s) {
-  constexpr int NT = 256, piece = NT * Vec<T>::N * 4;
-  const DistillArgs all = distill_args(q);
-  const int pieces = (q.ld + piece - 1) / piece;
-  const long long most = max_groups(NT) / pieces;
-  for (long long t = 0; t < q.tokens; t += most) {
-    const int n = (int)std::min(most, q.tokens - t);
-    const DistillArgs a = at_tokens(q, all, t, n);
-    hipLaunchKernelGGL((distill_bwd_kernel<T, NT, TWO>), dim3((unsigned)(n * pieces)), dim3(NT), entries_bytes(a.top), s,
-                       a, pieces, piece, (const T*)z + t * q.ld, stats + t * kDistillStats, dloss + t,
-                       (T*)dz + t * q.ld);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  return hipSuccess;
-}
-
-hipError_t launch_distill_bwd(int dtype, const DistillShape& q, const void* z, const float* stats, const float* dloss,
-                              void* dz, hipStream_t s) {
-  if (dtype == DT_BF16)
-    return two_sums(q) ? run_backward<bf16_t, true>(q, z, stats, dloss, dz, s)
-                       : run_backward<bf16_t, false>(q, z, stats, dloss, dz, s);
-  return two_sums(q) ? run_backward<float, true>(q, z, stats, dloss, dz, s)
-                     : run_backward<float, false>(q, z, stats, dloss, dz, s);
 }
 
 }  // namespace merak

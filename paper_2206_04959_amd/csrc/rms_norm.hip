@@ -18,34 +18,11 @@
 #include "act8_codes.h"
 #include "common.h"
 #include "kernels.h"
+#include "wave.h"
 
 namespace merak {
 
 constexpr int threads_of(int nt) { return nt < 256 ? 256 : nt; }  // of a workgroup: four rows of 64 threads, or one
-
-// Sums of N values over the NT threads of a row; every thread gets them.  `buf` alternates
-// between two LDS areas, so one barrier a call is enough.
-template <int NT, int N>
-__device__ __forceinline__ void row_sum(float (&v)[N], float* lds, int buf) {
-#pragma unroll
-  for (int n = 0; n < N; ++n) v[n] = wave_sum(v[n]);
-  if constexpr (NT > 64) {
-    constexpr int W = NT / 64;
-    float* p = lds + buf * W * N;
-    if ((threadIdx.x & 63) == 0) {
-#pragma unroll
-      for (int n = 0; n < N; ++n) p[(threadIdx.x >> 6) * N + n] = v[n];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int n = 0; n < N; ++n) {
-      float s = 0.0f;
-#pragma unroll
-      for (int w = 0; w < W; ++w) s += p[w * N + n];
-      v[n] = s;
-    }
-  }
-}
 
 // v rounded to T (what a store would keep).
 template <typename T>
@@ -89,7 +66,7 @@ __global__ void __launch_bounds__(threads_of(NT)) rms_fwd_kernel(NormFwd a, cons
       for (int e = 0; e < 8; ++e) s[0] += h[i][e] * h[i][e];
     }
   }
-  row_sum<NT>(s, red, 0);
+  block_reduce<AddOp, NT>(s, red);
   const float rstd = 1.0f / sqrtf(s[0] / (float)a.cols + a.eps);
 #pragma unroll
   for (int i = 0; i < CH; ++i) {
@@ -150,8 +127,8 @@ __global__ void __launch_bounds__(threads_of(NT)) rms_bwd_kernel(int rows, int c
         s[1] += d[i][e] * w[e] * v[i][e];
       }
     }
-    row_sum<NT>(s, red, buf);
-    buf ^= 1;
+    block_reduce<AddOp, NT>(s, red + buf);
+    buf ^= 2 * (NT / 64);  // two areas in turn: one barrier a row is enough
     const float rstd = 1.0f / sqrtf(s[0] / (float)cols + eps);
     const float m = s[1] * rstd / (float)cols;  // mean(dy g n)
 #pragma unroll

@@ -1,0 +1,440 @@
+"""The residual norm and the distillation loss on the GPU, through the C ABI, against the fp64
+oracle.
+
+Tolerances count roundings, as in test_gpu_operators.py: u = 2^-24, `half` half a step of the
+output's type relative to the value.  A sum of fp32 terms that each thread adds one after the
+other and that then meet in a tree is off by at most (additions on the longest way) u times the
+sum of the magnitudes; each test says how long that way is."""
+import numpy as np
+import pytest
+
+from oracle import operators as O
+from paper_2206_04959_amd import binding as B
+from paper_2206_04959_amd import synth
+from tests.gpu_util import need_gpu
+from tests.test_gpu_operators import HALF, TINY, U, _f64, _given, _guarded, _normal, _type
+
+pytestmark = pytest.mark.gpu
+
+
+def _close(got, ref, tol, what):
+    got = _f64(got)
+    bad = np.abs(got - ref) - tol
+    assert got.shape == ref.shape, what
+    assert np.isfinite(got).all() and (bad <= 0).all(), \
+        (what, bad.max(), np.unravel_index(np.argmax(bad), bad.shape), np.abs(got - ref).max())
+
+
+# ---------------------------------------------------------------------------
+# Residual addition and norm
+# ---------------------------------------------------------------------------
+
+# widths at and around every layout of a row: 64 lanes of 1 to 4 chunks, 256 of 2 to 4, 1024 of 2 and 4
+WIDTHS = [(1, 8), (5, 64), (257, 72), (9, 512), (3, 520), (66, 1024), (7, 1032), (5, 1536), (4, 1600), (6, 2048), (3, 2056),
+          (4, 4096), (3, 4104), (2, 6144), (3, 6152), (5, 8192), (3, 8200), (2, 16384), (3, 16392), (2, 32768)]
+NORM = 48 * U   # 32 squares in a thread, 6 and 4 steps of the tree; halved by the root; division, root, products
+
+
+def _rows(rng, rows, cols, dtype, spread=True):
+    v = rng.standard_normal(size=(rows, cols), dtype=np.float32)
+    if spread:  # a few channels many times larger
+        v *= np.where(rng.random(cols) < 0.02, 30.0, 1.0).astype(np.float32)
+    return _given(v, dtype)
+
+
+def _sum_as_kept(x, r, dtype):
+    """x + r in fp32, rounded to the type."""
+    s = x.astype(np.float32) + r.astype(np.float32)
+    return synth.bf16_bits_to_f64(synth.f32_to_bf16_bits(s)) if dtype == "bf16" else s.astype(np.float64)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,cols", WIDTHS)
+@pytest.mark.parametrize("form", ["sum", "no sum", "plain", "on x", "on resid"])
+def test_norm_forward(dtype, rows, cols, form):
+    torch = need_gpu()
+    print(f"[norm fwd] {dtype} {rows}x{cols} {form}", flush=True)
+    rng = np.random.default_rng(rows + cols)
+    dt = _type(torch, dtype)
+    x, xv = _rows(rng, rows, cols, dtype)
+    r, rv = (None, None) if form == "plain" else _rows(rng, rows, cols, dtype, False)
+    g, gv = _normal(rng, (cols,), dtype, 0.1, 1.0)
+    y, clean = _guarded(torch, (rows, cols), dt)
+    s, sclean = _guarded(torch, (rows, cols), dt)
+    eight = cols % 32 == 0
+    q = torch.full((rows, cols), 77, dtype=torch.uint8, device="cuda") if eight else None
+    sc = torch.full((rows, cols // 32), 77, dtype=torch.uint8, device="cuda") if eight else None
+    out = {"sum": s, "no sum": None, "plain": None, "on x": x, "on resid": r}[form]
+    h = xv if r is None else _sum_as_kept(xv, rv, dtype)
+    B.add_rms_norm_fwd(x, g, y, resid=r, sum=out, q=q, scales=sc, eps=1e-5)
+    torch.cuda.synchronize()
+    ref = O.rms_norm(h, gv, float(np.float32(1e-5)))
+    _close(y, ref, (HALF[dtype] + NORM) * np.abs(ref) + TINY, "y")
+    assert clean() and sclean()
+    if out is not None:
+        assert np.array_equal(_f64(out), h)
+    if form == "no sum":
+        assert bool((s == 7).all())
+    if eight:
+        kept = O.act8_restore(q.cpu().numpy(), sc.cpu().numpy())
+        most = np.repeat(np.abs(ref.reshape(rows, -1, 32)).max(-1), 32, axis=-1)
+        # e4m3's rounding of a y that is itself off by NORM; below 2^-6 of the scale (at most
+        # most / 224) a step of 2^-9 of it
+        tol = np.maximum(2.0 ** -4 * np.abs(ref), 2.0 ** -10 * most / 224) * (1 + 2 * NORM) + 2 * NORM * np.abs(ref)
+        assert (np.abs(kept - ref) <= tol).all()
+        if dtype == "fp32":  # the codes of the very y that is stored
+            q2, sc2 = torch.empty_like(q), torch.empty_like(sc)
+            B.act8_save(y, q2, sc2)
+            assert torch.equal(q, q2) and torch.equal(sc, sc2)
+        only, onlysc = torch.empty_like(q), torch.empty_like(sc)
+        if form in ("sum", "no sum", "plain"):  # y not wanted: the same codes
+            B.add_rms_norm_fwd(x, g, resid=r, q=only, scales=onlysc, eps=1e-5)
+            assert torch.equal(q, only) and torch.equal(sc, onlysc)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,cols", WIDTHS + [(1025, 64), (5000, 24), (2100, 1040), (1030, 4104), (40, 8200)])
+@pytest.mark.parametrize("form", ["both", "no dsum", "on dy", "on dsum", "added"])
+def test_norm_backward(dtype, rows, cols, form):
+    torch = need_gpu()
+    print(f"[norm bwd] {dtype} {rows}x{cols} {form}", flush=True)
+    rng = np.random.default_rng(rows * 3 + cols)
+    dt = _type(torch, dtype)
+    h, hv = _rows(rng, rows, cols, dtype)
+    dy, dyv = _normal(rng, (rows, cols), dtype)
+    ds, dsv = (None, None) if form == "no dsum" else _normal(rng, (rows, cols), dtype)
+    g, gv = _normal(rng, (cols,), dtype, 0.1, 1.0)
+    dx, clean = _guarded(torch, (rows, cols), dt)
+    dg, gclean = _guarded(torch, (cols,), torch.float32)
+    start = rng.standard_normal(cols).astype(np.float32)
+    if form == "added":
+        dg.copy_(torch.from_numpy(start))
+    out = {"on dy": dy, "on dsum": ds}.get(form, dx)
+    scratch, sclean = _guarded(torch, (B.add_rms_norm_scratch_elems(rows, cols),), torch.float32)
+    B.add_rms_norm_bwd(dy, h, g, out, dg, scratch, dsum=ds, eps=1e-5, accumulate=form == "added")
+    torch.cuda.synchronize()
+    rx, rg, mag, gmag = O.rms_norm_backward(dyv, hv, gv, dsv, float(np.float32(1e-5)))
+    # the two sums over a row as in the forward pass, whole; a few products
+    _close(out, rx, HALF[dtype] * np.abs(rx) + 100 * U * mag + TINY, "dx")
+    # a thread's rows one after the other (at most 1024 rows at once, and at least 256), then trees
+    # and the 64 parts; each term is off by NORM
+    way = rows / 128 + 40
+    if form == "added":
+        rg = rg + start
+        gmag = gmag + np.abs(start)
+    _close(dg, rg, (way * U + 2 * NORM) * gmag + TINY, "dgamma")
+    assert clean() and gclean() and sclean()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("cols", [64, 2048, 8192, 32768])
+def test_norm_of_zeros_and_of_nonfinite_rows(dtype, cols):
+    """A row of zeros gives zeros; NaN and infinity stay in their row (and in dgamma's columns)."""
+    torch = need_gpu()
+    print(f"[norm nonfinite] {dtype} {cols}", flush=True)
+    rng = np.random.default_rng(cols)
+    x, xv = _rows(rng, 6, cols, dtype)
+    x[1] = 0
+    x[3, 5] = float("nan")
+    x[4, 7] = float("inf")
+    g, gv = _normal(rng, (cols,), dtype, 0.1, 1.0)
+    y, q = torch.empty_like(x), torch.empty(6, cols, dtype=torch.uint8, device="cuda")
+    sc = torch.empty(6, cols // 32, dtype=torch.uint8, device="cuda")
+    B.add_rms_norm_fwd(x, g, y, q=q, scales=sc)
+    assert not y[1].any() and bool(torch.isnan(y[3]).all())
+    assert bool(torch.isnan(y[4, 7])) and not y[4, :7].any()  # infinity / infinity, and 1 / infinity
+    assert not (q[1] & 0x7f).any() and bool(((q[3] & 0x7f) == 0x7f).all())
+    ref = O.rms_norm(xv[[0, 2, 5]], gv)
+    _close(y[[0, 2, 5]], ref, (HALF[dtype] + NORM) * np.abs(ref) + TINY, "y")
+    dy, dyv = _normal(rng, (6, cols), dtype)
+    dx, dg = torch.empty_like(x), torch.empty(cols, device="cuda")
+    scratch = torch.empty(B.add_rms_norm_scratch_elems(6, cols), device="cuda")
+    B.add_rms_norm_bwd(dy, x, g, dx, dg, scratch)
+    good = [0, 2, 5]
+    rx, _, mag, _ = O.rms_norm_backward(dyv[good], xv[good], gv)
+    _close(dx[good], rx, HALF[dtype] * np.abs(rx) + 100 * U * mag + TINY, "dx")
+    assert bool(torch.isfinite(dx[1]).all()) and bool(torch.isnan(dx[3]).all()) and bool(torch.isnan(dg).all())
+
+
+def test_norm_gradient_sums_integers_exactly():
+    """h of +-1 and eps far below 1 ulp make n = h exactly; integer gradients then sum exactly in any
+    order, so one lost or doubled term shows."""
+    torch = need_gpu()
+    rng = np.random.default_rng(8)
+    for rows, cols in [(1, 64), (3, 64), (4097, 64), (5003, 1024), (1031, 2048), (1025, 4096), (700, 8192), (300, 16384)]:
+        print(f"[norm bwd integers] {rows}x{cols}", flush=True)
+        h = torch.from_numpy(rng.choice([-1.0, 1.0], size=(rows, cols)).astype(np.float32)).cuda()
+        dy = torch.from_numpy(rng.integers(-8, 9, size=(rows, cols)).astype(np.float32)).cuda()
+        dx, dg = torch.empty_like(h), torch.empty(cols, device="cuda")
+        B.add_rms_norm_bwd(dy, h, torch.ones(cols, device="cuda"), dx, dg,
+                           torch.empty(B.add_rms_norm_scratch_elems(rows, cols), device="cuda"), eps=1e-30)
+        assert torch.equal(dg, (dy.double() * h.double()).sum(0).float())
+
+
+# ---------------------------------------------------------------------------
+# Distillation loss
+# ---------------------------------------------------------------------------
+
+class _Loss:
+    """One loss: inputs on the device, the oracle's results and their tolerances."""
+
+    def __init__(self, torch, dtype, tokens, vocab, top, alpha, tau, seed=0, ld=None, ids="int32", teacher="bf16",
+                 labels="int64", std=3.0, change=None):
+        rng = np.random.default_rng(seed + vocab)
+        self.torch, self.dtype, self.vocab = torch, dtype, vocab
+        self.ld = ld or -(-vocab // 8) * 8
+        z = rng.standard_normal(size=(tokens, self.ld), dtype=np.float32) * np.float32(std)
+        self.at = np.stack([rng.choice(vocab, top, replace=top > vocab) for _ in range(tokens)]) if top else None
+        t = -np.sort(-rng.standard_normal(size=(tokens, top)), axis=1).astype(np.float32) * 3
+        self.lab = rng.integers(0, vocab, tokens)
+        w = rng.standard_normal(tokens).astype(np.float32)
+        if top and tokens > 3:
+            self.at[1, top // 2:] = -1                   # fewer entries
+            self.at[2] = [-1, vocab, 2 * vocab, -7][:1] * top  # none
+            self.at[3] = self.at[3, 0]                   # one, many times
+            self.at[0, 0] = self.lab[0]                  # the label is the first entry
+        if tokens > 3:
+            self.lab[1] = -100
+            self.lab[tokens - 1] = vocab                 # no label
+            w[tokens - 2] = 0.0
+        if change:
+            change(self, z, t, w)
+        self.z, zv = _given(z, dtype)
+        self.zv = zv[:, :vocab]
+        self.t, self.tv = _given(t, teacher) if top else (None, None)
+        self.w, self.wv = torch.from_numpy(w).cuda(), w.astype(np.float64)
+        self.ids = torch.from_numpy(self.at).to(getattr(torch, ids)).cuda() if top else None
+        self.labels = torch.from_numpy(self.lab).to(getattr(torch, labels)).cuda() if labels else None
+        self.kw = dict(teacher_ids=self.ids, teacher_logits=self.t, labels=self.labels, alpha=alpha, temperature=tau)
+        with np.errstate(all="ignore"):
+            a = float(np.float32(alpha))
+            self.loss, self.grad, m = O.distill(self.zv, self.at, self.tv, self.lab if labels else None, a, tau)
+            # A sum of exponentials: 8 values a thread and chunk, at most 32 chunks (or batches of four, 128
+            # values, rescaled once each), trees; an exponent's rounding counts |exponent| steps.
+            n = 16 // (2 if dtype == "bf16" else 4)
+            way = 300 + vocab / 512 if vocab > 16384 * n else 8 * 32 + 40
+            self.loss_tol = U * ((way + 60) * (a * tau ** 2 + 1 - a) + 80 * m["loss"])
+            d = np.abs(self.zv - np.max(self.zv, axis=1, keepdims=True))
+            self.grad_tol = (HALF[dtype] * np.abs(self.grad)
+                             + U * ((way + 100 + 8 * np.minimum(d, 100)) * m["plus"] + (top + 100) * m["minus"])) \
+                * np.abs(self.wv)[:, None] + TINY
+            self.grad = self.grad * self.wv[:, None]
+        self.grad[self.wv == 0] = 0
+
+    def whole(self):
+        """(loss, gradient) by the call that gives both."""
+        torch = self.torch
+        loss, lclean = _guarded(torch, (self.z.shape[0],), torch.float32)
+        dz, clean = _guarded(torch, tuple(self.z.shape), self.z.dtype)
+        B.distill_loss_fwd_bwd(self.z, self.w, loss, dz, vocab=self.vocab, **self.kw)
+        torch.cuda.synchronize()
+        assert lclean() and clean()
+        return loss, dz
+
+    def apart(self):
+        """The same by the forward call and its gradient, over the logits."""
+        torch = self.torch
+        T = self.z.shape[0]
+        loss, stats = torch.empty(T, device="cuda"), torch.empty(T, 8, device="cuda")
+        B.distill_loss_fwd(self.z, stats, loss, vocab=self.vocab, **self.kw)
+        dz = self.z.clone()
+        B.distill_loss_bwd(dz, stats, self.w, dz, vocab=self.vocab, **self.kw)
+        torch.cuda.synchronize()
+        return loss, dz
+
+    def shares(self, ranks):
+        torch = self.torch
+        T, per = self.z.shape[0], -(-self.vocab // ranks)
+        ld = -(-per // 8) * 8
+        parts, dz = torch.empty(ranks, T, 8, device="cuda"), []
+        spans = [(r * per, max(0, min(per, self.vocab - r * per))) for r in range(ranks)]
+        pieces = []
+        for first, n in spans:
+            p = torch.full((T, ld), float("nan"), device="cuda", dtype=self.z.dtype)
+            p[:, :n] = self.z[:, first:first + n]
+            pieces.append(p)
+        for p, part, (first, n) in zip(pieces, parts, spans):
+            B.distill_loss_fwd(p, part, vocab=n, first_id=first, vocab_total=self.vocab, **self.kw)
+        stats, loss = torch.empty(T, 8, device="cuda"), torch.empty(T, device="cuda")
+        B.distill_loss_join(parts, stats, loss, alpha=self.kw["alpha"], temperature=self.kw["temperature"])
+        for p, (first, n) in zip(pieces, spans):
+            d = torch.empty_like(p)
+            B.distill_loss_bwd(p, stats, self.w, d, vocab=n, first_id=first, vocab_total=self.vocab, **self.kw)
+            assert not d[:, n:].any()
+            dz.append(d[:, :n])
+        torch.cuda.synchronize()
+        return loss, torch.cat(dz, 1)
+
+    def check(self, got, what, rows=slice(None)):
+        loss, dz = got
+        _close(loss[rows], self.loss[rows], self.loss_tol[rows], what + ": loss")
+        _close(dz[rows, :self.vocab], self.grad[rows], self.grad_tol[rows], what + ": gradient")
+        assert not dz[rows, self.vocab:].any(), what + ": padding"
+
+
+MIX = [(0.5, 1.0), (0.5, 2.0), (0.3, 4.0), (0.6, 3.0), (1.0, 2.0), (0.0, 1.0)]
+# vocabularies at and behind every row layout (chunks of 8 in bf16, 4 in fp32), and odd ones
+VOCABS = [1, 7, 8, 9, 63, 512, 513, 1000, 1024, 1025, 2048, 2049, 3584, 3585, 4097, 6656, 6657, 7168, 7169, 13312, 13313]
+WIDE = [26624, 26625, 38913, 50257, 53248, 53249, 65536, 65537, 77825, 102401, 131073, 200003]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("alpha,tau", MIX)
+@pytest.mark.parametrize("vocab", VOCABS)
+def test_loss_and_gradient(dtype, vocab, alpha, tau):
+    torch = need_gpu()
+    print(f"[distill] {dtype} vocab {vocab} alpha {alpha} T {tau}", flush=True)
+    case = _Loss(torch, dtype, 7, vocab, min(vocab, 37), alpha, tau)
+    case.check(case.whole(), "both")
+    case.check(case.apart(), "apart")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("vocab", WIDE)
+def test_loss_and_gradient_of_wide_rows(dtype, vocab):
+    torch = need_gpu()
+    for alpha, tau in ((0.5, 2.0), (0.6, 3.0)):
+        print(f"[distill] {dtype} vocab {vocab} alpha {alpha} T {tau}", flush=True)
+        case = _Loss(torch, dtype, 5, vocab, 64, alpha, tau, ids="int64", teacher="fp32", labels="int32")
+        case.check(case.whole(), "both")
+        case.check(case.apart(), "apart")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("top", [0, 1, 3, 4, 5, 63, 64, 65, 127, 256, 257, 600, 1023, 1024])
+def test_numbers_of_entries(dtype, top):
+    torch = need_gpu()
+    for vocab in (2000, 30001):
+        print(f"[distill entries] {dtype} top {top} vocab {vocab}", flush=True)
+        case = _Loss(torch, dtype, 6, vocab, top, 0.5, 2.0)
+        case.check(case.whole(), "both")
+        case.check(case.apart(), "apart")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("ranks", [1, 2, 3, 8])
+@pytest.mark.parametrize("alpha,tau", [(0.5, 2.0), (0.6, 3.0), (1.0, 1.0), (0.0, 1.0)])
+def test_shares_of_the_vocabulary(dtype, ranks, alpha, tau):
+    torch = need_gpu()
+    for vocab in (37, 5003):
+        print(f"[distill shares] {dtype} {ranks} ranks vocab {vocab} alpha {alpha} T {tau}", flush=True)
+        case = _Loss(torch, dtype, 9, vocab, 20, alpha, tau)
+        case.check(case.shares(ranks), "shares")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("tokens", [1, 2, 511, 512, 700])
+def test_numbers_of_tokens(dtype, tokens):
+    torch = need_gpu()
+    for vocab in (1200, 9000):
+        print(f"[distill tokens] {dtype} {tokens} vocab {vocab}", flush=True)
+        case = _Loss(torch, dtype, tokens, vocab, 16, 0.5, 2.0)
+        case.check(case.whole(), "both")
+        case.check(case.apart(), "apart")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("vocab", [30, 1000, 7000, 53300, 140000])
+def test_offsets_and_masks(dtype, vocab):
+    """A common offset of the logits changes nothing; masked columns (-infinity, or the type's lowest
+    value) have no probability; a row of lowest values only is uniform."""
+    torch = need_gpu()
+    print(f"[distill masks] {dtype} vocab {vocab}", flush=True)
+    low = float(torch.finfo(_type(torch, dtype)).min)
+
+    def change(self, z, t, w):
+        z[0] += 1024.0
+        z[1] -= 5000.0
+        z[2, 1::2] = -np.inf
+        z[3, 1::2] = low
+        z[4] = low
+        z[5] = -np.inf
+        z[5, vocab // 2] = 1.0
+        z[6] *= 2.0 ** 60           # far apart: one token has all the probability
+        self.at[:7] = (self.at[:7] // 2 * 2) % vocab // 2 * 2  # entries and labels at even columns
+        self.lab[:7] = self.lab[:7] // 2 * 2 % vocab // 2 * 2
+        self.at[5], self.lab[5] = vocab // 2, vocab // 2
+        t[0, 3:] = -np.inf          # no entries
+        w[:7] = [1, 2, -1, 0.5, 1, 1, 1]
+
+    for alpha, tau in ((0.5, 2.0), (0.4, 3.0), (0.5, 1.0), (0.4, 4.0)):
+        case = _Loss(torch, dtype, 9, vocab, 8, alpha, tau, teacher="fp32", change=change)
+        assert np.isfinite(case.loss).all()
+        for got, what in ((case.whole(), "both"), (case.apart(), "apart"), (case.shares(2), "shares")):
+            case.check(got, what)
+            dz = _f64(got[1])
+            assert not dz[2, 1:vocab:2].any() and not dz[3, 1:vocab:2].any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("vocab", [45, 3001, 60001, 140001])
+def test_nonfinite_rows_stay_alone(dtype, vocab):
+    torch = need_gpu()
+    print(f"[distill nonfinite] {dtype} vocab {vocab}", flush=True)
+
+    def change(self, z, t, w):
+        z[0, vocab - 1] = np.nan
+        z[1, vocab // 3] = np.inf
+        z[2] = -np.inf
+        t[3, 1] = np.nan
+        t[4, 0] = np.inf
+        z[5] = np.nan               # no entry and no label
+        self.at[5], self.lab[5] = -1, -1
+        z[6] = np.nan               # a weight of 0
+        w[:] = 1.0
+        w[6] = 0.0
+        self.at[:5], self.lab[:5] = np.arange(8), 2
+        z[7, vocab // 2] = -np.inf  # the label has no probability
+        self.lab[7] = vocab // 2
+
+    for alpha, tau in ((0.5, 2.0), (0.4, 3.0), (0.5, 1.0)):
+        case = _Loss(torch, dtype, 10, vocab, 8, alpha, tau, teacher="fp32", change=change)
+        for got, what in ((case.whole(), "both"), (case.apart(), "apart"), (case.shares(2), "shares")):
+            loss, dz = _f64(got[0]), _f64(got[1])
+            assert np.isnan(loss[:5]).all() and np.isnan(dz[:5, :vocab]).all(), what
+            assert loss[5] == 0 and not dz[5].any() and np.isnan(loss[6]) and not dz[6].any(), what
+            assert loss[7] == np.inf and np.isfinite(dz[7]).all(), what
+            assert not dz[:, vocab:].any(), what
+            case.check(got, what, slice(8, 10))
+    one = _Loss(torch, dtype, 10, vocab, 8, 0.0, 1.0, change=change)  # entries are not looked at
+    assert np.isfinite(_f64(one.whole()[0])[3:5]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_losses_of_the_two_calls_and_runs_are_the_same_bits(dtype):
+    """Nothing depends on timing: the same bits again, with repeated ids and many entries."""
+    torch = need_gpu()
+    for vocab, top in ((900, 64), (20000, 300), (50304, 1024)):
+        print(f"[distill again] {dtype} {vocab} {top}", flush=True)
+
+        def change(self, z, t, w):
+            self.at[:] = self.at // 3 % max(1, vocab // 40)
+
+        case = _Loss(torch, dtype, 64, vocab, top, 0.5, 2.0, change=change)
+        bits = torch.int16 if dtype == "bf16" else torch.int32
+        first, apart = case.whole(), case.apart()
+        for _ in range(3):
+            for a, b in ((first, case.whole()), (apart, case.apart())):
+                assert torch.equal(a[0].view(torch.int32), b[0].view(torch.int32))
+                assert torch.equal(a[1].view(bits), b[1].view(bits))
+
+
+def test_gradient_against_differences():
+    """The gradient against differences of the kernel's own loss.  With steps of 2^-6 in fp32 a
+    central difference is off by step^2 / 6 times a third derivative below 1 (times 2 T^2 for
+    both terms' weights), and by the losses' roundings over the step."""
+    torch = need_gpu()
+    case = _Loss(torch, "fp32", 8, 300, 10, 0.5, 2.0, std=1.0)
+    loss, dz = case.whole()
+    step, rng = 2.0 ** -6, np.random.default_rng(5)
+    for _ in range(8):
+        v = torch.from_numpy(rng.choice([-1.0, 1.0], size=(8, 1)) * (rng.random((8, case.ld)) < 0.02)).float().cuda()
+        ends = []
+        for sign in (1, -1):
+            l = torch.empty(8, device="cuda")
+            B.distill_loss_fwd(case.z + sign * step * v, loss=l, vocab=300, **case.kw)
+            ends.append(_f64(l))
+        slope = (ends[0] - ends[1]) / (2 * step) * case.wv
+        want = (_f64(dz) * v.double().cpu().numpy()).sum(1)
+        tol = np.abs(case.wv) * (step ** 2 / 6 * 8 + 2 * case.loss_tol / step) + 1e-6
+        assert (np.abs(slope - want) <= tol).all(), (slope - want, tol)
