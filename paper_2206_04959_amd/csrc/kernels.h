@@ -185,7 +185,7 @@ hipError_t launch_act8_gemm_dw(int dtype, int tokens, int n_out, int n_in, const
 
 // Residual addition and RMS norm of the sum (rms_norm.hip): r, sum, y and q with scales may be
 // null.  The gradient's scratch: add_rms_norm_scratch_elems floats.
-constexpr int kMaxNormCols = 32768;
+constexpr int kMaxNormCols = 16384;
 hipError_t launch_add_rms_norm_fwd(int dtype, int rows, int cols, float eps, const void* x, const void* r,
                                    const void* g, void* sum, void* y, uint8_t* q, uint8_t* scales, hipStream_t stream);
 size_t add_rms_norm_scratch_elems(int rows, int cols);
