@@ -620,7 +620,7 @@ int merak_add_rms_norm_bwd(int dtype, int rows, int cols, float eps, const void*
  *                   -100, adds no label term
  * top is at most 1024.  With top = 0 or alpha = 0 there is no teacher term (its arrays may be
  * NULL and are not read), with labels NULL or alpha = 1 no label term; one of them must be
- * there.  0 <= alpha <= 1, T > 0.  A token without entry and label has the loss 0, and a
+ * there.  0 <= alpha <= 1, 2^-10 <= T <= 2^10.  A token without entry and label has the loss 0, and a
  * gradient of zeros, whatever its logits are.  A logit of -infinity has the probability 0; a
  * NaN or +infinity makes its token's loss and gradient NaN, as does a row of -infinity only.
  *

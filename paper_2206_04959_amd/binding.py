@@ -704,19 +704,20 @@ def act8_gemm_dw(dy, q, scales, dw, scratch=None, accumulate=False, stream=None)
 
 def _norm_rows(what, x, gamma) -> tuple:
     """(element type, rows, cols) of a row norm's input."""
-    dt = _element(what, x, gamma)
-    cols, n = gamma.numel(), x.numel()
-    if x.dim() == 0 or cols <= 0 or x.shape[-1] != cols:
+    dt, cols, shape = _element(what, x, gamma), gamma.numel(), x.shape
+    if not shape or cols <= 0 or shape[-1] != cols:
         raise ValueError(f"{what}: gamma holds one row's features")
-    rows = n // cols
+    rows = x.numel() // cols
     if (rows | cols) > _INT:
         _too_large(what, rows=rows, cols=cols)
     return dt, rows, cols
 
 
 def _same(what, x, names, *tensors) -> None:
+    dt, shape = x.dtype, x.shape
     for t in tensors:
-        if t is not None and (t.dtype is not x.dtype or t.numel() != x.numel() or t.shape[-1] != x.shape[-1]):
+        if t is not None and (t.dtype is not dt or t.shape != shape and (
+                t.numel() != x.numel() or t.shape[-1:] != shape[-1:])):
             raise ValueError(f"{what}: {names}")
 
 
@@ -770,24 +771,25 @@ DISTILL_STATS = 8  # floats of a token's statistics
 
 def _distill(what, logits, teacher_ids, teacher_logits, labels, vocab):
     """(element type, tokens, vocab, ld), (top, id type, teacher's type, label type) of a loss."""
-    dt = _element(what, logits)
-    if logits.dim() == 0:
+    dt, shape = _element(what, logits), logits.shape
+    if not shape:
         raise ValueError(f"{what}: logits is [tokens, columns]")
-    ld, n = logits.shape[-1], logits.numel()
-    tokens = n // ld if ld else 0
-    vocab = ld if vocab is None else vocab
-    if not 0 <= vocab <= ld:
+    ld = shape[-1]
+    tokens = logits.numel() // ld if ld else 0
+    if vocab is None:
+        vocab = ld
+    elif not 0 <= vocab <= ld:
         raise ValueError(f"{what}: vocab is at most the logits' columns")
-    if (teacher_ids is None) != (teacher_logits is None):
-        raise ValueError(f"{what}: teacher_ids and teacher_logits go together")
     top = it = tt = lt = 0
-    if teacher_ids is not None:
+    if teacher_ids is not None and teacher_logits is not None:
         it, tt = _id_type(what, teacher_ids), _element(what, teacher_logits)
-        count = teacher_ids.numel()
-        top = count // tokens if tokens else 0
-        if teacher_logits.numel() != count or count != top * tokens or (
-                count and (teacher_ids.shape[-1] != top or teacher_logits.shape[-1] != top)):
+        shape = teacher_ids.shape
+        top = shape[-1] if shape else 0
+        if not shape or teacher_ids.numel() != top * tokens or teacher_logits.shape != shape and (
+                teacher_logits.numel() != top * tokens or teacher_logits.shape[-1:] != shape[-1:]):
             raise ValueError(f"{what}: teacher_ids and teacher_logits are [tokens, top]")
+    elif teacher_ids is not None or teacher_logits is not None:
+        raise ValueError(f"{what}: teacher_ids and teacher_logits go together")
     if labels is not None:
         lt = _id_type(what, labels)
         if labels.numel() != tokens:
@@ -805,14 +807,14 @@ def _share(what, vocab: int, first_id: int, vocab_total) -> tuple:
     return first_id, total
 
 
-def _per_token(what, tokens: int, **tensors) -> None:
-    torch = _torch or _load_torch()
-    for name, t in tensors.items():
-        if t is None:
-            continue
-        wide = DISTILL_STATS if name == "stats" else 1
-        if t.dtype is not torch.float32 or t.numel() != tokens * wide or (wide > 1 and t.shape[-1] != wide):
-            raise ValueError(f"{what}: {name} is fp32 [tokens{', 8' if wide > 1 else ''}]")
+def _per_token(what, name, t, tokens: int) -> None:
+    """t (None: not given) is fp32 with one value a token; stats has eight."""
+    if t is None:
+        return
+    wide = DISTILL_STATS if name == "stats" else 1
+    if t.dtype is not (_torch or _load_torch()).float32 or t.numel() != tokens * wide or (
+            wide > 1 and t.shape[-1] != wide):
+        raise ValueError(f"{what}: {name} is fp32 [tokens{', 8' if wide > 1 else ''}]")
 
 
 def distill_loss_fwd(logits, stats=None, loss=None, teacher_ids=None, teacher_logits=None, labels=None, alpha=0.5,
@@ -825,7 +827,8 @@ def distill_loss_fwd(logits, stats=None, loss=None, teacher_ids=None, teacher_lo
     what = "distill_loss_fwd"
     head, tail = _distill(what, logits, teacher_ids, teacher_logits, labels, vocab)
     share = _share(what, head[2], first_id, vocab_total)
-    _per_token(what, head[1], stats=stats, loss=loss)
+    _per_token(what, "stats", stats, head[1])
+    _per_token(what, "loss", loss, head[1])
     if stats is None and loss is None:
         raise ValueError(f"{what}: stats or loss needed")
     if loss is not None and share != (0, head[2]):
@@ -842,7 +845,8 @@ def distill_loss_join(parts, stats, loss, alpha=0.5, temperature=1.0, stream=Non
     the loss of each token."""
     what = "distill_loss_join"
     tokens, ranks = loss.numel(), parts.shape[0] if parts.dim() else 0
-    _per_token(what, tokens, stats=stats, loss=loss)
+    _per_token(what, "stats", stats, tokens)
+    _per_token(what, "loss", loss, tokens)
     if parts.dtype is not stats.dtype or parts.numel() != ranks * stats.numel() or parts.shape[-1] != DISTILL_STATS:
         raise ValueError(f"{what}: parts is fp32 [ranks, tokens, 8]")
     if (tokens | ranks) > _INT:
@@ -859,7 +863,8 @@ def distill_loss_bwd(logits, stats, dloss, dlogits, teacher_ids=None, teacher_lo
     what = "distill_loss_bwd"
     head, tail = _distill(what, logits, teacher_ids, teacher_logits, labels, vocab)
     share = _share(what, head[2], first_id, vocab_total)
-    _per_token(what, head[1], stats=stats, dloss=dloss)
+    _per_token(what, "stats", stats, head[1])
+    _per_token(what, "dloss", dloss, head[1])
     _same(what, logits, "dlogits has the logits' type and shape", dlogits)
     _call(what, "merak_distill_loss_bwd", (*head, *share, *tail, alpha, temperature, logits.data_ptr(),
                                            _ptr(teacher_ids), _ptr(teacher_logits), _ptr(labels), stats.data_ptr(),
@@ -874,7 +879,8 @@ def distill_loss_fwd_bwd(logits, dloss, loss, dlogits, teacher_ids=None, teacher
     token's weight in the step) is known before the loss.  dlogits may be logits itself."""
     what = "distill_loss_fwd_bwd"
     head, tail = _distill(what, logits, teacher_ids, teacher_logits, labels, vocab)
-    _per_token(what, head[1], dloss=dloss, loss=loss)
+    _per_token(what, "dloss", dloss, head[1])
+    _per_token(what, "loss", loss, head[1])
     _same(what, logits, "dlogits has the logits' type and shape", dlogits)
     _call(what, "merak_distill_loss_fwd_bwd", (*head, *tail, alpha, temperature, logits.data_ptr(), _ptr(teacher_ids),
                                                _ptr(teacher_logits), _ptr(labels), dloss.data_ptr(), loss.data_ptr(),

@@ -287,9 +287,11 @@ __device__ __forceinline__ float far_sum(const DistillArgs& a, const T* z, float
 }
 
 template <typename T, int NT>
-__device__ __forceinline__ void write_zeros(T* dz, int lo, int hi) {
-  for (int c = lo + (int)threadIdx.x * Vec<T>::N; c < hi; c += NT * Vec<T>::N)
-    *reinterpret_cast<u32x4_t*>(dz + c) = u32x4_t{0, 0, 0, 0};
+__device__ __forceinline__ void write_zeros(const DistillArgs& a, T* dz, int lo, int hi) {
+  for (int c = lo + (int)threadIdx.x * Vec<T>::N; c < hi; c += NT * Vec<T>::N) {
+    if (a.past) store16<true>(dz + c, u32x4_t{0, 0, 0, 0});
+    else store16<false>(dz + c, u32x4_t{0, 0, 0, 0});
+  }
 }
 
 // The gradient at the columns that have entries, each formed by its first entry's thread from all
@@ -476,7 +478,7 @@ __global__ void __launch_bounds__(NT) distill_kernel(DistillArgs a, const T* z, 
     T* dr = dz + row * a.ld;
     const float w = dloss[row];
     if (idle || w == 0.0f) {
-      write_zeros<T, NT>(dr, 0, a.ld);
+      write_zeros<T, NT>(a, dr, 0, a.ld);
       return;
     }
     const Slopes<M> f(a, r, w, far);
@@ -588,7 +590,7 @@ __global__ void __launch_bounds__(NT) distill_row_kernel(DistillArgs a, const T*
   const Stats r = token_stats<NT, M>(a, en, mx[0], base, mx[1], st, s1, labelled, red[1], &inv, &idle);
   if (threadIdx.x == 0) loss[row] = idle ? 0.0f : loss_of(r, a.alpha, a.tau);
   if (idle || w == 0.0f) {  // whatever the logits are
-    write_zeros<T, NT>(dr, 0, a.ld);
+    write_zeros<T, NT>(a, dr, 0, a.ld);
     return;
   }
 #pragma unroll
@@ -607,7 +609,7 @@ __global__ void __launch_bounds__(NT) distill_row_kernel(DistillArgs a, const T*
       store_at(a.past, v, dr, bytes, off, i, NT * 16);
     }
     write_padding<T, NT>(a, dr, 0);
-    write_zeros<T, NT>(dr, (a.vocab + N - 1) / N * N, a.ld);
+    write_zeros<T, NT>(a, dr, (a.vocab + N - 1) / N * N, a.ld);
   }
 }
 
@@ -627,7 +629,7 @@ __global__ void __launch_bounds__(NT) distill_bwd_kernel(DistillArgs a, int piec
   const Stats s = load_stats(stats + row * kDistillStats);
   const float w = dloss[row];
   if ((s.mass == 0.0f && s.label == 0.0f) || w == 0.0f) {
-    write_zeros<T, NT>(dr, lo, hi);
+    write_zeros<T, NT>(a, dr, lo, hi);
     return;
   }
   const int end = (a.vocab + N - 1) / N * N;  // behind it there are zeros
@@ -669,7 +671,7 @@ __global__ void __launch_bounds__(NT) distill_bwd_kernel(DistillArgs a, int piec
       store_at(a.past, v, dr + lo, bytes, off, u, NT * 16);
     }
     if (lo <= a.vocab && a.vocab < hi) write_padding<T, NT>(a, dr, lo);
-    write_zeros<T, NT>(dr, max(lo, end), hi);
+    write_zeros<T, NT>(a, dr, max(lo, end), hi);
   }
 }
 

@@ -105,7 +105,8 @@ int check_norm(int dtype, int rows, int cols, float eps) {
 }
 
 int check_mix(float alpha, float tau) {
-  if (!(alpha >= 0.0f && alpha <= 1.0f) || !(tau > 0.0f) || !std::isfinite(tau)) return MERAK_ERR_INVALID_ARG;
+  // (the kernels' exponentials are made for these temperatures)
+  if (!(alpha >= 0.0f && alpha <= 1.0f) || !(tau >= 0x1p-10f && tau <= 0x1p10f)) return MERAK_ERR_INVALID_ARG;
   return MERAK_OK;
 }
 
