@@ -33,6 +33,7 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 // A launch's tokens; what it needs of the call.
 struct DistillArgs {
   int tokens, vocab, ld, top;
+  int slots;                     // of the entries' table
   long long first, total;
   float alpha, tau;
   float rate_t, rate_1;          // log2(e) / T, log2(e); with one sum rate_t is its rate
@@ -58,22 +59,68 @@ __device__ __forceinline__ float teacher_at(const DistillArgs& a, size_t i) {
   return a.teacher_bf16 ? bf2f(static_cast<const bf16_t*>(a.teacher)[i]) : static_cast<const float*>(a.teacher)[i];
 }
 
-// A token's entries and its label (entry `top`) in LDS, with room for whole groups of four.  The
-// gradient's values at their columns go to the threads that write those columns' 16 bytes,
-// as a list for each thread.
-struct Entries {
-  int* col;    // own column, or -1
-  float* t;    // teacher's logit; then exp((t - max) / T)
-  float* z;    // student's logit at the column; then the gradient there
-  int* next;   // the next entry of the thread, -1 at the end
-  int* head;   // [threads] the first one
+// A token's entries and its label (entry `top`) in LDS.  For the gradient there is a hash table of
+// their columns too, as an id may be there twice: the column's first and last entry and the sum of
+// its p = exp((t - max) / T) in units of 2^-52, whole numbers, which give the same sum in any order.
+// A column's first entry forms the gradient there, and is listed for the thread that writes the 16
+// bytes around it.
+struct Slot {
+  int col, first, last;
 };
-__host__ __device__ constexpr int entry_room(int top) { return (top + 4) & ~3; }
-__host__ __device__ constexpr size_t entries_bytes(int top, int nt) { return (size_t)entry_room(top) * 16 + nt * 4; }
-__device__ __forceinline__ Entries entries_in(char* lds, int top) {
-  const int n = entry_room(top);
+struct Entries {
+  int* col;     // own column, or -1
+  float* t;     // teacher's logit; then p
+  float* z;     // student's logit at the column; then the gradient there
+  int* next;    // place in the table; then the thread's next entry, -1 at the end
+  // gradient only
+  int* head;    // [threads] the thread's first entry
+  unsigned long long* sum;
+  Slot* slot;
+  int slots;    // a power of two
+};
+__host__ __device__ constexpr int entry_slots(int top) {
+  int n = 32;
+  while (4 * n < 5 * (top + 1)) n *= 2;
+  return n;
+}
+__host__ __device__ constexpr size_t entries_bytes(int top, int nt, bool grad) {
+  return (size_t)(top + 1) * 16 + (grad ? 8 + nt * 4 + (size_t)entry_slots(top) * (8 + sizeof(Slot)) : 0);
+}
+__device__ __forceinline__ Entries entries_in(char* lds, int top, int nt, int slots) {
+  const int n = top + 1;
   int* p = reinterpret_cast<int*>(lds);
-  return Entries{p, reinterpret_cast<float*>(p + n), reinterpret_cast<float*>(p + 2 * n), p + 3 * n, p + 4 * n};
+  Entries en{p, reinterpret_cast<float*>(p + n), reinterpret_cast<float*>(p + 2 * n), p + 3 * n};
+  en.sum = reinterpret_cast<unsigned long long*>(p + 4 * n);  // 16 bytes an entry: aligned
+  en.slot = reinterpret_cast<Slot*>(en.sum + slots);
+  en.head = reinterpret_cast<int*>(en.slot + slots);
+  en.slots = slots;
+  return en;
+}
+
+// An empty table and empty lists; a barrier follows before the first entry.
+template <int NT>
+__device__ __forceinline__ void clear_table(const Entries& en) {
+  for (int i = threadIdx.x; i < en.slots; i += NT) {
+    en.sum[i] = 0;
+    en.slot[i] = Slot{-1, 0x7fffffff, -1};
+  }
+  en.head[threadIdx.x] = -1;
+}
+
+// Entry k, with its p (the label: k = top), into the table.
+__device__ __forceinline__ void into_table(const Entries& en, int top, int k, int c, float p) {
+  int h = (int)(((unsigned)c * 2654435761u >> 8) & (unsigned)(en.slots - 1));
+  for (;;) {  // there are more slots than entries
+    const int was = atomicCAS(&en.slot[h].col, -1, c);
+    if (was == -1 || was == c) break;
+    h = (h + 1) & (en.slots - 1);
+  }
+  en.next[k] = h;
+  atomicMin(&en.slot[h].first, k);
+  if (k < top) {
+    atomicMax(&en.slot[h].last, k);
+    atomicAdd(&en.sum[h], (unsigned long long)__float2ull_rn(p * 0x1p52f));
+  }
 }
 
 // 16 bytes of logits as floats; NONE is -infinity in each of them.
@@ -168,7 +215,7 @@ __device__ __forceinline__ u32x4_t near_logits(u32x4_t r, float base) {
 // The two exponentials, exp((z - base) / T) and exp(z - base): ONE is enough where the loss needs
 // one or T = 1, at T = 2 and T = 4 the second is the first's square or its square's (their c and
 // off are exact multiples then), else there are TWO.  In bf16 the second one is a quarter of the
-// work: loss of 8192 x 50304 162 us with both, 147 so.
+// work: loss of 8192 x 50304 171 us with both (T = 3), 146 so.
 enum Sums { ONE = 0, TWO = 1, SQUARE = 2, FOURTH = 4 };
 template <int M>
 struct Exponents {
@@ -294,35 +341,26 @@ __device__ __forceinline__ void write_zeros(const DistillArgs& a, T* dz, int lo,
   }
 }
 
-// The gradient at the columns that have entries, each formed by its first entry's thread from all
-// that lies on it in the entries' order (columns are compared four at a time: 64 entries cost a
-// thread 16 LDS reads) and listed for the thread that writes the 16 bytes around it, which puts
-// it there.  A column's place in a list is the one thing that depends on timing, and it changes
-// nothing.  (Written by a store of its own behind that of the 16 bytes, each entry cost a part of
-// a line once more: loss and gradient of 32768 x 6288 with 64 entries 266 us, 201 so.)
-// wt: weight of exp((t - max) / T), wl: of the label.  A barrier follows.
+// The gradient at the columns that have entries: the table is filled (behind a barrier), the lists
+// are whole behind the next one.  A column's place in a list is the one thing that depends on
+// timing, and it changes nothing.  wt: weight of p, wl: of the label.
+// (Written by a store of its own behind that of the 16 bytes, each entry cost a part of a line once
+// more: loss and gradient of 32768 x 6288 with 64 entries 266 us, 201 so.  Looking for repeated
+// ids by comparing every pair instead of a table: 8192 x 50304 with 256 entries 409 us,
+// with 1024 1697; so 318 and 600.)
 template <typename T, int NT, int M>
 __device__ __forceinline__ void resolve_entries(const DistillArgs& a, const Slopes<M>& f, const Entries& en, float wt,
                                                 float wl, int lo, bool far, float base) {
-  typedef int i32x4 __attribute__((ext_vector_type(4)));
+  const int label = en.col[a.top];
   for (int e = threadIdx.x; e <= a.top; e += NT) {
     const int c = en.col[e];
     if (c < 0) continue;
-    float p = 0.0f, l = 0.0f;
-    bool first = true;
-    for (int k = 0; k <= a.top; k += 4) {
-      const i32x4 four = *reinterpret_cast<const i32x4*>(en.col + k);
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (four[u] == c) {
-          first = first && k + u >= e;
-          if (k + u < a.top) p += en.t[k + u];
-          else l = wl;
-        }
-    }
-    if (!first) continue;
+    const int h = en.next[e];
+    const Slot s = en.slot[h];
+    if (s.first != e) continue;
+    const float p = e == a.top ? 0.0f : s.first == s.last ? en.t[e] : __ull2float_rn(en.sum[h]) * 0x1p-52f;
     const float z = en.z[e];
-    en.z[e] = f.of(far ? near_logit(z, base) : z) - (wt * p + l);
+    en.z[e] = f.of(far ? near_logit(z, base) : z) - (wt * p + (c == label ? wl : 0.0f));
     en.next[e] = atomicExch(&en.head[(c - lo) / Vec<T>::N % NT], e);
   }
 }
@@ -340,20 +378,20 @@ __device__ __forceinline__ float keep_entry(const DistillArgs& a, const Entries&
   return t != t ? INFINITY : t;  // NaN: no probabilities
 }
 
-// The token's label as entry `top`, and no columns in the places behind it.
+// The token's label as entry `top`.
 template <typename T>
 __device__ __forceinline__ void keep_label(const DistillArgs& a, const Entries& en, const T* zr, long long label) {
   if (threadIdx.x == 0) {
     const int c = column_of(a, label);
     en.col[a.top] = c;
     en.z[a.top] = c >= 0 ? Elem<T>::to_f(zr[c]) : 0.0f;
-    for (int k = a.top + 1; k & 3; ++k) en.col[k] = -1;
   }
 }
 
 // The sums of a token over its workgroup, once its maxima are known: st and s1 are the thread's
-// (relative to base), the rest comes from the entries, which keep exp((t - max) / T).
-template <int NT, int M>
+// (relative to base), the rest comes from the entries, which keep p = exp((t - max) / T) and, for
+// the gradient, go into the table.
+template <int NT, int M, bool GRAD>
 __device__ __forceinline__ Stats token_stats(const DistillArgs& a, const Entries& en, float m, float base, float tmax,
                                              float st, float s1, bool labelled, float* red, float* inv_teacher,
                                              bool* idle) {
@@ -369,12 +407,15 @@ __device__ __forceinline__ Stats token_stats(const DistillArgs& a, const Entries
       continue;
     }
     s[2] += p;
-    if (en.col[k] >= 0) {
+    const int c = en.col[k];
+    if (c >= 0) {
       s[3] += p;
       s[4] += p * (en.z[k] - base);
       s[5] += p * d;
+      if (GRAD) into_table(en, a.top, k, c, p);
     }
   }
+  if (GRAD && threadIdx.x == 0 && en.col[a.top] >= 0) into_table(en, a.top, a.top, en.col[a.top], 0.0f);
   block_reduce<AddOp, NT>(s, red);
   Stats r;
   r.m = m;
@@ -400,8 +441,8 @@ __global__ void __launch_bounds__(NT) distill_kernel(DistillArgs a, const T* z, 
                                                      float* __restrict__ loss, const float* __restrict__ dloss, T* dz) {
   extern __shared__ __align__(16) char smem[];
   __shared__ float red[2][NT / 64 * 6];
-  const Entries en = entries_in(smem, a.top);
-  if (GRAD) en.head[threadIdx.x] = -1;
+  const Entries en = entries_in(smem, a.top, NT, GRAD ? a.slots : 0);
+  if (GRAD) clear_table<NT>(en);
   const size_t row = blockIdx.x;
   const T* zr = z + row * a.ld;
 
@@ -469,7 +510,7 @@ __global__ void __launch_bounds__(NT) distill_kernel(DistillArgs a, const T* z, 
   }
   float inv;
   bool idle;
-  const Stats r = token_stats<NT, M>(a, en, mx[0], base, mx[1], st, s1, labelled, red[1], &inv, &idle);
+  const Stats r = token_stats<NT, M, GRAD>(a, en, mx[0], base, mx[1], st, s1, labelled, red[1], &inv, &idle);
   if (threadIdx.x == 0) {
     if (stats) store_stats(stats + row * kDistillStats, r);
     if (loss) loss[row] = idle ? 0.0f : loss_of(r, a.alpha, a.tau);
@@ -520,8 +561,8 @@ __global__ void __launch_bounds__(NT) distill_row_kernel(DistillArgs a, const T*
   extern __shared__ __align__(16) char smem[];
   __shared__ float red[2][NT / 64 * 6];
   constexpr int N = Vec<T>::N;
-  const Entries en = entries_in(smem, a.top);
-  en.head[threadIdx.x] = -1;
+  const Entries en = entries_in(smem, a.top, NT, a.slots);
+  clear_table<NT>(en);
   const size_t row = blockIdx.x;
   const T* zr = z + row * a.ld;
   T* dr = dz + row * a.ld;
@@ -587,7 +628,7 @@ __global__ void __launch_bounds__(NT) distill_row_kernel(DistillArgs a, const T*
   }
   float inv;
   bool idle;
-  const Stats r = token_stats<NT, M>(a, en, mx[0], base, mx[1], st, s1, labelled, red[1], &inv, &idle);
+  const Stats r = token_stats<NT, M, true>(a, en, mx[0], base, mx[1], st, s1, labelled, red[1], &inv, &idle);
   if (threadIdx.x == 0) loss[row] = idle ? 0.0f : loss_of(r, a.alpha, a.tau);
   if (idle || w == 0.0f) {  // whatever the logits are
     write_zeros<T, NT>(a, dr, 0, a.ld);
@@ -621,7 +662,7 @@ __global__ void __launch_bounds__(NT) distill_bwd_kernel(DistillArgs a, int piec
                                                          const float* __restrict__ dloss, T* dz) {
   extern __shared__ __align__(16) char smem[];
   constexpr int N = Vec<T>::N, piece = NT * N * U;
-  const Entries en = entries_in(smem, a.top);
+  const Entries en = entries_in(smem, a.top, NT, a.slots);
   const size_t row = blockIdx.x / pieces;
   const int lo = (int)(blockIdx.x % pieces) * piece, hi = min(lo + piece, a.ld);
   const T* zr = z + row * a.ld;
@@ -638,21 +679,25 @@ __global__ void __launch_bounds__(NT) distill_bwd_kernel(DistillArgs a, int piec
   u32x4_t raw[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) raw[u] = __builtin_amdgcn_raw_buffer_load_b128(zb, off, u * NT * 16, kPast);
-  en.head[threadIdx.x] = -1;
-  for (int k = threadIdx.x; k < entry_room(a.top); k += NT) {
+  clear_table<NT>(en);
+  __syncthreads();
+  for (int k = threadIdx.x; k <= a.top; k += NT) {
     int c = -1;
+    float p = 0.0f;
     if (k < a.top) {
       const size_t i = row * a.top + k;
       c = column_of(a, id_at(a.ids, a.id64, i));
-      const float p = exp2_fast((teacher_at(a, i) - s.tm) * a.rate_t);
-      en.t[k] = p;
+      p = exp2_fast((teacher_at(a, i) - s.tm) * a.rate_t);
       if (p == 0.0f) c = -1;
-    } else if (k == a.top && a.labels) {
+    } else if (a.labels) {
       c = column_of(a, id_at(a.labels, a.label64, row));
     }
     if (c < lo || c >= hi) c = -1;
     en.col[k] = c;
-    if (c >= 0) en.z[k] = Elem<T>::to_f(zr[c]);
+    if (c < 0) continue;
+    en.t[k] = p;
+    en.z[k] = Elem<T>::to_f(zr[c]);
+    into_table(en, a.top, k, c, p);
   }
   __syncthreads();  // the entries' logits are read, too: dz may be z
   const bool far = is_far(s.m);
@@ -713,6 +758,7 @@ static DistillArgs distill_args(const DistillShape& q) {
   a.want_t = q.top > 0 && q.alpha > 0.0f;
   a.want_1 = q.labels && q.alpha < 1.0f;
   a.top = a.want_t ? q.top : 0;
+  a.slots = entry_slots(a.top);
   a.rate_1 = kLog2e;
   a.rate_t = a.want_t ? kLog2e / q.tau : kLog2e;
   a.id64 = q.id_type == ID_I64, a.label64 = q.label_type == ID_I64, a.teacher_bf16 = q.teacher_type == DT_BF16;
@@ -769,7 +815,7 @@ template <typename T, int NT, int M, bool GRAD>
 static hipError_t run_rows(const DistillCall& c) {
   const DistillShape& q = c.q;
   return over_tokens(q, NT, 1, GRAD ? out_bytes<T>(q) : 0, [&](const DistillArgs& a, long long t) {
-    hipLaunchKernelGGL((distill_kernel<T, NT, M, GRAD>), dim3(a.tokens), dim3(NT), entries_bytes(a.top, NT), c.s, a,
+    hipLaunchKernelGGL((distill_kernel<T, NT, M, GRAD>), dim3(a.tokens), dim3(NT), entries_bytes(a.top, NT, GRAD), c.s, a,
                        (const T*)c.z + t * q.ld, c.stats ? c.stats + t * kDistillStats : nullptr,
                        c.loss ? c.loss + t : nullptr, GRAD ? c.dloss + t : nullptr, GRAD ? (T*)c.dz + t * q.ld : nullptr);
   });
@@ -779,7 +825,7 @@ template <typename T, int NT, int CH, int M>
 static hipError_t run_kept(const DistillCall& c) {
   const DistillShape& q = c.q;
   return over_tokens(q, NT, 1, out_bytes<T>(q), [&](const DistillArgs& a, long long t) {
-    hipLaunchKernelGGL((distill_row_kernel<T, NT, CH, M>), dim3(a.tokens), dim3(NT), entries_bytes(a.top, NT), c.s, a,
+    hipLaunchKernelGGL((distill_row_kernel<T, NT, CH, M>), dim3(a.tokens), dim3(NT), entries_bytes(a.top, NT, true), c.s, a,
                        (const T*)c.z + t * q.ld, c.loss + t, c.dloss + t, (T*)c.dz + t * q.ld);
   });
 }
@@ -815,7 +861,7 @@ static hipError_t run_pieces(const DistillCall& c) {
   const int pieces = (q.ld + piece - 1) / piece;
   return over_tokens(q, NT, pieces, out_bytes<T>(q), [&](const DistillArgs& a, long long t) {
     hipLaunchKernelGGL((distill_bwd_kernel<T, NT, U, M>), dim3((unsigned)(a.tokens * pieces)), dim3(NT),
-                       entries_bytes(a.top, NT), c.s, a, pieces, (const T*)c.z + t * q.ld, c.in + t * kDistillStats,
+                       entries_bytes(a.top, NT, true), c.s, a, pieces, (const T*)c.z + t * q.ld, c.in + t * kDistillStats,
                        c.dloss + t, (T*)c.dz + t * q.ld);
   });
 }
