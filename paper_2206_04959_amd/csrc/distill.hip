@@ -158,9 +158,6 @@ __device__ __forceinline__ u32x4_t first_values(u32x4_t r, int n, float rest) {
 // What a maximum's differences are formed from: 0 where nothing was above -infinity.
 __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.0f : m; }
 
-// The same within 2^50 on both sides, where 2^(z rate - base rate) is formed in one step.
-__device__ __forceinline__ float near_base(float m) { return m == -INFINITY ? 0.0f : fminf(fmaxf(m, -0x1p50f), 0x1p50f); }
-
 // By how much sums relative to the maximum m move to those relative to `base` (sums that are 0
 // stay 0: the difference from a base far below 0 would have no finite exponential).
 __device__ __forceinline__ float moved(float m, float base) { return m == -INFINITY ? 0.0f : m - base; }
@@ -186,7 +183,8 @@ __device__ __forceinline__ Stats load_stats(const float* p) {
 }
 
 // exp((z - base) / T) as 2^(z rate - c), c = base * rate rounded: one fused step an element.  What c
-// is off by, the same for every z, is put back into the sum of them (`off`, a factor next to 1).
+// is off by, the same for every z, is put back into the sum of them (`off`, a factor that stays
+// within 2^-4 and 2^4 for bases up to 2^16, at every temperature).
 struct Exponent {
   float rate, c, base;
   __device__ __forceinline__ Exponent(float base, float rate) : rate(rate), c(base * rate), base(base) {}
@@ -194,23 +192,11 @@ struct Exponent {
   __device__ __forceinline__ float off() const { return exp2_fast(fmaf(-base, rate, c)); }
 };
 
-// A maximum beyond 2^50, such as that of a row that is masked with the type's lowest value, would
-// leave the range on the way.  Any logit below it is so far below that its exponential is 0, at
-// every temperature (2^-10 to 2^10), so there 0 and -infinity stand for the maximum and the rest.
-constexpr float kFar = 0x1p50f;
+// Where the maximum is further out (logits with a large offset; a row that is masked with the type's
+// lowest value) the base is subtracted first and the exponentials' own base is 0.
+constexpr float kFar = 0x1p16f;
 __device__ __forceinline__ bool is_far(float base) { return fabsf(base) > kFar && fabsf(base) < INFINITY; }
-__device__ __forceinline__ float near_logit(float z, float base) {
-  return z == base ? 0.0f : z != z ? z : -INFINITY;
-}
-
-template <typename T>
-__device__ __forceinline__ u32x4_t near_logits(u32x4_t r, float base) {
-  float v[Vec<T>::N];
-  Vec<T>::get(r, v);
-#pragma unroll
-  for (int e = 0; e < Vec<T>::N; ++e) v[e] = near_logit(v[e], base);
-  return Vec<T>::put(v);
-}
+__device__ __forceinline__ float near_base(float m) { return m == -INFINITY ? 0.0f : fminf(fmaxf(m, -kFar), kFar); }
 
 // The two exponentials, exp((z - base) / T) and exp(z - base): ONE is enough where the loss needs
 // one or T = 1, at T = 2 and T = 4 the second is the first's square or its square's (their c and
@@ -252,14 +238,15 @@ struct Slopes {
   }
 };
 
-// 16 bytes of the gradient from those of the logits, of which `n` are columns of the vocabulary.
-template <typename T, int M>
-__device__ __forceinline__ u32x4_t slopes_of(const Slopes<M>& f, u32x4_t z, int n) {
+// 16 bytes of the gradient from those of the logits, less `from`, of which `n` are columns of the
+// vocabulary.
+template <typename T, int M, bool FAR = false>
+__device__ __forceinline__ u32x4_t slopes_of(const Slopes<M>& f, u32x4_t z, int n, float from = 0.0f) {
   constexpr int N = Vec<T>::N;
   float v[N];
   Vec<T>::get(z, v);
 #pragma unroll
-  for (int e = 0; e < N; ++e) v[e] = f.of(v[e]);
+  for (int e = 0; e < N; ++e) v[e] = f.of(FAR ? v[e] - from : v[e]);
   if (n < N) {
 #pragma unroll
     for (int e = 0; e < N; ++e) v[e] = e < n ? v[e] : 0.0f;
@@ -304,14 +291,10 @@ __device__ __forceinline__ void write_slopes(const DistillArgs& a, const Slopes<
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (c0 + NT * N * u < hi) r[u] = *reinterpret_cast<const u32x4_t*>(z + c0 + NT * N * u);
-    if (FAR) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) r[u] = near_logits<T>(r[u], base);
-    }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int c = c0 + NT * N * u;
-      if (c < hi) *reinterpret_cast<u32x4_t*>(dz + c) = with_entries<T>(en, slopes_of<T, M>(f, r[u], a.vocab - c), c);
+      if (c < hi) *reinterpret_cast<u32x4_t*>(dz + c) = with_entries<T>(en, slopes_of<T, M, FAR>(f, r[u], a.vocab - c, base), c);
     }
   }
 }
@@ -325,12 +308,17 @@ __device__ __forceinline__ void write_padding(const DistillArgs& a, T* dz, int l
     for (int c = a.vocab; c % N; ++c) dz[c] = T(0);
 }
 
-// A thread's sum of exponentials where the maximum is far.
-template <typename T, int NT>
-__device__ __forceinline__ float far_sum(const DistillArgs& a, const T* z, float base) {
-  float s = 0.0f;
-  for (int c = threadIdx.x; c < a.vocab; c += NT) s += exp2_fast(near_logit(Elem<T>::to_f(z[c]), base));
-  return s;
+// A thread's sums of exponentials where the maximum is far.
+template <typename T, int NT, int M>
+__device__ __forceinline__ void far_sums(const DistillArgs& a, const T* z, float base, float* st, float* s1) {
+  const Exponents<M> exps(a, 0.0f);
+  *st = *s1 = 0.0f;
+  for (int c = threadIdx.x; c < a.vocab; c += NT) {
+    float et, e1;
+    exps.of(Elem<T>::to_f(z[c]) - base, &et, &e1);
+    *st += et;
+    *s1 += e1;
+  }
 }
 
 template <typename T, int NT>
@@ -360,7 +348,7 @@ __device__ __forceinline__ void resolve_entries(const DistillArgs& a, const Slop
     if (s.first != e) continue;
     const float p = e == a.top ? 0.0f : s.first == s.last ? en.t[e] : __ull2float_rn(en.sum[h]) * 0x1p-52f;
     const float z = en.z[e];
-    en.z[e] = f.of(far ? near_logit(z, base) : z) - (wt * p + (c == label ? wl : 0.0f));
+    en.z[e] = f.of(far ? z - base : z) - (wt * p + (c == label ? wl : 0.0f));
     en.next[e] = atomicExch(&en.head[(c - lo) / Vec<T>::N % NT], e);
   }
 }
@@ -456,7 +444,7 @@ __global__ void __launch_bounds__(NT) distill_kernel(DistillArgs a, const T* z, 
   keep_label(a, en, zr, label);
 
   // Maximum and sums of the logits in one pass: a thread's sums are relative to the maximum of what
-  // it has seen (kept within 2^50: see Exponent), of a batch of U loads at a time.
+  // it has seen (kept within 2^16: see Exponent), of a batch of U loads at a time.
   constexpr int N = Vec<T>::N, U = 4;
   float st = 0.0f, s1 = 0.0f;
   for (int c0 = (int)threadIdx.x * N; c0 < a.vocab; c0 += NT * N * U) {
@@ -503,7 +491,7 @@ __global__ void __launch_bounds__(NT) distill_kernel(DistillArgs a, const T* z, 
   const float base = base_of(mx[0]);
   const bool far = is_far(base);
   if (far) {
-    st = s1 = far_sum<T, NT>(a, zr, base);
+    far_sums<T, NT, M>(a, zr, base, &st, &s1);
   } else if (own != -INFINITY) {
     st *= exp2_fast(fmaf(-base, a.rate_t, Exponent(near_base(own), a.rate_t).c));
     if (M != ONE) s1 *= exp2_fast(fmaf(-base, a.rate_1, Exponent(near_base(own), a.rate_1).c));
@@ -608,7 +596,7 @@ __global__ void __launch_bounds__(NT) distill_row_kernel(DistillArgs a, const T*
   for (int i = 0; i < CH; ++i) forget(raw[i]);
   float st = 0.0f, s1 = 0.0f;
   if (far) {
-    st = s1 = far_sum<T, NT>(a, zr, base);
+    far_sums<T, NT, M>(a, zr, base, &st, &s1);
   } else {
     const Exponents<M> exps(a, base);
 #pragma unroll

@@ -367,6 +367,30 @@ def test_offsets_and_masks(dtype, vocab):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("vocab", [50, 2000, 60000, 140000])
+@pytest.mark.parametrize("tau", [1.0, 2.0, 3.0, 900.0, 2.0 ** -10])
+def test_large_offsets(dtype, vocab, tau):
+    """Offsets on both sides of 2^16, from which on the base is subtracted first, up to 2^40, at ordinary and extreme
+    temperatures; the spread grows with the type's steps out there, so that several logits count."""
+    torch = need_gpu()
+    print(f"[distill offsets] {dtype} vocab {vocab} T {tau}", flush=True)
+    places = [0.0, 2.0 ** 15, -2.0 ** 15, 65000.0, -65000.0, 2.0 ** 17, -2.0 ** 17, 2.0 ** 24, -2.0 ** 30, 2.0 ** 40, -2.0 ** 50]
+
+    def change(self, z, t, w):
+        for i, p in enumerate(places):
+            z[i] = z[i] * max(1.0, min(tau, 50.0)) + p
+        w[:] = 1.0
+
+    case = _Loss(torch, dtype, len(places) + 3, vocab, 8, 0.5, tau, teacher="fp32", change=change)
+    assert np.isfinite(case.loss).all()
+    # An exponent x is off by up to two steps of itself (at T = 2^-10 by more than grad_tol's 8 |z - max|
+    # holds), and exp(-x) x is at most 1/e.
+    case.grad_tol = case.grad_tol + 4 * U * (0.5 * tau + 0.5)
+    for got, what in ((case.whole(), "both"), (case.apart(), "apart"), (case.shares(3), "shares")):
+        case.check(got, what)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("vocab", [45, 3001, 60001, 140001])
 def test_nonfinite_rows_stay_alone(dtype, vocab):
     torch = need_gpu()
