@@ -820,7 +820,9 @@ static hipError_t run_kept(const DistillCall& c) {
 
 // Threads for a row of n chunks of 16 bytes.  A short row has few threads, so that as many bytes
 // are on their way in a CU as its registers hold: 32768 x 6288 (n = 786) loss 88 us with 128
-// threads (108 with 256), loss and gradient 197 with 128 (252 with 256).
+// threads (108 with 256), loss and gradient 197 with 128 (252 with 256).  Few rows have more: what
+// counts then is how long one takes (32 x 6288 8.0 us with 512, 9.7 with 128; 200 x 25152
+// 11.7 with 512, 14.0 with 256; 700 x 25152 22.9 and 23.9).
 template <typename T, int M>
 static hipError_t run_forward(const DistillCall& c) {
   const int n = (c.q.vocab + Vec<T>::N - 1) / Vec<T>::N;
@@ -831,6 +833,10 @@ static hipError_t run_forward(const DistillCall& c) {
   }
   if (n <= 128) return run_kept<T, 64, 2, M>(c);
   if (n <= 256) return run_kept<T, 64, 4, M>(c);
+  if (c.q.tokens <= 1024) {
+    if (n <= 1024) return run_kept<T, 512, 2, M>(c);
+    if (n <= 3584) return run_kept<T, 512, 7, M>(c);
+  }
   if (n <= 512) return run_kept<T, 64, 8, M>(c);
   if (n <= 896) return run_kept<T, 128, 7, M>(c);
   if (n <= 1664) return run_kept<T, 128, 13, M>(c);

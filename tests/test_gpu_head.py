@@ -323,10 +323,11 @@ def test_shares_of_the_vocabulary(dtype, ranks, alpha, tau):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-@pytest.mark.parametrize("tokens", [1, 2, 511, 512, 700])
+@pytest.mark.parametrize("tokens", [1, 2, 511, 512, 700, 1024, 1025])
 def test_numbers_of_tokens(dtype, tokens):
+    """Fewer and more tokens than there are where the row layout and the gradient's pieces change."""
     torch = need_gpu()
-    for vocab in (1200, 9000):
+    for vocab in (1200, 2500, 3600, 7160, 9000, 14000):
         print(f"[distill tokens] {dtype} {tokens} vocab {vocab}", flush=True)
         case = _Loss(torch, dtype, tokens, vocab, 16, 0.5, 2.0)
         case.check(case.whole(), "both")
