@@ -16,8 +16,11 @@
 // statistics.  Ranks' rows join by moving to the largest m.
 //
 // Bound by memory: the logits are read once (maximum and sums in one pass, the sums rescaled
-// when the maximum grows), the gradient is written once.  Sums are fp32, each value of the gradient
-// is formed in fp32 and rounded once, nothing depends on timing.
+// when the maximum grows), the gradient is written once.  8192 x 50304 in bf16 with 64 entries, T =
+// 2: loss 144 us (5.7 TB/s, reading only; a large copy has 5.1 both ways), loss and gradient 297
+// (5.5), gradient from the statistics 305; in fp32 half the rows take 140, 298 and 299.  Three
+// quarters of the loss's time the vector units are busy too: two exponentials a logit.  Sums are
+// fp32, each value of the gradient is formed in fp32 and rounded once, nothing depends on timing.
 #include <algorithm>
 
 #include "common.h"
@@ -67,15 +70,18 @@ __device__ __forceinline__ float teacher_at(const DistillArgs& a, size_t i) {
 struct Slot {
   int col, first, last;
 };
+struct Entry {
+  int col;      // own column, or -1
+  float t;      // teacher's logit; then p
+  float z;      // student's logit at the column; then the bits of the gradient there
+  int next;     // place in the table; then the thread's next entry, -1 at the end
+};
 struct Entries {
-  int* col;     // own column, or -1
-  float* t;     // teacher's logit; then p
-  float* z;     // student's logit at the column; then the gradient there
-  int* next;    // place in the table; then the thread's next entry, -1 at the end
+  Entry* at;
   // gradient only
-  int* head;    // [threads] the thread's first entry
   unsigned long long* sum;
   Slot* slot;
+  int* head;    // [threads] the thread's first entry
   int slots;    // a power of two
 };
 __host__ __device__ constexpr int entry_slots(int top) {
@@ -84,13 +90,12 @@ __host__ __device__ constexpr int entry_slots(int top) {
   return n;
 }
 __host__ __device__ constexpr size_t entries_bytes(int top, int nt, bool grad) {
-  return (size_t)(top + 1) * 16 + (grad ? 8 + nt * 4 + (size_t)entry_slots(top) * (8 + sizeof(Slot)) : 0);
+  return (size_t)(top + 1) * sizeof(Entry) + (grad ? nt * 4 + (size_t)entry_slots(top) * (8 + sizeof(Slot)) : 0);
 }
 __device__ __forceinline__ Entries entries_in(char* lds, int top, int nt, int slots) {
-  const int n = top + 1;
-  int* p = reinterpret_cast<int*>(lds);
-  Entries en{p, reinterpret_cast<float*>(p + n), reinterpret_cast<float*>(p + 2 * n), p + 3 * n};
-  en.sum = reinterpret_cast<unsigned long long*>(p + 4 * n);  // 16 bytes an entry: aligned
+  Entries en;
+  en.at = reinterpret_cast<Entry*>(lds);
+  en.sum = reinterpret_cast<unsigned long long*>(en.at + top + 1);
   en.slot = reinterpret_cast<Slot*>(en.sum + slots);
   en.head = reinterpret_cast<int*>(en.slot + slots);
   en.slots = slots;
@@ -107,6 +112,14 @@ __device__ __forceinline__ void clear_table(const Entries& en) {
   en.head[threadIdx.x] = -1;
 }
 
+// p in units of 2^-52, 0 <= p <= 1 (what is below 2^-52 of it is cut off).
+__device__ __forceinline__ unsigned long long fixed52(float p) {
+  const uint32_t b = __float_as_uint(p);
+  const int shift = (int)(b >> 23) - 127 + 29;  // 24 significant bits at 2^0 are 2^29 units each
+  const unsigned long long m = (b & 0x7fffffu) | 0x800000u;
+  return shift >= 0 ? m << (shift & 63) : shift > -24 ? m >> (-shift & 31) : 0;
+}
+
 // Entry k, with its p (the label: k = top), into the table.
 __device__ __forceinline__ void into_table(const Entries& en, int top, int k, int c, float p) {
   int h = (int)(((unsigned)c * 2654435761u >> 8) & (unsigned)(en.slots - 1));
@@ -115,11 +128,11 @@ __device__ __forceinline__ void into_table(const Entries& en, int top, int k, in
     if (was == -1 || was == c) break;
     h = (h + 1) & (en.slots - 1);
   }
-  en.next[k] = h;
+  en.at[k].next = h;
   atomicMin(&en.slot[h].first, k);
   if (k < top) {
     atomicMax(&en.slot[h].last, k);
-    atomicAdd(&en.sum[h], (unsigned long long)__float2ull_rn(p * 0x1p52f));
+    atomicAdd(&en.sum[h], fixed52(p));
   }
 }
 
@@ -201,7 +214,7 @@ __device__ __forceinline__ float near_base(float m) { return m == -INFINITY ? 0.
 // The two exponentials, exp((z - base) / T) and exp(z - base): ONE is enough where the loss needs
 // one or T = 1, at T = 2 and T = 4 the second is the first's square or its square's (their c and
 // off are exact multiples then), else there are TWO.  In bf16 the second one is a quarter of the
-// work: loss of 8192 x 50304 171 us with both (T = 3), 146 so.
+// work: loss of 8192 x 50304 165 us with both (T = 3), 144 so.
 enum Sums { ONE = 0, TWO = 1, SQUARE = 2, FOURTH = 4 };
 template <int M>
 struct Exponents {
@@ -258,26 +271,31 @@ __device__ __forceinline__ u32x4_t slopes_of(const Slopes<M>& f, u32x4_t z, int 
 template <typename T, int NT>
 __device__ __forceinline__ uint32_t chunks_with_entries(const Entries& en, int lo) {
   uint32_t m = 0;
-  for (int k = en.head[threadIdx.x]; k >= 0; k = en.next[k]) m |= 1u << ((en.col[k] - lo) / (Vec<T>::N * NT));
+  for (int k = en.head[threadIdx.x]; k >= 0; k = en.at[k].next) m |= 1u << ((en.at[k].col - lo) / (Vec<T>::N * NT));
   return m;
 }
 
-// The thread's 16 bytes from column c on, with the entries' values in their places.
-__device__ __forceinline__ void put_value(u32x4_t& v, int e, float x, bf16_t) {
+// x's bits in the place of value e of 16 bytes, if it is one of theirs.
+__device__ __forceinline__ void put_value(u32x4_t& v, int e, uint32_t x, bf16_t) {
+  const uint32_t shift = (e & 1) * 16, mask = 0xffffu << shift, bits = x << shift;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (e == 2 * i) v[i] = (v[i] & 0xffff0000u) | f2bf(x);
-    if (e == 2 * i + 1) v[i] = (v[i] & 0xffffu) | (uint32_t)f2bf(x) << 16;
-  }
+  for (int i = 0; i < 4; ++i) v[i] = (e >> 1) == i ? (v[i] & ~mask) | bits : v[i];
 }
-__device__ __forceinline__ void put_value(u32x4_t& v, int e, float x, float) {
+__device__ __forceinline__ void put_value(u32x4_t& v, int e, uint32_t x, float) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (e == i) v[i] = __float_as_uint(x);
+  for (int i = 0; i < 4; ++i) v[i] = e == i ? x : v[i];
 }
+__device__ __forceinline__ uint32_t bits_of(float x, bf16_t) { return f2bf(x); }
+__device__ __forceinline__ uint32_t bits_of(float x, float) { return __float_as_uint(x); }
+
+// A thread's 16 bytes from column c on, with the entries' values in their places.
 template <typename T>
 __device__ __forceinline__ u32x4_t with_entries(const Entries& en, u32x4_t v, int c) {
-  for (int k = en.head[threadIdx.x]; k >= 0; k = en.next[k]) put_value(v, en.col[k] - c, en.z[k], T());
+  for (int k = en.head[threadIdx.x]; k >= 0;) {
+    const Entry e = en.at[k];
+    put_value(v, e.col - c, __float_as_uint(e.z), T());
+    k = e.next;
+  }
   return v;
 }
 
@@ -294,7 +312,8 @@ __device__ __forceinline__ void write_slopes(const DistillArgs& a, const Slopes<
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int c = c0 + NT * N * u;
-      if (c < hi) *reinterpret_cast<u32x4_t*>(dz + c) = with_entries<T>(en, slopes_of<T, M, FAR>(f, r[u], a.vocab - c, base), c);
+      if (c < hi)
+        *reinterpret_cast<u32x4_t*>(dz + c) = with_entries<T>(en, slopes_of<T, M, FAR>(f, r[u], a.vocab - c, base), c);
     }
   }
 }
@@ -333,23 +352,23 @@ __device__ __forceinline__ void write_zeros(const DistillArgs& a, T* dz, int lo,
 // are whole behind the next one.  A column's place in a list is the one thing that depends on
 // timing, and it changes nothing.  wt: weight of p, wl: of the label.
 // (Written by a store of its own behind that of the 16 bytes, each entry cost a part of a line once
-// more: loss and gradient of 32768 x 6288 with 64 entries 266 us, 201 so.  Looking for repeated
-// ids by comparing every pair instead of a table: 8192 x 50304 with 256 entries 409 us,
-// with 1024 1697; so 318 and 600.)
+// more: loss and gradient of 32768 x 6288 with 64 entries 266 us, 201 so, 174 today.  Looking for
+// repeated ids by comparing every pair instead of a table: 8192 x 50304 with 256 entries 409 us,
+// with 1024 1697; so 298 and 502.)
 template <typename T, int NT, int M>
 __device__ __forceinline__ void resolve_entries(const DistillArgs& a, const Slopes<M>& f, const Entries& en, float wt,
                                                 float wl, int lo, bool far, float base) {
-  const int label = en.col[a.top];
+  const int label = en.at[a.top].col;
   for (int e = threadIdx.x; e <= a.top; e += NT) {
-    const int c = en.col[e];
+    const Entry own = en.at[e];
+    const int c = own.col;
     if (c < 0) continue;
-    const int h = en.next[e];
-    const Slot s = en.slot[h];
+    const Slot s = en.slot[own.next];
     if (s.first != e) continue;
-    const float p = e == a.top ? 0.0f : s.first == s.last ? en.t[e] : __ull2float_rn(en.sum[h]) * 0x1p-52f;
-    const float z = en.z[e];
-    en.z[e] = f.of(far ? z - base : z) - (wt * p + (c == label ? wl : 0.0f));
-    en.next[e] = atomicExch(&en.head[(c - lo) / Vec<T>::N % NT], e);
+    const float p = e == a.top ? 0.0f : s.first == s.last ? own.t : __ull2float_rn(en.sum[own.next]) * 0x1p-52f;
+    const float g = f.of(far ? own.z - base : own.z) - (wt * p + (c == label ? wl : 0.0f));
+    en.at[e].z = __uint_as_float(bits_of(g, T()));
+    en.at[e].next = atomicExch(&en.head[(c - lo) / Vec<T>::N % NT], e);
   }
 }
 
@@ -360,9 +379,9 @@ __device__ __forceinline__ float keep_entry(const DistillArgs& a, const Entries&
                                             float t) {
   const int c = column_of(a, id);
   if (id < 0 || id >= a.total) t = -INFINITY;
-  en.col[k] = c;
-  en.t[k] = t;
-  en.z[k] = c >= 0 ? Elem<T>::to_f(zr[c]) : 0.0f;
+  en.at[k].col = c;
+  en.at[k].t = t;
+  en.at[k].z = c >= 0 ? Elem<T>::to_f(zr[c]) : 0.0f;
   return t != t ? INFINITY : t;  // NaN: no probabilities
 }
 
@@ -371,8 +390,8 @@ template <typename T>
 __device__ __forceinline__ void keep_label(const DistillArgs& a, const Entries& en, const T* zr, long long label) {
   if (threadIdx.x == 0) {
     const int c = column_of(a, label);
-    en.col[a.top] = c;
-    en.z[a.top] = c >= 0 ? Elem<T>::to_f(zr[c]) : 0.0f;
+    en.at[a.top].col = c;
+    en.at[a.top].z = c >= 0 ? Elem<T>::to_f(zr[c]) : 0.0f;
   }
 }
 
@@ -384,26 +403,28 @@ __device__ __forceinline__ Stats token_stats(const DistillArgs& a, const Entries
                                              float st, float s1, bool labelled, float* red, float* inv_teacher,
                                              bool* idle) {
   const float tm = base_of(tmax);
-  const float zl = en.z[a.top];  // (its place is used again behind the next barrier)
+  const float zl = en.at[a.top].z;  // (its place is used again behind the next barrier)
   // S_T, S_1, teacher's sum, mass here, sum p (z - m), sum p t
   float s[6] = {st, s1, 0.0f, 0.0f, 0.0f, 0.0f};
   for (int k = threadIdx.x; k < a.top; k += NT) {
-    const float d = en.t[k] - tm, p = exp2_fast(d * a.rate_t);
-    en.t[k] = p;
+    const float d = en.at[k].t - tm, p = exp2_fast(d * a.rate_t);
+    en.at[k].t = p;
     if (p == 0.0f) {
-      en.col[k] = -1;
+      en.at[k].col = -1;
       continue;
     }
     s[2] += p;
-    const int c = en.col[k];
-    if (c >= 0) {
+    if (en.at[k].col >= 0) {
       s[3] += p;
-      s[4] += p * (en.z[k] - base);
+      s[4] += p * (en.at[k].z - base);
       s[5] += p * d;
-      if (GRAD) into_table(en, a.top, k, c, p);
     }
   }
-  if (GRAD && threadIdx.x == 0 && en.col[a.top] >= 0) into_table(en, a.top, a.top, en.col[a.top], 0.0f);
+  if (GRAD) {  // (in a loop of its own: both at once need registers that the row has)
+    for (int k = threadIdx.x; k < a.top; k += NT)
+      if (en.at[k].col >= 0) into_table(en, a.top, k, en.at[k].col, en.at[k].t);
+    if (threadIdx.x == 0 && en.at[a.top].col >= 0) into_table(en, a.top, a.top, en.at[a.top].col, 0.0f);
+  }
   block_reduce<AddOp, NT>(s, red);
   Stats r;
   r.m = m;
@@ -413,7 +434,7 @@ __device__ __forceinline__ Stats token_stats(const DistillArgs& a, const Entries
   r.ts = s[2];
   const float inv = s[2] != 0.0f ? 1.0f / s[2] : 0.0f;
   r.mass = s[3] * inv;
-  r.label = labelled && en.col[a.top] >= 0 ? 1.0f : 0.0f;
+  r.label = labelled && en.at[a.top].col >= 0 ? 1.0f : 0.0f;
   r.lin = 0.0f;
   if (s[2] != 0.0f) r.lin = a.alpha * a.tau * (inv * s[4] - inv * s[5] + a.tau * r.mass * logf(s[2]));
   if (r.label != 0.0f) r.lin += (1.0f - a.alpha) * (zl - base);
@@ -681,10 +702,10 @@ __global__ void __launch_bounds__(NT) distill_bwd_kernel(DistillArgs a, int piec
       c = column_of(a, id_at(a.labels, a.label64, row));
     }
     if (c < lo || c >= hi) c = -1;
-    en.col[k] = c;
+    en.at[k].col = c;
     if (c < 0) continue;
-    en.t[k] = p;
-    en.z[k] = Elem<T>::to_f(zr[c]);
+    en.at[k].t = p;
+    en.at[k].z = Elem<T>::to_f(zr[c]);
     into_table(en, a.top, k, c, p);
   }
   __syncthreads();  // the entries' logits are read, too: dz may be z
@@ -820,7 +841,7 @@ static hipError_t run_kept(const DistillCall& c) {
 
 // Threads for a row of n chunks of 16 bytes.  A short row has few threads, so that as many bytes
 // are on their way in a CU as its registers hold: 32768 x 6288 (n = 786) loss 88 us with 128
-// threads (108 with 256), loss and gradient 197 with 128 (252 with 256).  Few rows have more: what
+// threads (108 with 256), loss and gradient 197 with 128 (252 with 256; both 174 and less today).  Few rows have more: what
 // counts then is how long one takes (32 x 6288 8.0 us with 512, 9.7 with 128; 200 x 25152
 // 11.7 with 512, 14.0 with 256; 700 x 25152 22.9 and 23.9).
 template <typename T, int M>
