@@ -54,8 +54,7 @@ __device__ __forceinline__ long long id_at(const void* p, bool wide, size_t i) {
 
 // The token's own columns of the vocabulary, -1 for an id that is another rank's or none's.
 __device__ __forceinline__ int column_of(const DistillArgs& a, long long id) {
-  const long long c = id - a.first;
-  return id >= 0 && id < a.total && c >= 0 && c < a.vocab ? (int)c : -1;
+  return id >= a.first && id < a.total && id - a.first < a.vocab ? (int)(id - a.first) : -1;
 }
 
 __device__ __forceinline__ float teacher_at(const DistillArgs& a, size_t i) {
@@ -174,6 +173,14 @@ __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.0f
 // By how much sums relative to the maximum m move to those relative to `base` (sums that are 0
 // stay 0: the difference from a base far below 0 would have no finite exponential).
 __device__ __forceinline__ float moved(float m, float base) { return m == -INFINITY ? 0.0f : m - base; }
+
+// A sum or maximum over the workgroup, behind which all its threads see the entries in LDS (a
+// workgroup of one wave exchanges nothing through LDS for it, so the barrier comes by itself).
+template <typename Op, int NT, int N>
+__device__ __forceinline__ void reduce_behind_barrier(float (&v)[N], float* red) {
+  block_reduce<Op, NT>(v, red);
+  if constexpr (NT == 64) __syncthreads();
+}
 
 struct Stats {
   float m, s1, st, lin, mass, label, tm, ts;
@@ -425,7 +432,7 @@ __device__ __forceinline__ Stats token_stats(const DistillArgs& a, const Entries
       if (en.at[k].col >= 0) into_table(en, a.top, k, en.at[k].col, en.at[k].t);
     if (threadIdx.x == 0 && en.at[a.top].col >= 0) into_table(en, a.top, a.top, en.at[a.top].col, 0.0f);
   }
-  block_reduce<AddOp, NT>(s, red);
+  reduce_behind_barrier<AddOp, NT>(s, red);
   Stats r;
   r.m = m;
   r.st = a.want_t ? s[0] : 0.0f;
@@ -508,7 +515,7 @@ __global__ void __launch_bounds__(NT) distill_kernel(DistillArgs a, const T* z, 
     mx[0] = m;
   }
   const float own = mx[0];
-  block_reduce<MaxOp, NT>(mx, red[0]);
+  reduce_behind_barrier<MaxOp, NT>(mx, red[0]);
   const float base = base_of(mx[0]);
   const bool far = is_far(base);
   if (far) {
@@ -610,7 +617,7 @@ __global__ void __launch_bounds__(NT) distill_row_kernel(DistillArgs a, const T*
 #pragma unroll
     for (int e = 0; e < N; ++e) mx[0] = fmaxf(mx[0], v[e]);
   }
-  block_reduce<MaxOp, NT>(mx, red[0]);
+  reduce_behind_barrier<MaxOp, NT>(mx, red[0]);
   const float base = base_of(mx[0]);
   const bool far = is_far(base);
 #pragma unroll

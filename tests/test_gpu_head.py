@@ -425,6 +425,23 @@ def test_nonfinite_rows_stay_alone(dtype, vocab):
     assert np.isfinite(_f64(one.whole()[0])[3:5]).all()
 
 
+@pytest.mark.parametrize("ranks", [1, 3])
+def test_ids_far_outside_the_vocabulary(ranks):
+    """Ids and labels at the ends of 64 bits, and around a share's ends, are no entries."""
+    torch = need_gpu()
+    for vocab in (90, 5000):
+        print(f"[distill ids] {ranks} ranks vocab {vocab}", flush=True)
+        wild = [-2 ** 63, -2 ** 63 + vocab, -2 ** 62, -1, vocab, 2 ** 31, 2 ** 32, 2 ** 32 + 5, 2 ** 63 - 1, -2 ** 32 + 1]
+
+        def change(self, z, t, w):
+            for k, i in enumerate(wild):
+                self.at[k % 8, 1 + k // 8] = i
+                self.lab[k % 8] = i
+
+        case = _Loss(torch, "bf16", 9, vocab, 12, 0.5, 2.0, ids="int64", change=change)
+        case.check(case.shares(ranks) if ranks > 1 else case.whole(), "wild ids")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_losses_of_the_two_calls_and_runs_are_the_same_bits(dtype):
     """Nothing depends on timing: the same bits again, with repeated ids and many entries."""
