@@ -848,26 +848,45 @@ static hipError_t run_kept(const DistillCall& c) {
 
 // Threads for a row of n chunks of 16 bytes.  A short row has few threads, so that as many bytes
 // are on their way in a CU as its registers hold: 32768 x 6288 (n = 786) loss 88 us with 128
-// threads (108 with 256), loss and gradient 197 with 128 (252 with 256; both 174 and less today).  Few rows have more: what
+// threads (108 with 256), loss and gradient 197 with 128 (252 with 256).  Few rows have more: what
 // counts then is how long one takes (32 x 6288 8.0 us with 512, 9.7 with 128; 200 x 25152
-// 11.7 with 512, 14.0 with 256; 700 x 25152 22.9 and 23.9).
+// 11.7 with 512, 14.0 with 256; 700 x 25152 22.9 and 23.9).  So have rows with many entries, whose
+// table leaves room for fewer workgroups in a CU from 205 and from 410 entries on.  Loss and
+// gradient of 8192 x 3496: with 192 entries 63 us on 128 threads and 64 on 256, with 256 72 and
+// 61; on 256 and 512 with 408 entries 83 and 94, with 512 86 and 83, with 1024 235 and 160.  The loss
+// alone, of 8192 x 1000: 256 entries 14.6 us on 64 threads and 17.9 on 128, 512 28.5 and 24.3,
+// 768 35.3 on 128 and 31.6 on 256; of 8192 x 6288 512 entries 54 on 128 and 41 on 256; of 8192 x 12568
+// 1024 entries 93 on 256 and 78 on 512.
+static bool many_entries(int top) { return entry_slots(top) >= 512; }       // 205 and more
+static bool most_entries(int top) { return entry_slots(top) >= 1024; }      // 410 and more
+
+static int loss_threads(int n, int top) {
+  if (n <= 256) return top <= 256 ? 64 : top <= 512 ? 128 : 256;
+  const int few = n <= 1024 ? 128 : n <= 2048 ? 256 : 512;
+  return few < 512 && top > 2 * few ? 2 * few : few;
+}
+
 template <typename T, int M>
 static hipError_t run_forward(const DistillCall& c) {
-  const int n = (c.q.vocab + Vec<T>::N - 1) / Vec<T>::N;
+  const int n = (c.q.vocab + Vec<T>::N - 1) / Vec<T>::N, top = distill_args(c.q).top;
   if (!c.dz) {
-    if (n <= 256) return run_rows<T, 64, M, false>(c);
-    if (n <= 1024) return run_rows<T, 128, M, false>(c);
-    return n <= 2048 ? run_rows<T, 256, M, false>(c) : run_rows<T, 512, M, false>(c);
+    switch (loss_threads(n, top)) {
+      case 64: return run_rows<T, 64, M, false>(c);
+      case 128: return run_rows<T, 128, M, false>(c);
+      case 256: return run_rows<T, 256, M, false>(c);
+      default: return run_rows<T, 512, M, false>(c);
+    }
   }
-  if (n <= 128) return run_kept<T, 64, 2, M>(c);
-  if (n <= 256) return run_kept<T, 64, 4, M>(c);
-  if (c.q.tokens <= 1024) {
+  if ((c.q.tokens <= 1024 && n > 256) || most_entries(top)) {
     if (n <= 1024) return run_kept<T, 512, 2, M>(c);
     if (n <= 3584) return run_kept<T, 512, 7, M>(c);
   }
+  if (many_entries(top) && n <= 1024) return run_kept<T, 256, 4, M>(c);
+  if (n <= 128) return run_kept<T, 64, 2, M>(c);
+  if (n <= 256) return run_kept<T, 64, 4, M>(c);
   if (n <= 512) return run_kept<T, 64, 8, M>(c);
   if (n <= 896) return run_kept<T, 128, 7, M>(c);
-  if (n <= 1664) return run_kept<T, 128, 13, M>(c);
+  if (n <= 1792) return run_kept<T, 256, 7, M>(c);  // 4096 x 12568, 64 entries 51 us (55 with 128 x 13)
   if (n <= 3328) return run_kept<T, 256, 13, M>(c);
   if (n <= 6656) return run_kept<T, 512, 13, M>(c);
   if (n <= 9728) return run_kept<T, 512, 19, M>(c);
@@ -888,14 +907,21 @@ static hipError_t run_pieces(const DistillCall& c) {
   });
 }
 
+// Threads and pieces of a row of n chunks.  Many entries: as above (4096 x 6288 with 256 entries
+// 47 us on 128 threads and 38 on 256; 8192 x 1000 with 1024 184 on 256 and 133 on 512; 2048 x 25152
+// with 512 69 on 256 and 60 on 512).  One piece a row up to 3328 chunks; longer ones are cut small
+// (8192 x 50304 268 us with U = 4, 302 with 13), and so are few rows (1 x 50304 8.0 and 9.6), but
+// for a number of rows that fills the card once in large pieces (600 x 50304 29.0 and 24.7).
 template <typename T, int M>
 static hipError_t run_backward(const DistillCall& c) {
-  const int n = c.q.ld / Vec<T>::N;
+  const int n = c.q.ld / Vec<T>::N, tokens = c.q.tokens, top = distill_args(c.q).top;
+  if (n <= 1024 && many_entries(top))
+    return entry_slots(top) >= 2048 ? run_pieces<T, 512, 2, M>(c) : run_pieces<T, 256, 4, M>(c);
+  if (most_entries(top)) return run_pieces<T, 512, 7, M>(c);
   if (n <= 128) return run_pieces<T, 64, 2, M>(c);
   if (n <= 896) return run_pieces<T, 128, 7, M>(c);
-  // Few rows are cut into more pieces: 1 x 50304 8.0 us with U = 4 (9.6 with 13); 2047 x 25152
-  // 50 us with U = 13 (55 with 4).
-  return c.q.tokens < 512 ? run_pieces<T, 256, 4, M>(c) : run_pieces<T, 256, 13, M>(c);
+  if (tokens < 512 || (n > 3328 && tokens >= 1024)) return run_pieces<T, 256, 4, M>(c);
+  return n <= 1792 ? run_pieces<T, 256, 7, M>(c) : run_pieces<T, 256, 13, M>(c);
 }
 
 template <typename T, int M>

@@ -312,6 +312,18 @@ def test_numbers_of_entries(dtype, top):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("top", [204, 205, 409, 410, 819, 820])
+def test_many_entries(dtype, top):
+    """Numbers of entries from which a row has more threads, in rows and on calls of each layout."""
+    torch = need_gpu()
+    for tokens, vocab in ((6, 600), (6, 4097), (6, 8192), (6, 8200), (5, 28672), (5, 28680), (1025, 700), (1025, 3500)):
+        print(f"[distill entries] {dtype} top {top} tokens {tokens} vocab {vocab}", flush=True)
+        case = _Loss(torch, dtype, tokens, vocab, top, 0.5, 2.0)
+        case.check(case.whole(), "both")
+        case.check(case.apart(), "apart")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("ranks", [1, 2, 3, 8])
 @pytest.mark.parametrize("alpha,tau", [(0.5, 2.0), (0.6, 3.0), (1.0, 1.0), (0.0, 1.0)])
 def test_shares_of_the_vocabulary(dtype, ranks, alpha, tau):

@@ -14,7 +14,7 @@ def test_no_kernel_spills(src, least):
     assert not spills, spills
     if src == "distill.hip":  # 13 chunks of 16 bytes a thread: 52 of at most 80 registers
         kept = {k: v["Occupancy"] for k, v in rows.items() if "distill_row_kernel" in k and "ELi13ELi" in k}
-        assert len(kept) == 24 and min(kept.values()) >= 6, kept
+        assert len(kept) == 16 and min(kept.values()) >= 6, kept
     else:                     # the gradient's workgroups of 1024 threads: one a CU at least twice over
         most = {k: v["Occupancy"] for k, v in rows.items() if "rms_bwd_kernel" in k}
         assert most and min(most.values()) >= 4, most
