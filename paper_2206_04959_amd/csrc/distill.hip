@@ -17,8 +17,8 @@
 //
 // Bound by memory: the logits are read once (maximum and sums in one pass, the sums rescaled
 // when the maximum grows), the gradient is written once.  8192 x 50304 in bf16 with 64 entries, T =
-// 2: loss 144 us (5.7 TB/s, reading only; a large copy has 5.1 both ways), loss and gradient 297
-// (5.5), gradient from the statistics 305; in fp32 half the rows take 140, 298 and 299.  Three
+// 2: loss 142 us (5.8 TB/s, reading only; a large copy has 5.1 both ways), loss and gradient 295
+// (5.6), gradient from the statistics 270 (6.1); in fp32 half the rows take 140, 298 and 270.  Three
 // quarters of the loss's time the vector units are busy too: two exponentials a logit.  Sums are
 // fp32, each value of the gradient is formed in fp32 and rounded once, nothing depends on timing.
 #include <algorithm>
@@ -91,7 +91,7 @@ __host__ __device__ constexpr int entry_slots(int top) {
 __host__ __device__ constexpr size_t entries_bytes(int top, int nt, bool grad) {
   return (size_t)(top + 1) * sizeof(Entry) + (grad ? nt * 4 + (size_t)entry_slots(top) * (8 + sizeof(Slot)) : 0);
 }
-__device__ __forceinline__ Entries entries_in(char* lds, int top, int nt, int slots) {
+__device__ __forceinline__ Entries entries_in(char* lds, int top, int slots) {
   Entries en;
   en.at = reinterpret_cast<Entry*>(lds);
   en.sum = reinterpret_cast<unsigned long long*>(en.at + top + 1);
@@ -359,9 +359,9 @@ __device__ __forceinline__ void write_zeros(const DistillArgs& a, T* dz, int lo,
 // are whole behind the next one.  A column's place in a list is the one thing that depends on
 // timing, and it changes nothing.  wt: weight of p, wl: of the label.
 // (Written by a store of its own behind that of the 16 bytes, each entry cost a part of a line once
-// more: loss and gradient of 32768 x 6288 with 64 entries 266 us, 201 so, 174 today.  Looking for
+// more: loss and gradient of 32768 x 6288 with 64 entries 266 us, 201 so.  Looking for
 // repeated ids by comparing every pair instead of a table: 8192 x 50304 with 256 entries 409 us,
-// with 1024 1697; so 298 and 502.)
+// with 1024 1697; so 300 and 501.)
 template <typename T, int NT, int M>
 __device__ __forceinline__ void resolve_entries(const DistillArgs& a, const Slopes<M>& f, const Entries& en, float wt,
                                                 float wl, int lo, bool far, float base) {
@@ -457,7 +457,7 @@ __global__ void __launch_bounds__(NT) distill_kernel(DistillArgs a, const T* z, 
                                                      float* __restrict__ loss, const float* __restrict__ dloss, T* dz) {
   extern __shared__ __align__(16) char smem[];
   __shared__ float red[2][NT / 64 * 6];
-  const Entries en = entries_in(smem, a.top, NT, GRAD ? a.slots : 0);
+  const Entries en = entries_in(smem, a.top, GRAD ? a.slots : 0);
   if (GRAD) clear_table<NT>(en);
   const size_t row = blockIdx.x;
   const T* zr = z + row * a.ld;
@@ -577,7 +577,7 @@ __global__ void __launch_bounds__(NT) distill_row_kernel(DistillArgs a, const T*
   extern __shared__ __align__(16) char smem[];
   __shared__ float red[2][NT / 64 * 6];
   constexpr int N = Vec<T>::N;
-  const Entries en = entries_in(smem, a.top, NT, a.slots);
+  const Entries en = entries_in(smem, a.top, a.slots);
   clear_table<NT>(en);
   const size_t row = blockIdx.x;
   const T* zr = z + row * a.ld;
@@ -678,7 +678,7 @@ __global__ void __launch_bounds__(NT) distill_bwd_kernel(DistillArgs a, int piec
                                                          const float* __restrict__ dloss, T* dz) {
   extern __shared__ __align__(16) char smem[];
   constexpr int N = Vec<T>::N, piece = NT * N * U;
-  const Entries en = entries_in(smem, a.top, NT, a.slots);
+  const Entries en = entries_in(smem, a.top, a.slots);
   const size_t row = blockIdx.x / pieces;
   const int lo = (int)(blockIdx.x % pieces) * piece, hi = min(lo + piece, a.ld);
   const T* zr = z + row * a.ld;
