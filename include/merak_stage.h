@@ -618,9 +618,9 @@ int merak_add_rms_norm_bwd(int dtype, int rows, int cols, float eps, const void*
  *                   no entry
  *   labels          [tokens] of label_type; a label outside 0 .. vocab_total - 1, such as
  *                   -100, adds no label term
- * top is at most 1024.  With top = 0 or alpha = 0 there is no teacher term (its arrays may be
- * NULL and are not read), with labels NULL or alpha = 1 no label term; one of them must be
- * there.  0 <= alpha <= 1, 2^-10 <= T <= 2^10.  A token without entry and label has the loss 0, and a
+ * top is at most 1024.  With top = 0 or alpha = 0 there is no teacher term, with labels NULL or
+ * alpha = 1 no label term (the arrays and types of a term that is not there are not looked at; they
+ * may be NULL and anything); one of them must be there.  0 <= alpha <= 1, 2^-10 <= T <= 2^10.  A token without entry and label has the loss 0, and a
  * gradient of zeros, whatever its logits are.  A logit of -infinity has the probability 0; a
  * NaN or +infinity makes its token's loss and gradient NaN, as does a row of -infinity only.
  *

@@ -112,6 +112,10 @@ int check_mix(float alpha, float tau) {
 
 int check_id_type(int t) { return t == MERAK_I32 || t == MERAK_I64 ? MERAK_OK : MERAK_ERR_INVALID_ARG; }
 
+// The loss's terms that have a weight; the arrays of another one are not looked at.
+bool has_teacher(const DistillShape& q) { return q.top > 0 && q.alpha > 0.0f; }
+bool has_labels(const DistillShape& q) { return q.labels && q.alpha < 1.0f; }
+
 int check_distill(int dtype, const DistillShape& q, const void* logits) {
   TRY(check_dtype(dtype));
   TRY(check_mix(q.alpha, q.tau));
@@ -120,24 +124,29 @@ int check_distill(int dtype, const DistillShape& q, const void* logits) {
     return MERAK_ERR_SHAPE;
   if (q.first < 0 || q.total < q.vocab || q.first > q.total - q.vocab) return MERAK_ERR_INVALID_ARG;
   TRY(check_ptr(logits));
-  if (q.top > 0) {
+  if (has_teacher(q)) {
     TRY(check_id_type(q.id_type));
     TRY(check_dtype(q.teacher_type));
     TRY(check_ptr(q.ids)); TRY(check_ptr(q.teacher));
   }
-  if (q.labels) {
+  if (has_labels(q)) {
     TRY(check_id_type(q.label_type));
     TRY(check_ptr(q.labels));
   }
-  const bool teacher = q.top > 0 && q.alpha > 0.0f, labels = q.labels && q.alpha < 1.0f;
-  return teacher || labels ? MERAK_OK : MERAK_ERR_INVALID_ARG;  // else nothing to learn from
+  return has_teacher(q) || has_labels(q) ? MERAK_OK : MERAK_ERR_INVALID_ARG;  // else nothing to learn from
 }
 
 size_t logits_bytes(int dtype, const DistillShape& q) { return (size_t)q.tokens * q.ld * elem(dtype); }
 size_t stats_bytes(int tokens) { return (size_t)tokens * kDistillStats * sizeof(float); }
-Span ids_span(const DistillShape& q) { return {q.ids, (size_t)q.tokens * q.top * id_bytes(q.id_type)}; }
-Span teacher_span(const DistillShape& q) { return {q.teacher, (size_t)q.tokens * q.top * elem(q.teacher_type)}; }
-Span labels_span(const DistillShape& q) { return {q.labels, (size_t)q.tokens * id_bytes(q.label_type)}; }
+Span ids_span(const DistillShape& q) {
+  return {q.ids, has_teacher(q) ? (size_t)q.tokens * q.top * id_bytes(q.id_type) : 0};
+}
+Span teacher_span(const DistillShape& q) {
+  return {q.teacher, has_teacher(q) ? (size_t)q.tokens * q.top * elem(q.teacher_type) : 0};
+}
+Span labels_span(const DistillShape& q) {
+  return {q.labels, has_labels(q) ? (size_t)q.tokens * id_bytes(q.label_type) : 0};
+}
 
 }  // namespace
 

@@ -492,3 +492,33 @@ def test_gradient_against_differences():
         want = (_f64(dz) * v.double().cpu().numpy()).sum(1)
         tol = np.abs(case.wv) * (step ** 2 / 6 * 8 + 2 * case.loss_tol / step) + 1e-6
         assert (np.abs(slope - want) <= tol).all(), (slope - want, tol)
+
+
+@pytest.mark.parametrize("vocab", [100, 2000])
+def test_a_term_without_weight_needs_no_arrays(vocab):
+    """At the C entry points, alpha = 0 with `top` entries but no arrays of them is the labels' loss, and
+    alpha = 1 with a label type that is none the teacher's."""
+    torch = need_gpu()
+    print(f"[distill weights] vocab {vocab}", flush=True)
+    T, ld, stream = 5, -(-vocab // 8) * 8, torch.cuda.current_stream().cuda_stream
+    L, case = B.lib(), _Loss(torch, "bf16", T, vocab, 6, 0.5, 2.0)
+    for alpha, top, given in ((0.0, 6, (None, None, case.labels.data_ptr())),
+                              (1.0, 6, (case.ids.data_ptr(), case.t.data_ptr(), case.labels.data_ptr()))):
+        got, want = [[torch.empty(T, device="cuda"), torch.empty(T, 8, device="cuda"), torch.empty(T, device="cuda"),
+                      torch.empty_like(case.z), torch.empty_like(case.z)] for _ in range(2)]
+        kinds = (0, 0, 1) if alpha == 0.0 else (0, 0, 9)
+        for loss, stats, loss2, dz, dz2 in (got,):
+            mix = (top, *kinds, alpha, 2.0, case.z.data_ptr(), *given)
+            assert L.merak_distill_loss_fwd_bwd(0, T, vocab, ld, *mix, case.w.data_ptr(), loss.data_ptr(), dz.data_ptr(),
+                                                stream) == 0
+            assert L.merak_distill_loss_fwd(0, T, vocab, ld, 0, vocab, *mix, stats.data_ptr(), loss2.data_ptr(), stream) == 0
+            assert L.merak_distill_loss_bwd(0, T, vocab, ld, 0, vocab, *mix, stats.data_ptr(), case.w.data_ptr(),
+                                            dz2.data_ptr(), stream) == 0
+        kw = dict(labels=case.labels) if alpha == 0.0 else dict(teacher_ids=case.ids, teacher_logits=case.t)
+        kw.update(alpha=alpha, temperature=2.0, vocab=vocab)
+        B.distill_loss_fwd_bwd(case.z, case.w, want[0], want[3], **kw)
+        B.distill_loss_fwd(case.z, want[1], want[2], **kw)
+        B.distill_loss_bwd(case.z, want[1], case.w, want[4], **kw)
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a.view(torch.int16), b.view(torch.int16))

@@ -131,6 +131,21 @@ def test_largest_sizes_reach_the_launch():
                                     FAR[3], FAR[4], None, None) == INVALID
 
 
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the calls would be launched")
+@pytest.mark.parametrize("call", [_loss, _grad, _both])
+def test_arrays_of_a_term_without_weight_are_not_looked_at(call):
+    """With alpha = 0 the teacher's arrays and their types, with alpha = 1 the labels, may be anything
+    (the calls get as far as the launch, which fails here, without a GPU); `top` keeps its limits."""
+    for change in (dict(ids=None, t=None), dict(ids=None), dict(t=None), dict(ids=P[1] + 8, t=P[2] + 2),
+                   dict(id_type=7, teacher=7), dict(ids=P[0], t=P[0]), dict(ids=P[6], t=P[5]), dict(top=0)):
+        assert call(alpha=0.0, **change) == HIP, change
+    for change in (dict(labels=None), dict(labels=P[3] + 4), dict(label_type=7), dict(labels=P[5]), dict(labels=P[0])):
+        assert call(alpha=1.0, **change) == HIP, change
+    assert call(alpha=0.0, top=1025) == SHAPE and call(alpha=0.0, top=-1) == SHAPE
+    assert call(alpha=1.0, ids=None) == INVALID and call(alpha=0.0, label_type=7) == INVALID
+    assert call(alpha=2.0 ** -30, ids=None, t=None) == INVALID and call(alpha=1.0 - 2.0 ** -24, label_type=7) == INVALID
+
+
 def _t(*shape, dtype=torch.bfloat16):
     return torch.zeros(shape, dtype=dtype)
 
