@@ -587,9 +587,10 @@ int merak_act8_gemm_dw(int dtype, int tokens, int n_out, int n_in, const void* d
  *   y          [rows, cols] of dtype
  *   q, scales  y as an activation checkpoint in 8 bits (above; cols % 32 == 0), taken from
  *              the unrounded y: what merak_act8_gemm_dw reads as its X.
- * Squares are summed in fp32: magnitudes above 2^63 overflow (y is then 0).  cols % 8 == 0, at
- * most 16384 (else MERAK_ERR_UNSUPPORTED); rows at most 2^30; eps > 0; with q rows * cols at
- * most 2^40. */
+ * The row's sum may have any finite magnitudes, here and in the gradient: where squares leave fp32
+ * they are taken of a scaled row.  (Small ones lose bits below 2^-63 each, which shows only with an
+ * eps as small as their squares.)  cols % 8 == 0, at most 16384 (else MERAK_ERR_UNSUPPORTED); rows
+ * at most 2^30; eps > 0; with q rows * cols at most 2^40. */
 int merak_add_rms_norm_fwd(int dtype, int rows, int cols, float eps, const void* x, const void* resid,
                            const void* gamma, void* sum, void* y, uint8_t* q, uint8_t* scales, void* stream);
 

@@ -65,6 +65,14 @@ __device__ __forceinline__ void put8(float* p, const float v[8]) {
                                  __float_as_uint(v[i + 3])});
 }
 
+// Where a row's squares leave fp32 (a sum of 2^128: a row of 16384 features of 2^57) the sums are taken
+// again of 2^-80 h, whose squares stay below 2^110; rstd is 2^-80 times that of the scaled row,
+// down to 2^-128 (22 bits).  The branch is the whole row's, taken by no ordinary one.
+constexpr float kUnit = 0x1p-80f;
+__device__ __forceinline__ float scaled_rstd(float squares, int cols, float eps) {
+  return 1.0f / sqrtf(squares / (float)cols + eps * kUnit * kUnit);
+}
+
 struct NormFwd {
   int rows, cols;
   float eps;
@@ -101,7 +109,19 @@ __global__ void __launch_bounds__(threads_of(NT)) rms_fwd_kernel(NormFwd a, cons
     }
   }
   block_reduce<AddOp, NT>(s, red);
-  const float rstd = 1.0f / sqrtf(s[0] / (float)a.cols + a.eps);
+  float rstd = 1.0f / sqrtf(s[0] / (float)a.cols + a.eps);
+  if (s[0] == INFINITY) {
+    s[0] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      if ((j + NT * i) * 8 >= a.cols) continue;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[0] += (h[i][e] * kUnit) * (h[i][e] * kUnit);
+    }
+    if constexpr (NT > 64) __syncthreads();  // the first sums are read
+    block_reduce<AddOp, NT>(s, red);
+    rstd = scaled_rstd(s[0], a.cols, a.eps) * kUnit;
+  }
 #pragma unroll
   for (int i = 0; i < CH; ++i) {
     const int c = (j + NT * i) * 8;
@@ -190,8 +210,30 @@ __global__ void __launch_bounds__(threads_of(NT)) rms_bwd_kernel(int rows, int c
     if (AHEAD && row + step < rows) load_row(row + step);
     block_reduce<AddOp, NT>(t, red + buf);
     buf ^= 2 * (NT / 64);  // two areas in turn: one barrier a row is enough
-    const float rstd = 1.0f / sqrtf(t[0] / (float)cols + eps);
-    const float m = t[1] * rstd / (float)cols;  // mean(dy g n)
+    float rstd = 1.0f / sqrtf(t[0] / (float)cols + eps);
+    float m = t[1] * rstd / (float)cols;  // mean(dy g n)
+    if (t[0] == INFINITY) {
+      t[0] = t[1] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        const int c = (j + NT * i) * 8;
+        if (c >= cols) continue;
+        float g8[8];
+        if (!AHEAD) w[i].load(g + c);
+        w[i].get(g8);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float u = hv[i][e] * kUnit;
+          t[0] += u * u;
+          t[1] += dv[i][e] * g8[e] * u;
+        }
+      }
+      block_reduce<AddOp, NT>(t, red + buf);
+      buf ^= 2 * (NT / 64);
+      rstd = scaled_rstd(t[0], cols, eps);
+      m = t[1] * rstd / (float)cols;
+      rstd *= kUnit;
+    }
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
       const int c = (j + NT * i) * 8;

@@ -156,6 +156,43 @@ def test_norm_of_zeros_and_of_nonfinite_rows(dtype, cols):
     assert bool(torch.isfinite(dx[1]).all()) and bool(torch.isnan(dx[3]).all()) and bool(torch.isnan(dg).all())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("cols", [8, 64, 1024, 2048, 4096, 8192, 16384])
+def test_norm_of_large_magnitudes(dtype, cols):
+    """Rows whose squares leave fp32, alone or only in their sum, beside ordinary ones: magnitudes from below
+    2^57 (16384 of them sum to 2^128) to the type's largest, in whole rows and in one feature."""
+    torch = need_gpu()
+    print(f"[norm large] {dtype} {cols}", flush=True)
+    rng = np.random.default_rng(cols)
+    powers = [0, 50, 55, 56, 57, 58, 60, 62, 63, 64, 65, 80, 100, 120, 125, 126]
+    v = rng.uniform(1.0, 2.0, size=(2 * len(powers), cols)) * rng.choice([-1.0, 1.0], size=(2 * len(powers), cols))
+    for i, p in enumerate(powers):
+        v[i] *= 2.0 ** p
+        v[len(powers) + i, cols // 2] *= 2.0 ** p
+    x, xv = _given(v.astype(np.float32), dtype)
+    g, gv = _normal(rng, (cols,), dtype, 0.1, 1.0)
+    rows, eps = x.shape[0], float(np.float32(1e-6))
+    y, eight = torch.empty_like(x), cols % 32 == 0
+    q = torch.empty(rows, cols, dtype=torch.uint8, device="cuda") if eight else None
+    sc = torch.empty(rows, cols // 32, dtype=torch.uint8, device="cuda") if eight else None
+    B.add_rms_norm_fwd(x, g, y, q=q, scales=sc)
+    ref = O.rms_norm(xv, gv, eps)
+    norm = NORM + 8 * U  # the inverse root has 22 bits at 2^-128
+    _close(y, ref, (HALF[dtype] + norm) * np.abs(ref) + TINY, "y")
+    if eight and dtype == "fp32":
+        q2, sc2 = torch.empty_like(q), torch.empty_like(sc)
+        B.act8_save(y, q2, sc2)
+        assert torch.equal(q, q2) and torch.equal(sc, sc2)
+    dy, dyv = _normal(rng, (rows, cols), dtype)
+    dx, dg = torch.empty_like(x), torch.empty(cols, device="cuda")
+    for some in (slice(0, rows), slice(4, 8)):  # many workgroups; one
+        n = dyv[some].shape[0]
+        B.add_rms_norm_bwd(dy[some], x[some], g, dx[some], dg, torch.empty(B.add_rms_norm_scratch_elems(n, cols), device="cuda"))
+        rx, rg, mag, gmag = O.rms_norm_backward(dyv[some], xv[some], gv, None, eps)
+        _close(dx[some], rx, HALF[dtype] * np.abs(rx) + 110 * U * mag + TINY, "dx")
+        _close(dg, rg, (rows / 256 + 40) * U * gmag + 2 * norm * gmag + TINY, "dgamma")
+
+
 def test_norm_gradient_sums_integers_exactly():
     """h of +-1 and eps far below 1 ulp make n = h exactly; integer gradients then sum exactly in any
     order, so one lost or doubled term shows."""
