@@ -147,11 +147,15 @@ __global__ void __launch_bounds__(threads_of(NT)) rms_fwd_kernel(NormFwd a, cons
   }
 }
 
+constexpr int kRun = 256;  // rows that a thread of the gradient adds up one after the other
+
 // The workgroups step through the rows; each thread keeps its columns' sums of dy * n, and a
 // workgroup's go to part[workgroup][cols] (without part there is one workgroup, whose sums are
 // the gain's gradient).  With one chunk a thread a row's loads are issued while the row before
 // it is reduced and written: 16384 x 1920 in bf16 57 -> 51 us, x 6144 156 -> 144; with more the
 // registers would not hold both.  dx may be dy or ds: a row is loaded whole before it is written.
+// A thread's sum of kRun rows goes into memory (into LDS with 64 threads a row) and the next one starts
+// at 0, so a column's longest chain of additions is kRun + rows / (rows at a time) / kRun and a tree.
 template <typename T, int NT, int CH, bool PAST>
 __global__ void __launch_bounds__(threads_of(NT)) rms_bwd_kernel(int rows, int cols, float eps, const T* dy,
                                                                  const T* ds, const T* __restrict__ h,
@@ -160,7 +164,7 @@ __global__ void __launch_bounds__(threads_of(NT)) rms_bwd_kernel(int rows, int c
                                                                  int accumulate) {
   constexpr int R = threads_of(NT) / NT;
   constexpr bool AHEAD = CH == 1;
-  __shared__ float red[NT > 64 ? 2 * 2 * (NT / 64) : R * CH * 512];
+  __shared__ __align__(16) float red[NT > 64 ? 2 * 2 * (NT / 64) : R * CH * 512];
   const int j = threadIdx.x % NT;
   const long long step = (long long)gridDim.x * R;
   float sum[CH][8];
@@ -186,6 +190,25 @@ __global__ void __launch_bounds__(threads_of(NT)) rms_bwd_kernel(int rows, int c
   const long long first = (long long)blockIdx.x * R + threadIdx.x / NT;
   if (AHEAD && first < rows) load_row(first);
   int buf = 0;
+  float* const out = part ? part + (size_t)blockIdx.x * cols : dg;
+  // The thread's sums to its place, on top of what is there if `add`.
+  auto give = [&](bool add) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const int c = (j + NT * i) * 8;
+      if (c >= cols) continue;
+      float* const to = NT > 64 ? out + c : red + (threadIdx.x / NT) * CH * 512 + c;
+      if (add) {
+        float before[8];
+        load8(to, before);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[i][e] += before[e];
+      }
+      store8(to, sum[i]);
+    }
+  };
+  bool given = false;
+  int run = 0;
   for (long long row = first; row < rows; row += step) {
     const size_t at = (size_t)row * cols;
     if (!AHEAD) load_row(row);
@@ -255,27 +278,21 @@ __global__ void __launch_bounds__(threads_of(NT)) rms_bwd_kernel(int rows, int c
       }
       put8<PAST>(dx + at + c, o[i]);
     }
+    if (++run == kRun) {  // (one workgroup without part has four rows)
+      give(given);
+      given = true;
+      run = 0;
+#pragma unroll
+      for (int i = 0; i < CH; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[i][e] = 0.0f;
+    }
   }
-  float* const out = part ? part + (size_t)blockIdx.x * cols : dg;
   const bool add = !part && accumulate;
   if constexpr (NT > 64) {
-#pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      const int c = (j + NT * i) * 8;
-      if (c >= cols) continue;
-      if (add) {
-        float before[8];
-        load8(out + c, before);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum[i][e] += before[e];
-      }
-      store8(out + c, sum[i]);
-    }
+    give(given || add);
   } else {
-#pragma unroll
-    for (int i = 0; i < CH; ++i)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) red[(threadIdx.x / NT) * CH * 512 + (j + NT * i) * 8 + e] = sum[i][e];
+    give(given);
     __syncthreads();
     for (int c = threadIdx.x; c < cols; c += 256) {
       const float v = (red[c] + red[CH * 512 + c]) + (red[2 * CH * 512 + c] + red[3 * CH * 512 + c]);

@@ -208,6 +208,61 @@ def test_norm_gradient_sums_integers_exactly():
         assert torch.equal(dg, (dy.double() * h.double()).sum(0).float())
 
 
+# a width of each layout of the gradient, with the rows that it takes at once
+@pytest.mark.parametrize("cols,at_once", [(8, 2048), (520, 1024), (1032, 512), (2056, 256), (4104, 256), (8200, 256)])
+def test_norm_gradient_of_many_rows(cols, at_once):
+    """Equal terms, whose roundings all go one way: h of 1 and an eps far below 1 ulp make n = 1, and a dy of
+    1 + half a step of fp32 at half of 2048 (less one step at 1) would lose that half in each of the last 1024 of
+    2048 additions in a row.  A column's additions, one behind the other: 256, the runs of 256, the tree."""
+    torch = need_gpu()
+    n = 4096 if cols == 8 else 2048   # rows a thread
+    rows = n * at_once
+    print(f"[norm bwd many rows] {rows}x{cols}", flush=True)
+    dy = torch.full((rows, cols), 1.0 + n / 2 * 2.0 ** -24 - 2.0 ** -23, device="cuda")
+    term = float(dy[0, 0])
+    assert term != 1.0 and float(dy[0, 0] + n / 2) == n / 2 + 1.0
+    h, dg = torch.ones_like(dy), torch.empty(cols, device="cuda")
+    start = torch.full_like(dg, 3.0)
+    scratch, clean = _guarded(torch, (B.add_rms_norm_scratch_elems(rows, cols),), torch.float32)
+    for accumulate in (False, True):
+        dy.fill_(term)
+        if accumulate:
+            dg.copy_(start)
+        B.add_rms_norm_bwd(dy, h, torch.ones(cols, device="cuda"), dy, dg, scratch, eps=1e-30, accumulate=accumulate)
+        torch.cuda.synchronize()
+        want = np.full(cols, rows * term + (3.0 if accumulate else 0.0))
+        _close(dg, want, (256 + n / 256 + 40) * U * want, "dgamma")
+    assert clean()
+
+
+def test_norm_gradient_of_half_a_million_rows():
+    """Whole dgamma of 540000 x 8192, and of an odd part of its rows, against 64-bit sums."""
+    torch = need_gpu()
+    print("[norm bwd half a million rows]", flush=True)
+    rows, cols, eps = 540000, 8192, float(np.float32(1e-6))
+    h, dy = [torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(4)
+    for a in range(0, rows, 60000):
+        h[a:a + 60000].normal_(generator=gen)
+        dy[a:a + 60000].normal_(mean=0.5, generator=gen)
+    g = torch.randn(cols, device="cuda", generator=gen).bfloat16()
+    dx, dg = torch.empty_like(h), torch.empty(cols, device="cuda")
+    for n in (rows, 131073):
+        want, size = torch.zeros(cols, dtype=torch.float64, device="cuda"), torch.zeros(cols, dtype=torch.float64, device="cuda")
+        for a in range(0, n, 20000):
+            v = h[a:min(a + 20000, n)].double()
+            v *= torch.rsqrt(v.square().mean(1, keepdim=True) + eps)
+            v *= dy[a:min(a + 20000, n)]
+            want += v.sum(0)
+            size += v.abs().sum(0)
+        B.add_rms_norm_bwd(dy[:n], h[:n], g, dx[:n], dg,
+                           torch.empty(B.add_rms_norm_scratch_elems(n, cols), device="cuda"))
+        torch.cuda.synchronize()
+        # each term is off by NORM and a product
+        _close(dg, _f64(want), ((256 + rows / 256 / 256 + 40) * U + 2 * NORM) * _f64(size), "dgamma")
+
+
 # ---------------------------------------------------------------------------
 # Distillation loss
 # ---------------------------------------------------------------------------
