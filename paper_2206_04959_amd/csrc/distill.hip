@@ -334,16 +334,40 @@ __device__ __forceinline__ void write_padding(const DistillArgs& a, T* dz, int l
     for (int c = a.vocab; c % N; ++c) dz[c] = T(0);
 }
 
-// A thread's sums of exponentials where the maximum is far.
+// A thread's maximum and sums of a part of its columns, relative to near_base(m).
+struct Part {
+  float m, st, s1;
+};
+
+template <int M>
+__device__ __forceinline__ void join_part(const DistillArgs& a, Part& all, const Part& p) {
+  if (all.m == -INFINITY || p.m == -INFINITY) {  // a sum of nothing is 0 (or NaN) and stays it, wherever the base goes
+    all = Part{fmaxf(all.m, p.m), all.st + p.st, all.s1 + p.s1};
+    return;
+  }
+  const float m = fmaxf(all.m, p.m);
+  const Exponents<M> now(a, near_base(m)), x(a, near_base(all.m)), y(a, near_base(p.m));
+  all.st = all.st * exp2_fast(x.t.c - now.t.c) + p.st * exp2_fast(y.t.c - now.t.c);
+  if (M != ONE) all.s1 = all.s1 * exp2_fast(x.one.c - now.one.c) + p.s1 * exp2_fast(y.one.c - now.one.c);
+  all.m = m;
+}
+
+// A thread's sums of exponentials where the maximum is far, kFarRun at a time.
+constexpr int kFarRun = 1024;
 template <typename T, int NT, int M>
 __device__ __forceinline__ void far_sums(const DistillArgs& a, const T* z, float base, float* st, float* s1) {
   const Exponents<M> exps(a, 0.0f);
   *st = *s1 = 0.0f;
-  for (int c = threadIdx.x; c < a.vocab; c += NT) {
-    float et, e1;
-    exps.of(Elem<T>::to_f(z[c]) - base, &et, &e1);
-    *st += et;
-    *s1 += e1;
+  for (int c = threadIdx.x; c < a.vocab;) {
+    float rt = 0.0f, r1 = 0.0f;
+    for (int n = 0; n < kFarRun && c < a.vocab; ++n, c += NT) {
+      float et, e1;
+      exps.of(Elem<T>::to_f(z[c]) - base, &et, &e1);
+      rt += et;
+      r1 += e1;
+    }
+    *st += rt;
+    *s1 += r1;
   }
 }
 
@@ -472,9 +496,12 @@ __global__ void __launch_bounds__(NT) distill_kernel(DistillArgs a, const T* z, 
   keep_label(a, en, zr, label);
 
   // Maximum and sums of the logits in one pass: a thread's sums are relative to the maximum of what
-  // it has seen (kept within 2^16: see Exponent), of a batch of U loads at a time.
-  constexpr int N = Vec<T>::N, U = 4;
-  float st = 0.0f, s1 = 0.0f;
+  // it has seen (kept within 2^16: see Exponent), of a batch of U loads at a time.  A batch is
+  // summed by itself, and so are kRun of them, so that a row of 2^28 columns (2^19 a thread) has no
+  // chain of more than about 800 additions and rescalings in fp32.
+  constexpr int N = Vec<T>::N, U = 4, kRun = 128;
+  Part all{-INFINITY, 0.0f, 0.0f}, p = all;
+  int run = 0;
   for (int c0 = (int)threadIdx.x * N; c0 < a.vocab; c0 += NT * N * U) {
     u32x4_t raw[U];
 #pragma unroll
@@ -483,7 +510,7 @@ __global__ void __launch_bounds__(NT) distill_kernel(DistillArgs a, const T* z, 
       if (c < a.vocab) raw[u] = *reinterpret_cast<const u32x4_t*>(zr + c);
       else raw[u] = u32x4_t{Vec<T>::NONE, Vec<T>::NONE, Vec<T>::NONE, Vec<T>::NONE};
     }
-    float m = mx[0];
+    float m = p.m;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int c = c0 + NT * N * u;
@@ -493,13 +520,13 @@ __global__ void __launch_bounds__(NT) distill_kernel(DistillArgs a, const T* z, 
 #pragma unroll
       for (int e = 0; e < N; ++e) m = fmaxf(m, v[e]);
     }
-    const float base = near_base(m);
-    const Exponents<M> exps(a, base);
-    if (m > mx[0] && mx[0] != -INFINITY) {  // (a sum of nothing stays 0, wherever the base goes)
-      const Exponents<M> old(a, near_base(mx[0]));
-      st *= exp2_fast(old.t.c - exps.t.c);
-      if (M != ONE) s1 *= exp2_fast(old.one.c - exps.one.c);
+    const Exponents<M> exps(a, near_base(m));
+    if (m > p.m && p.m != -INFINITY) {  // (a sum of nothing stays 0, wherever the base goes)
+      const Exponents<M> old(a, near_base(p.m));
+      p.st *= exp2_fast(old.t.c - exps.t.c);
+      if (M != ONE) p.s1 *= exp2_fast(old.one.c - exps.one.c);
     }
+    float bt = 0.0f, b1 = 0.0f;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       float v[N];
@@ -508,16 +535,23 @@ __global__ void __launch_bounds__(NT) distill_kernel(DistillArgs a, const T* z, 
       for (int e = 0; e < N; ++e) {
         float et, e1;
         exps.of(v[e], &et, &e1);
-        st += et;
-        if (M != ONE) s1 += e1;
+        bt += et;
+        if (M != ONE) b1 += e1;
       }
     }
-    mx[0] = m;
+    p = Part{m, p.st + bt, p.s1 + b1};
+    if (++run == kRun) {
+      join_part<M>(a, all, p);
+      p = Part{-INFINITY, 0.0f, 0.0f};
+      run = 0;
+    }
   }
-  const float own = mx[0];
+  join_part<M>(a, all, p);
+  const float own = mx[0] = all.m;
   reduce_behind_barrier<MaxOp, NT>(mx, red[0]);
   const float base = base_of(mx[0]);
   const bool far = is_far(base);
+  float st = all.st, s1 = all.s1;
   if (far) {
     far_sums<T, NT, M>(a, zr, base, &st, &s1);
   } else if (own != -INFINITY) {

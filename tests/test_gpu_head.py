@@ -586,6 +586,69 @@ def test_gradient_against_differences():
         assert (np.abs(slope - want) <= tol).all(), (slope - want, tol)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("alpha,tau", [(0.0, 1.0), (0.5, 2.0), (0.4, 3.0), (0.5, 900.0)])
+def test_sums_of_the_widest_rows(dtype, alpha, tau):
+    """Rows of nearly 2^28 columns (2^19 a thread): one logit above equal ones, normal ones, ascending ones and
+    one far from 0, against 64-bit sums.  A thread's terms: 32 in a row, 128 such sums with a rescaling, 128 of
+    those in bf16 and 256 in fp32, each rescaling a factor that is off by two steps and a product, then the tree; or 1024 and 512
+    where the maximum is far."""
+    torch = need_gpu()
+    print(f"[distill widest] {dtype} alpha {alpha} T {tau}", flush=True)
+    V, ld, top, way = 2 ** 28 - 3, 2 ** 28, 4, 1700
+    dt, f64 = _type(torch, dtype), torch.float64
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(6)
+    z = torch.empty(4, ld, dtype=dt, device="cuda")
+    z[0], z[0, 12345678] = -0.75, 0.0
+    z[1].normal_(std=2.0, generator=gen)
+    z[2] = torch.linspace(-8.0, 0.0, ld, device="cuda")
+    z[3], z[3, 200000001] = 2.0 ** 17 - 1024.0, 2.0 ** 17
+    ids = torch.tensor([[12345678, 5, 2 ** 28 - 4, 7], [1, 2, 3, 4], [2 ** 28 - 4, 2 ** 27, 9, 3], [200000001, 1, 2, 3]], device="cuda")
+    lab = torch.tensor([12345678, 77, 2 ** 28 - 4, 200000001], device="cuda")
+    t = torch.randn(4, top, device="cuda", generator=gen)
+    w = torch.tensor([1.0, 0.5, 2.0, -1.0], device="cuda")
+    kw = dict(teacher_ids=ids, teacher_logits=t, labels=lab, alpha=alpha, temperature=tau, vocab=V)
+    loss, loss2, stats, dz = torch.empty(4, device="cuda"), torch.empty(4, device="cuda"), torch.empty(4, 8, device="cuda"), \
+        torch.empty_like(z)
+    B.distill_loss_fwd_bwd(z, w, loss, dz, **kw)
+    B.distill_loss_fwd(z, stats, loss2, **kw)
+    a, piece = float(np.float32(alpha)), 2 ** 24
+    cuts = [slice(c, min(c + piece, V)) for c in range(0, V, piece)]
+    for r in range(4):
+        m = z[r, :V].max().to(f64)
+        s_t, s_1 = [sum(torch.exp((z[r, c].to(f64) - m) / k).sum() for c in cuts) for k in (tau, 1.0)]
+        p = torch.softmax(t[r].to(f64) / tau, 0)
+        d, dl = z[r, ids[r]].to(f64) - m, z[r, lab[r]].to(f64) - m
+        want = a * tau ** 2 * (p * (torch.log(p) - d / tau + torch.log(s_t))).sum() + (1 - a) * (torch.log(s_1) - dl)
+        size = a * tau ** 2 * (p * (torch.log(p).abs() + d.abs() / tau + 1)).sum() + (1 - a) * (dl.abs() + 1)
+        tol = U * ((way + 60) * (a * tau ** 2 + 1 - a) + 80 * float(size))
+        for l in (loss, loss2):
+            assert abs(float(l[r]) - float(want)) <= tol, (r, float(l[r]), float(want), tol)
+    for turn in range(2):  # the gradient of the call that gives both; the one from the statistics, in the logits' place
+        got = dz
+        if turn:
+            got = z.clone()
+            B.distill_loss_bwd(got, stats, w, got, **kw)
+        for r in range(4):
+            m = z[r, :V].max().to(f64)
+            s_t, s_1 = [sum(torch.exp((z[r, c].to(f64) - m) / k).sum() for c in cuts) for k in (tau, 1.0)]
+            p = torch.softmax(t[r].to(f64) / tau, 0)
+            for c in cuts:
+                d = z[r, c].to(f64) - m
+                plus = a * tau * torch.exp(d / tau) / s_t + (1 - a) * torch.exp(d) / s_1
+                minus = torch.zeros_like(plus)
+                for k in range(top):
+                    if c.start <= int(ids[r, k]) < c.stop:
+                        minus[int(ids[r, k]) - c.start] += a * tau * p[k]
+                if c.start <= int(lab[r]) < c.stop:
+                    minus[int(lab[r]) - c.start] += 1 - a
+                tol = HALF[dtype] * (plus - minus).abs() + U * ((way + 100 + 8 * d.abs().clamp(max=100)) * plus + (top + 100) * minus)
+                off = (got[r, c].to(f64) - float(w[r]) * (plus - minus)).abs()
+                assert bool((off <= tol * abs(float(w[r])) + TINY).all()), (turn, r, c, float((off - tol).max()))
+        assert not got[:, V:].any()
+
+
 @pytest.mark.parametrize("vocab", [100, 2000])
 def test_a_term_without_weight_needs_no_arrays(vocab):
     """At the C entry points, alpha = 0 with `top` entries but no arrays of them is the labels' loss, and
