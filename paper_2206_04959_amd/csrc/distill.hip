@@ -770,7 +770,9 @@ __global__ void __launch_bounds__(NT) distill_bwd_kernel(DistillArgs a, int piec
   }
 }
 
-// Ranks' statistics [ranks][tokens] to the whole vocabulary's, in the ranks' order.
+// Ranks' statistics [ranks][tokens] to the whole vocabulary's, in the ranks' order, summed kJoinRun at
+// a time.
+constexpr int kJoinRun = 256;
 __global__ void __launch_bounds__(256) distill_join_kernel(int tokens, int ranks, float alpha, float tau, float rate_t,
                                                            const float* __restrict__ parts, float* __restrict__ stats,
                                                            float* __restrict__ loss) {
@@ -780,18 +782,26 @@ __global__ void __launch_bounds__(256) distill_join_kernel(int tokens, int ranks
   for (int r = 0; r < ranks; ++r) m = fmaxf(m, parts[((size_t)r * tokens + t) * kDistillStats]);
   const float base = base_of(m);
   Stats s{m, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-  for (int r = 0; r < ranks; ++r) {
-    const Stats p = load_stats(parts + ((size_t)r * tokens + t) * kDistillStats);
-    const float d = moved(p.m, base);
-    s.s1 += p.s1 * exp2_fast(d * kLog2e);
-    s.st += p.st * exp2_fast(d * rate_t);
-    s.lin += p.lin;
-    if (p.mass != 0.0f) s.lin += alpha * tau * p.mass * d;
-    if (p.label != 0.0f) s.lin += (1.0f - alpha) * p.label * d;
-    s.mass += p.mass;
-    s.label += p.label;
-    s.tm = p.tm;
-    s.ts = p.ts;
+  for (int r = 0; r < ranks;) {
+    float s1 = 0.0f, st = 0.0f, lin = 0.0f, mass = 0.0f, label = 0.0f;
+    for (int n = 0; n < kJoinRun && r < ranks; ++n, ++r) {
+      const Stats p = load_stats(parts + ((size_t)r * tokens + t) * kDistillStats);
+      const float d = moved(p.m, base);
+      s1 += p.s1 * exp2_fast(d * kLog2e);
+      st += p.st * exp2_fast(d * rate_t);
+      lin += p.lin;
+      if (p.mass != 0.0f) lin += alpha * tau * p.mass * d;
+      if (p.label != 0.0f) lin += (1.0f - alpha) * p.label * d;
+      mass += p.mass;
+      label += p.label;
+      s.tm = p.tm;
+      s.ts = p.ts;
+    }
+    s.s1 += s1;
+    s.st += st;
+    s.lin += lin;
+    s.mass += mass;
+    s.label += label;
   }
   store_stats(stats + t * kDistillStats, s);
   loss[t] = loss_of(s, alpha, tau);

@@ -438,6 +438,28 @@ def test_numbers_of_tokens(dtype, tokens):
         case.check(case.apart(), "apart")
 
 
+@pytest.mark.parametrize("ranks", [1, 255, 256, 257, 2 ** 16])
+def test_join_of_many_ranks(ranks):
+    """Equal sums, whose roundings all go one way: 1 + half a step of fp32 at 2^15 (less one step at 1) would lose that
+    half in each of the last 2^15 of 2^16 additions in a row.  There are 256 in a row, and 256 of those."""
+    torch = need_gpu()
+    print(f"[distill join] {ranks} ranks", flush=True)
+    T, alpha, tau, each = 300, 0.5, 2.0, 1.0 + 2.0 ** -9 - 2.0 ** -23
+    parts = torch.zeros(ranks, T, 8, device="cuda")
+    parts[:, :, 0] = -3.0
+    parts[:, :, 1:3] = each
+    parts[ranks // 2, :, 3:6] = torch.tensor([-0.5, 1.0, 1.0], device="cuda")  # the entries' rank and the label's
+    parts[:, :, 6:] = torch.tensor([2.5, 1.5], device="cuda")
+    stats, loss = torch.empty(T, 8, device="cuda"), torch.empty(T, device="cuda")
+    B.distill_loss_join(parts, stats, loss, alpha=alpha, temperature=tau)
+    torch.cuda.synchronize()
+    want = np.tile([-3.0, ranks * each, ranks * each, -0.5, 1.0, 1.0, 2.5, 1.5], (T, 1))
+    way = min(ranks, 256) + ranks / 256
+    _close(stats, want, np.array([0, way * U * ranks * 1.01, way * U * ranks * 1.01, 0, 0, 0, 0, 0]), "stats")
+    ref = 0.5 + (alpha * tau ** 2 + 1 - alpha) * np.log(ranks * each)
+    _close(loss, np.full(T, ref), (way + 8) * U * (alpha * tau ** 2 + 1 - alpha) + 8 * U * abs(ref), "loss")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("vocab", [30, 1000, 7000, 53300, 140000])
 def test_offsets_and_masks(dtype, vocab):
