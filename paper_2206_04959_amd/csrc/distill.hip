@@ -62,10 +62,10 @@ __device__ __forceinline__ float teacher_at(const DistillArgs& a, size_t i) {
 }
 
 // A token's entries and its label (entry `top`) in LDS.  For the gradient there is a hash table of
-// their columns too, as an id may be there twice: the column's first and last entry and the sum of
-// its p = exp((t - max) / T) in units of 2^-52, whole numbers, which give the same sum in any order.
-// A column's first entry forms the gradient there, and is listed for the thread that writes the 16
-// bytes around it.
+// their columns too, as an id may be there more than once.  A column's first entry forms the gradient
+// there, and is listed for the thread that writes the 16 bytes around it.  It needs the sum of
+// the column's p = exp((t - max) / T), the same in any order: of two entries it is their fp32 sum, of
+// more (or two and the label) a whole number of units of 2^-44 of the power of two of the largest one.
 struct Slot {
   int col, first, last;
 };
@@ -78,9 +78,10 @@ struct Entry {
 struct Entries {
   Entry* at;
   // gradient only
-  unsigned long long* sum;
+  unsigned long long* sum;  // how many came behind the first one, the label too; then see sum_many
   Slot* slot;
   int* head;    // [threads] the thread's first entry
+  int* many;    // whether more than one came anywhere
   int slots;    // a power of two
 };
 __host__ __device__ constexpr int entry_slots(int top) {
@@ -91,8 +92,9 @@ __host__ __device__ constexpr int entry_slots(int top) {
 __host__ __device__ constexpr size_t entries_bytes(int top, int nt, bool grad) {
   return (size_t)(top + 1) * sizeof(Entry) + (grad ? nt * 4 + (size_t)entry_slots(top) * (8 + sizeof(Slot)) : 0);
 }
-__device__ __forceinline__ Entries entries_in(char* lds, int top, int slots) {
+__device__ __forceinline__ Entries entries_in(char* lds, int* many, int top, int slots) {
   Entries en;
+  en.many = many;
   en.at = reinterpret_cast<Entry*>(lds);
   en.sum = reinterpret_cast<unsigned long long*>(en.at + top + 1);
   en.slot = reinterpret_cast<Slot*>(en.sum + slots);
@@ -109,30 +111,61 @@ __device__ __forceinline__ void clear_table(const Entries& en) {
     en.slot[i] = Slot{-1, 0x7fffffff, -1};
   }
   en.head[threadIdx.x] = -1;
+  if (threadIdx.x == 0) *en.many = 0;
 }
 
-// p in units of 2^-52, 0 <= p <= 1 (what is below 2^-52 of it is cut off).
-__device__ __forceinline__ unsigned long long fixed52(float p) {
-  const uint32_t b = __float_as_uint(p);
-  const int shift = (int)(b >> 23) - 127 + 29;  // 24 significant bits at 2^0 are 2^29 units each
-  const unsigned long long m = (b & 0x7fffffu) | 0x800000u;
-  return shift >= 0 ? m << (shift & 63) : shift > -24 ? m >> (-shift & 31) : 0;
-}
-
-// Entry k, with its p (the label: k = top), into the table.
-__device__ __forceinline__ void into_table(const Entries& en, int top, int k, int c, float p) {
+// Entry k (the label: k = top) into the table.
+__device__ __forceinline__ void into_table(const Entries& en, int top, int k, int c) {
   int h = (int)(((unsigned)c * 2654435761u >> 8) & (unsigned)(en.slots - 1));
   for (;;) {  // there are more slots than entries
     const int was = atomicCAS(&en.slot[h].col, -1, c);
+    if (was == c && atomicAdd(&en.sum[h], 1ull) > 0) *en.many = 1;
     if (was == -1 || was == c) break;
     h = (h + 1) & (en.slots - 1);
   }
   en.at[k].next = h;
   atomicMin(&en.slot[h].first, k);
-  if (k < top) {
-    atomicMax(&en.slot[h].last, k);
-    atomicAdd(&en.sum[h], fixed52(p));
-  }
+  if (k < top) atomicMax(&en.slot[h].last, k);
+}
+
+constexpr int kUnitBits = 44, kSumBits = 56;  // 1024 p below 2^45 units each
+
+__device__ __forceinline__ unsigned long long sum_now(const unsigned long long& sum) {
+  return __hip_atomic_load(&sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+}
+
+// The sums of p (a normal number) of columns where more than one came behind the first, between
+// barriers: the exponent of the largest one goes into the upper 8 bits (more than any number of entries),
+// then all into the others in units of 2^-44 of that (what is below one is cut off: 2^-34 of the sum at most).
+// In units that are the same for all columns the small p of such a column lose their digits, which
+// the gradient has where the student's probability is as small.
+template <int NT>
+__device__ __forceinline__ void sum_many(const Entries& en, int top) {
+  if (!*en.many) return;  // the same for the whole workgroup
+  auto each = [&](auto f) {
+    for (int k = threadIdx.x; k < top; k += NT) {
+      const Entry e = en.at[k];
+      if (e.col >= 0 && sum_now(en.sum[e.next]) > 1) f(en.sum[e.next], __float_as_uint(e.t));
+    }
+    __syncthreads();
+  };
+  each([](unsigned long long& sum, uint32_t p) {
+    atomicMax(&sum, (unsigned long long)(p >> 23 & 255) << kSumBits);
+  });
+  each([](unsigned long long& sum, uint32_t p) {
+    const int most = (int)(sum_now(sum) >> kSumBits);
+    const int shift = kUnitBits - 23 - (most - (int)(p >> 23 & 255));
+    const unsigned long long m = (p & 0x7fffffu) | 0x800000u;
+    atomicAdd(&sum, shift >= 0 ? m << shift : shift > -24 ? m >> -shift : 0);
+  });
+}
+
+// The sum of p of a column with the first entry's p.
+__device__ __forceinline__ float column_sum(const Entries& en, int h, const Slot& at, float p) {
+  if (at.first >= at.last) return p;  // (a label alone has no last)
+  const unsigned long long s = en.sum[h];
+  if (s == 1) return p + en.at[at.last].t;
+  return ldexpf(__ull2float_rn(s & ((1ull << kSumBits) - 1)), (int)(s >> kSumBits) - 127 - kUnitBits);
 }
 
 // 16 bytes of logits as floats; NONE is -infinity in each of them.
@@ -389,6 +422,7 @@ __device__ __forceinline__ void write_zeros(const DistillArgs& a, T* dz, int lo,
 template <typename T, int NT, int M>
 __device__ __forceinline__ void resolve_entries(const DistillArgs& a, const Slopes<M>& f, const Entries& en, float wt,
                                                 float wl, int lo, bool far, float base) {
+  sum_many<NT>(en, a.top);
   const int label = en.at[a.top].col;
   for (int e = threadIdx.x; e <= a.top; e += NT) {
     const Entry own = en.at[e];
@@ -396,7 +430,7 @@ __device__ __forceinline__ void resolve_entries(const DistillArgs& a, const Slop
     if (c < 0) continue;
     const Slot s = en.slot[own.next];
     if (s.first != e) continue;
-    const float p = e == a.top ? 0.0f : s.first == s.last ? own.t : __ull2float_rn(en.sum[own.next]) * 0x1p-52f;
+    const float p = e == a.top ? 0.0f : column_sum(en, own.next, s, own.t);
     const float g = f.of(far ? own.z - base : own.z) - (wt * p + (c == label ? wl : 0.0f));
     en.at[e].z = __uint_as_float(bits_of(g, T()));
     en.at[e].next = atomicExch(&en.head[(c - lo) / Vec<T>::N % NT], e);
@@ -453,8 +487,8 @@ __device__ __forceinline__ Stats token_stats(const DistillArgs& a, const Entries
   }
   if (GRAD) {  // (in a loop of its own: both at once need registers that the row has)
     for (int k = threadIdx.x; k < a.top; k += NT)
-      if (en.at[k].col >= 0) into_table(en, a.top, k, en.at[k].col, en.at[k].t);
-    if (threadIdx.x == 0 && en.at[a.top].col >= 0) into_table(en, a.top, a.top, en.at[a.top].col, 0.0f);
+      if (en.at[k].col >= 0) into_table(en, a.top, k, en.at[k].col);
+    if (threadIdx.x == 0 && en.at[a.top].col >= 0) into_table(en, a.top, a.top, en.at[a.top].col);
   }
   reduce_behind_barrier<AddOp, NT>(s, red);
   Stats r;
@@ -481,7 +515,8 @@ __global__ void __launch_bounds__(NT) distill_kernel(DistillArgs a, const T* z, 
                                                      float* __restrict__ loss, const float* __restrict__ dloss, T* dz) {
   extern __shared__ __align__(16) char smem[];
   __shared__ float red[2][NT / 64 * 6];
-  const Entries en = entries_in(smem, a.top, GRAD ? a.slots : 0);
+  __shared__ int many;
+  const Entries en = entries_in(smem, &many, a.top, GRAD ? a.slots : 0);
   if (GRAD) clear_table<NT>(en);
   const size_t row = blockIdx.x;
   const T* zr = z + row * a.ld;
@@ -611,7 +646,8 @@ __global__ void __launch_bounds__(NT) distill_row_kernel(DistillArgs a, const T*
   extern __shared__ __align__(16) char smem[];
   __shared__ float red[2][NT / 64 * 6];
   constexpr int N = Vec<T>::N;
-  const Entries en = entries_in(smem, a.top, a.slots);
+  __shared__ int many;
+  const Entries en = entries_in(smem, &many, a.top, a.slots);
   clear_table<NT>(en);
   const size_t row = blockIdx.x;
   const T* zr = z + row * a.ld;
@@ -712,7 +748,8 @@ __global__ void __launch_bounds__(NT) distill_bwd_kernel(DistillArgs a, int piec
                                                          const float* __restrict__ dloss, T* dz) {
   extern __shared__ __align__(16) char smem[];
   constexpr int N = Vec<T>::N, piece = NT * N * U;
-  const Entries en = entries_in(smem, a.top, a.slots);
+  __shared__ int many;
+  const Entries en = entries_in(smem, &many, a.top, a.slots);
   const size_t row = blockIdx.x / pieces;
   const int lo = (int)(blockIdx.x % pieces) * piece, hi = min(lo + piece, a.ld);
   const T* zr = z + row * a.ld;
@@ -747,7 +784,7 @@ __global__ void __launch_bounds__(NT) distill_bwd_kernel(DistillArgs a, int piec
     if (c < 0) continue;
     en.at[k].t = p;
     en.at[k].z = Elem<T>::to_f(zr[c]);
-    into_table(en, a.top, k, c, p);
+    into_table(en, a.top, k, c);
   }
   __syncthreads();  // the entries' logits are read, too: dz may be z
   const bool far = is_far(s.m);

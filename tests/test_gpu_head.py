@@ -438,6 +438,41 @@ def test_numbers_of_tokens(dtype, tokens):
         case.check(case.apart(), "apart")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("vocab,top", [(60, 12), (2500, 12), (9000, 300), (27000, 40), (140000, 12), (3000, 1024)])
+@pytest.mark.parametrize("tau", [1.0, 2.0, 3.0])
+def test_repeated_ids_of_small_probability(dtype, vocab, top, tau):
+    """An id that is there twice or more, with logits 30 to 60 T below the teacher's largest, and a student whose
+    logit there is as low: the gradient there is that of the sum of its probabilities, in all its digits."""
+    torch = need_gpu()
+    print(f"[distill repeats] {dtype} vocab {vocab} top {top} T {tau}", flush=True)
+
+    def change(self, z, t, w):
+        low = [5, 17, 29, 41, 53]
+        z[:, low] = -400.0
+        w[:] = 1.0
+        for i in range(8):
+            self.lab[i] = 3 if i else 17    # (a label there, too)
+            t[i] = -tau * np.linspace(0.0, 60.0, top)
+            at = 100 + np.arange(top) if vocab > top + 100 else 50 - np.arange(top) % 4 * 2
+            n = 5 if top > 20 else 3
+            for k, c in enumerate(low[:n]):  # two entries each, or many; far apart or not
+                at[top // 2 + k::n] = c
+            if i % 2:
+                t[i, top // 2 + i % 5::2] -= 20.0 * tau
+            order = np.random.default_rng(i).permutation(top)
+            self.at[i], t[i] = at[order], t[i][order]
+
+    case = _Loss(torch, dtype, 9, vocab, top, 0.5, tau, teacher="fp32", change=change)
+    _, _, m = O.distill(case.zv, case.at, case.tv, case.lab, 0.5, tau)
+    # a p is off by two roundings of its exponent, up to 80 (in steps of e)
+    case.grad_tol = case.grad_tol + 4 * 80 * U * m["minus"] * np.abs(case.wv)[:, None]
+    small = np.abs(case.grad[:8][:, [5, 29]])
+    assert (0 < small).all() and small.max() < 2.0 ** -38
+    for got, what in ((case.whole(), "both"), (case.apart(), "apart"), (case.shares(2), "shares")):
+        case.check(got, what)
+
+
 @pytest.mark.parametrize("ranks", [1, 255, 256, 257, 2 ** 16])
 def test_join_of_many_ranks(ranks):
     """Equal sums, whose roundings all go one way: 1 + half a step of fp32 at 2^15 (less one step at 1) would lose that
