@@ -942,14 +942,14 @@ static hipError_t run_kept(const DistillCall& c) {
 // threads (108 with 256), loss and gradient 197 with 128 (252 with 256).  Few rows have more: what
 // counts then is how long one takes (32 x 6288 8.0 us with 512, 9.7 with 128; 200 x 25152
 // 11.7 with 512, 14.0 with 256; 700 x 25152 22.9 and 23.9).  So have rows with many entries, whose
-// table leaves room for fewer workgroups in a CU from 205 and from 410 entries on.  Loss and
+// table leaves room for fewer workgroups in a CU from 204 and from 409 entries on.  Loss and
 // gradient of 8192 x 3496: with 192 entries 63 us on 128 threads and 64 on 256, with 256 72 and
 // 61; on 256 and 512 with 408 entries 83 and 94, with 512 86 and 83, with 1024 235 and 160.  The loss
 // alone, of 8192 x 1000: 256 entries 14.6 us on 64 threads and 17.9 on 128, 512 28.5 and 24.3,
 // 768 35.3 on 128 and 31.6 on 256; of 8192 x 6288 512 entries 54 on 128 and 41 on 256; of 8192 x 12568
 // 1024 entries 93 on 256 and 78 on 512.
-static bool many_entries(int top) { return entry_slots(top) >= 512; }       // 205 and more
-static bool most_entries(int top) { return entry_slots(top) >= 1024; }      // 410 and more
+static bool many_entries(int top) { return entry_slots(top) >= 512; }       // 204 and more
+static bool most_entries(int top) { return entry_slots(top) >= 1024; }      // 409 and more
 
 static int loss_threads(int n, int top) {
   if (n <= 256) return top <= 256 ? 64 : top <= 512 ? 128 : 256;

@@ -416,6 +416,37 @@ def test_many_entries(dtype, top):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("top", [24, 25, 50, 51, 101, 102, 203, 204, 408, 409, 818, 819, 1024])
+@pytest.mark.parametrize("clash", [False, True])
+def test_fullest_tables(dtype, top, clash):
+    """Most entries that a table of each size has (four fifths of its slots, less one), and one more, which has
+    the next size (so have the rules for rows with many entries, at 204, 409 and 819).  With `clash` all columns begin their
+    search in the table's last two slots, so that it goes on from its start, past many others."""
+    torch = need_gpu()
+    slots = 32
+    while 4 * slots < 5 * (top + 1):
+        slots *= 2
+    for tokens, vocab in ((5, 4097), (5, 8192), (5, 28672), (5, 60000), (1025, 3500), (5, 140000)):
+        print(f"[distill tables] {dtype} top {top} clash {clash} tokens {tokens} vocab {vocab}", flush=True)
+
+        def change(self, z, t, w):
+            if not clash:
+                return
+            c = np.arange(vocab, dtype=np.uint64)
+            home = ((c * 2654435761 & 0xffffffff) >> 8) & (slots - 1)
+            c = c[home >= slots - 2]
+            rng = np.random.default_rng(top)
+            for i in range(tokens):
+                if i not in (2, 3):
+                    self.at[i] = rng.choice(c, top, replace=len(c) < top)
+            self.lab[0] = self.at[0, top // 2]
+
+        case = _Loss(torch, dtype, tokens, vocab, top, 0.5, 2.0, change=change)
+        case.check(case.whole(), "both")
+        case.check(case.apart(), "apart")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("ranks", [1, 2, 3, 8])
 @pytest.mark.parametrize("alpha,tau", [(0.5, 2.0), (0.6, 3.0), (1.0, 1.0), (0.0, 1.0)])
 def test_shares_of_the_vocabulary(dtype, ranks, alpha, tau):
