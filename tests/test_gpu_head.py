@@ -617,6 +617,48 @@ def test_nonfinite_rows_stay_alone(dtype, vocab):
     assert np.isfinite(_f64(one.whole()[0])[3:5]).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("tokens", [12, 1030])
+@pytest.mark.parametrize("vocab", [30, 1001, 2047, 3500, 4100, 7001, 13300, 26700, 50257, 77000, 102000, 131001, 140001])
+def test_gradient_in_the_place_of_the_logits(dtype, tokens, vocab):
+    """Both calls that may write the gradient over the logits, in every layout of a row, give the bits that they give
+    apart: ordinary rows, rows far from 0, masked ones, NaN, tokens without anything and without weight."""
+    torch = need_gpu()
+    if tokens * vocab > 3e7:
+        pytest.skip("the layouts of few and of many rows part below 3584 chunks")
+    print(f"[distill in place] {dtype} tokens {tokens} vocab {vocab}", flush=True)
+    dt, bits = _type(torch, dtype), torch.int16 if dtype == "bf16" else torch.int32
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(vocab)
+    ld, top = -(-vocab // 8) * 8 + 8, 20
+    z = (3 * torch.randn(tokens, ld, device="cuda", generator=gen)).to(dt)
+    z[1] += 2.0 ** 20
+    z[2, 1::2] = -float("inf")
+    z[3] = torch.finfo(dt).min
+    z[4] = float("nan")
+    ids = torch.randint(0, vocab, (tokens, top), device="cuda", generator=gen)
+    ids[5], ids[6, ::2] = -1, ids[6, 1]
+    lab = torch.randint(0, vocab, (tokens,), device="cuda", generator=gen)
+    lab[5], w = -100, torch.rand(tokens, device="cuda", generator=gen)
+    w[7] = 0.0
+    for alpha, tau in ((0.5, 2.0), (0.4, 3.0)):
+        kw = dict(teacher_ids=ids, teacher_logits=torch.randn(tokens, top, device="cuda", generator=gen), labels=lab, alpha=alpha,
+                  temperature=tau, vocab=vocab)
+        loss, loss2, stats = torch.empty(tokens, device="cuda"), torch.empty(tokens, device="cuda"), torch.empty(tokens, 8, device="cuda")
+        apart, place = torch.empty_like(z), z.clone()
+        B.distill_loss_fwd_bwd(z, w, loss, apart, **kw)
+        B.distill_loss_fwd_bwd(place, w, loss2, place, **kw)
+        assert torch.equal(loss.view(torch.int32), loss2.view(torch.int32))
+        assert torch.equal(apart.view(bits), place.view(bits))
+        B.distill_loss_fwd(z, stats, **kw)
+        B.distill_loss_bwd(z, stats, w, apart, **kw)
+        place.copy_(z)
+        B.distill_loss_bwd(place, stats, w, place, **kw)
+        torch.cuda.synchronize()
+        assert torch.equal(apart.view(bits), place.view(bits))
+        assert not apart[:, vocab:].any()
+
+
 @pytest.mark.parametrize("ranks", [1, 3])
 def test_ids_far_outside_the_vocabulary(ranks):
     """Ids and labels at the ends of 64 bits, and around a share's ends, are no entries."""
