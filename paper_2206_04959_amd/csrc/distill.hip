@@ -17,10 +17,12 @@
 //
 // Bound by memory: the logits are read once (maximum and sums in one pass, the sums rescaled
 // when the maximum grows), the gradient is written once.  8192 x 50304 in bf16 with 64 entries, T =
-// 2: loss 142 us (5.8 TB/s, reading only; a large copy has 5.1 both ways), loss and gradient 295
-// (5.6), gradient from the statistics 270 (6.1); in fp32 half the rows take 140, 298 and 270.  Three
-// quarters of the loss's time the vector units are busy too: two exponentials a logit.  Sums are
-// fp32, each value of the gradient is formed in fp32 and rounded once, nothing depends on timing.
+// 2, the kernels in passes over changing inputs: loss 142 us (5.8 TB/s, reading only; a large copy has
+// 5.1 both ways), loss and gradient 302 (5.5); called one after another on buffers in turn: loss with
+// statistics 164, loss and gradient 294, gradient from the statistics 269 (6.1), in fp32 on half
+// the rows 152, 301 and 270.  Three quarters of the loss's time the vector units are busy too: two
+// exponentials a logit.  Sums are fp32, of no more than some hundred terms in a row, each value of
+// the gradient is formed in fp32 and rounded once, nothing depends on timing.
 #include <algorithm>
 
 #include "common.h"
@@ -253,8 +255,9 @@ __device__ __forceinline__ float near_base(float m) { return m == -INFINITY ? 0.
 
 // The two exponentials, exp((z - base) / T) and exp(z - base): ONE is enough where the loss needs
 // one or T = 1, at T = 2 and T = 4 the second is the first's square or its square's (their c and
-// off are exact multiples then), else there are TWO.  In bf16 the second one is a quarter of the
-// work: loss of 8192 x 50304 165 us with both (T = 3), 144 so.
+// off are exact multiples then; the first's relative error is doubled or taken four times), else
+// there are TWO.  In passes over changing inputs the loss of 8192 x 50304 in bf16 takes 142 us at T = 2,
+// 166 with both (T = 3).
 enum Sums { ONE = 0, TWO = 1, SQUARE = 2, FOURTH = 4 };
 template <int M>
 struct Exponents {
@@ -416,9 +419,9 @@ __device__ __forceinline__ void write_zeros(const DistillArgs& a, T* dz, int lo,
 // are whole behind the next one.  A column's place in a list is the one thing that depends on
 // timing, and it changes nothing.  wt: weight of p, wl: of the label.
 // (Written by a store of its own behind that of the 16 bytes, each entry cost a part of a line once
-// more: loss and gradient of 32768 x 6288 with 64 entries 266 us, 201 so.  Looking for
-// repeated ids by comparing every pair instead of a table: 8192 x 50304 with 256 entries 409 us,
-// with 1024 1697; so 300 and 501.)
+// more: loss and gradient of 32768 x 6288 with 64 entries 266 us, 201 so, in the form of that time
+// (now 180).  Looking for repeated ids by comparing every pair instead of a table: 8192 x 50304 with
+// 256 entries 409 us, with 1024 1697; so 307 and 500.)
 template <typename T, int NT, int M>
 __device__ __forceinline__ void resolve_entries(const DistillArgs& a, const Slopes<M>& f, const Entries& en, float wt,
                                                 float wl, int lo, bool far, float base) {
@@ -938,16 +941,18 @@ static hipError_t run_kept(const DistillCall& c) {
 }
 
 // Threads for a row of n chunks of 16 bytes.  A short row has few threads, so that as many bytes
-// are on their way in a CU as its registers hold: 32768 x 6288 (n = 786) loss 88 us with 128
-// threads (108 with 256), loss and gradient 197 with 128 (252 with 256).  Few rows have more: what
-// counts then is how long one takes (32 x 6288 8.0 us with 512, 9.7 with 128; 200 x 25152
-// 11.7 with 512, 14.0 with 256; 700 x 25152 22.9 and 23.9).  So have rows with many entries, whose
-// table leaves room for fewer workgroups in a CU from 204 and from 409 entries on.  Loss and
-// gradient of 8192 x 3496: with 192 entries 63 us on 128 threads and 64 on 256, with 256 72 and
-// 61; on 256 and 512 with 408 entries 83 and 94, with 512 86 and 83, with 1024 235 and 160.  The loss
-// alone, of 8192 x 1000: 256 entries 14.6 us on 64 threads and 17.9 on 128, 512 28.5 and 24.3,
-// 768 35.3 on 128 and 31.6 on 256; of 8192 x 6288 512 entries 54 on 128 and 41 on 256; of 8192 x 12568
-// 1024 entries 93 on 256 and 78 on 512.
+// are on their way in a CU as its registers hold: 32768 x 6288 (n = 786) loss 90 us with 128
+// threads (108 with 256), loss and gradient 178 with 128 (202 with 256; in fp32, where a row has half
+// the columns, 191 and 168).  Few rows have more: what counts then is how long one takes (32 x 6288
+// 7.7 us with 512, 8.9 with 128; 200 x 25152 11.4 with 512, 13.5 with 256; 700 x 25152 22.6 and
+// 23.4).  So have rows with many entries, whose table leaves room for fewer workgroups in a CU from 204
+// and from 409 entries on.  Loss and gradient of 8192 x 3496: with 203 entries 67 us on 128
+// threads and on 256, with 204 66 and 57; on 256 and 512 with 408 entries 83 and 101, with 409
+// 75 and 73, with 1024 228 and 157.  (On 64 threads, which these rows have up to 203 entries, 64
+// entries take 39 us, 47 on 128; 128 take 54 and 50, 203 78 and 67.)  The loss alone, of 8192 x
+// 1000: 256 entries 14.6 us on 64 threads and 18.3 on 128, 512 28.9 and 24.6, 768 36 on 128 and 32 on
+// 256; of 8192 x 6288 512 entries 58 on 128 and 41 on 256; of 8192 x 12568 1000 entries 98 on 256 and 77
+// on 512.
 static bool many_entries(int top) { return entry_slots(top) >= 512; }       // 204 and more
 static bool most_entries(int top) { return entry_slots(top) >= 1024; }      // 409 and more
 
@@ -977,7 +982,7 @@ static hipError_t run_forward(const DistillCall& c) {
   if (n <= 256) return run_kept<T, 64, 4, M>(c);
   if (n <= 512) return run_kept<T, 64, 8, M>(c);
   if (n <= 896) return run_kept<T, 128, 7, M>(c);
-  if (n <= 1792) return run_kept<T, 256, 7, M>(c);  // 4096 x 12568, 64 entries 51 us (55 with 128 x 13)
+  if (n <= 1792) return run_kept<T, 256, 7, M>(c);  // 4096 x 12568, 64 entries 52 us (57 with 128 x 13)
   if (n <= 3328) return run_kept<T, 256, 13, M>(c);
   if (n <= 6656) return run_kept<T, 512, 13, M>(c);
   if (n <= 9728) return run_kept<T, 512, 19, M>(c);
@@ -999,10 +1004,11 @@ static hipError_t run_pieces(const DistillCall& c) {
 }
 
 // Threads and pieces of a row of n chunks.  Many entries: as above (4096 x 6288 with 256 entries
-// 47 us on 128 threads and 38 on 256; 8192 x 1000 with 1024 184 on 256 and 133 on 512; 2048 x 25152
-// with 512 69 on 256 and 60 on 512).  One piece a row up to 3328 chunks; longer ones are cut small
-// (8192 x 50304 268 us with U = 4, 302 with 13), and so are few rows (1 x 50304 8.0 and 9.6), but
-// for a number of rows that fills the card once in large pieces (600 x 50304 29.0 and 24.7).
+// 46 us on 128 threads and 35 on 256, with 203 43 and 41; 8192 x 1000 with 1000 199 on 256 and 140 on
+// 512; 2048 x 25152 with 512 71 on 256 and 59 on 512).  One piece a row up to 3328 chunks; longer ones are
+// cut small (8192 x 50304 276 us with U = 4, 304 with 13), and so are few rows (300 x 12800 9.5 and
+// 11.5, but 300 x 50304 18.0 and 16.7), but for a number of rows that fills the card once in large
+// pieces (600 x 50304 28.9 and 25.6).
 template <typename T, int M>
 static hipError_t run_backward(const DistillCall& c) {
   const int n = c.q.ld / Vec<T>::N, tokens = c.q.tokens, top = distill_args(c.q).top;

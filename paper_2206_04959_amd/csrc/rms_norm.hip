@@ -14,7 +14,7 @@
 // Bound by memory.  A row stays in the registers of its NT threads, CH chunks of 8 features
 // each: chunk i of thread j holds the features from (j + NT i) * 8 on.  In bf16 with a residual:
 // 32768 x 6144 262 us (6.1 TB/s; a large copy has 5.1), 16384 x 1920 with y and its 8 bits 54
-// (5.3); gradients of 16384 x 6144 139 (5.8), of 4097 x 1600 13 and 4 for the gain (4.1).
+// (5.3); gradients of 16384 x 6144 139 (5.8), of 4097 x 1600 13.6 and 4 for the gain (3.9).
 #include <algorithm>
 
 #include "act8_codes.h"
